@@ -256,6 +256,37 @@ spice_status spice_moe_layer_fwd_fp8(spice_ctx *ctx, const spice_layer_weights_f
                                      int32_t *resid_tok, int32_t *resid_k, int32_t *resid_expert,
                                      float *resid_gate, void *stream);
 
+/* ---- Steps next to the layer: the norm between two layers, a dense FFN in 8-bit integers, routing by scores ----
+ * What the paper's decode loop runs beside the offloaded experts: the residual stream is normalised before the next
+ * layer, the always-on shared expert (or a dense FFN) runs at any batch size with 8-bit integer weights and activations,
+ * and models whose routers are not plain softmax top-k get their idx / gate from logits.  None of these calls needs a
+ * spice_ctx or a workspace; the GPU is the calling thread's current device; all of them can be captured into a graph.
+ * Used together: spice_residual_rmsnorm -> h, (q, scale);  spice_route_topk(h) -> logits;  spice_route_scored -> idx, gate
+ * for spice_classify_misses and spice_grouped_expert_ffn;  spice_swiglu_i8(q) -> act;  spice_quantize_i8_rows(act);
+ * spice_gemm_i8 -> y fp32 (SPICE_OUT_F32_ADD: into the sum of the routed experts), the next norm's delta_f32. */
+
+/* Residual addition and root-mean-square norm, for every token t:
+ *     s = bf16(x_resid + delta) (added in fp32),   x_resid <- s,   r = 1 / sqrt(mean_j s_j^2 + eps)
+ *     h_j = bf16(s_j * weight_j * r)
+ *     m = max_j |s_j * weight_j|,   q_j = 127 s_j weight_j / m to the nearest integer (ties to even),   scale = m * r / 127
+ * so q_j * scale stands for the normalised value before its rounding to bf16.  The codes do not depend on r and are
+ * rounded exactly.
+ *   x_resid [T,d] bf16, in/out (only read without a delta).  delta [T,d] bf16 or delta_f32 [T,d] fp32: one of them, or
+ *   neither (the norm of the stream as it is); it must not overlap x_resid.  weight [d] bf16.  eps >= 0.
+ *   h [T,d] bf16 out, q [T,d] int8 out with scale [T] fp32 out: either may be NULL, not both.
+ *   A row of zeros has codes 0 and scale 1.  A row with a value that is not finite (or a product s_j * weight_j, or
+ *   r, beyond fp32) has codes 0 and scale NaN; its h is what the formula gives.
+ *   d a multiple of 8 up to 32768 (SPICE_ERR_UNSUPPORTED_SHAPE above); q 8-byte aligned, the other arrays of rows 16-byte. */
+spice_status spice_residual_rmsnorm(spice_bf16 *x_resid, const spice_bf16 *delta, const float *delta_f32,
+                                    const spice_bf16 *weight, float eps, int32_t T, int32_t d, spice_bf16 *h, int8_t *q,
+                                    float *scale, void *stream);
+
+/* 8-bit integer rows of a bf16 matrix w [rows, cols] (weights once; activations every step):
+ *     m = max_j |w[r,j]|,   q[r,j] = 127 w[r,j] / m to the nearest integer (ties to even, rounded exactly),   scale[r] = m / 127
+ * Rows of zeros and rows with a value that is not finite as in spice_residual_rmsnorm.  cols a multiple of 8 up to 32768,
+ * rows below 2^31 (SPICE_ERR_UNSUPPORTED_SHAPE above); w 16-byte, q 8-byte aligned. */
+spice_status spice_quantize_i8_rows(const spice_bf16 *w, int64_t rows, int32_t cols, int8_t *q, float *scale, void *stream);
+
 /* The resident-expert FFN for callers that cannot allocate (the paper has no counterpart: this is
  * a packaging variant of spice_grouped_expert_ffn, not a step of the method).
  *

@@ -66,6 +66,10 @@ def lib() -> C.CDLL:
                      "spice_grouped_expert_ffn_static", "spice_draft_confidence", "spice_prefetch_rollout",
                      "spice_quantize_e4m3_rows", "spice_moe_layer_fwd_fp8"):
             getattr(L, name).restype = C.c_int
+        i32, i64, f32, ptr = C.c_int32, C.c_int64, C.c_float, C.c_void_p
+        for name, args in (("spice_residual_rmsnorm", [ptr, ptr, ptr, ptr, f32, i32, i32, ptr, ptr, ptr, ptr]),
+                           ("spice_quantize_i8_rows", [ptr, i64, i32, ptr, ptr, ptr])):
+            getattr(L, name).argtypes, getattr(L, name).restype = args, C.c_int
         L.spice_static_scratch_bytes.restype = C.c_size_t
         L.spice_lore_calibrate.restype = C.c_int
         L.spice_lore_calibrate_workspace_bytes.restype = C.c_size_t
@@ -251,6 +255,65 @@ def spice_moe_layer_fwd_fp8(ctx, weights: "LayerWeightsFp8C", h, conf, T, y, y_c
                                          _ptr(resid_tok, torch.int32), _ptr(resid_k, torch.int32),
                                          _ptr(resid_expert, torch.int32), _ptr(resid_gate, torch.float32),
                                          _stream(stream)), "spice_moe_layer_fwd_fp8")
+
+
+# ---- steps next to the layer: no ctx; shapes are read off the tensors and checked, the call goes to the tensors' device
+
+
+def _addr(what: str, t: Optional[torch.Tensor], dtype, shape, dev) -> Optional[int]:
+    """Device address of a tensor of this type and shape on this device (or in pinned host memory); None for None."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous() or not (t.device == dev or t.is_pinned()):
+        raise SpiceError(f"{what}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {dev}, got {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}")
+    return t.data_ptr()
+
+
+def _rows_of(what: str, t: torch.Tensor):
+    """(rows, columns, device) of the 2-D CUDA tensor that gives a call its sizes."""
+    if t.dim() != 2 or not t.is_cuda:
+        raise SpiceError(f"{what}: expected a 2-D CUDA tensor, got shape {tuple(t.shape)} on {t.device}")
+    if t.shape[0] > 0x7fffffff or t.shape[1] > 0x7fffffff:
+        raise SpiceError(f"{what}: too many rows or columns: {tuple(t.shape)}")
+    return t.shape[0], t.shape[1], t.device
+
+
+def _call_on(dev: torch.device, name: str, stream, *args) -> None:
+    st = (torch.cuda.current_stream(dev) if stream is None else stream).cuda_stream
+    if dev.index == torch.cuda.current_device():
+        code = getattr(lib(), name)(*args, st)
+    else:
+        with torch.cuda.device(dev):
+            code = getattr(lib(), name)(*args, st)
+    if code != SPICE_OK:
+        _check(code, name)
+
+
+def spice_residual_rmsnorm(x_resid, weight, eps, q=None, scale=None, h=None, delta=None, stream=None) -> None:
+    """x_resid [T,d] bf16 (in/out), delta [T,d] bf16 or fp32 or None, weight [d] bf16 -> h [T,d] bf16 and / or q [T,d] int8
+    with scale [T] fp32."""
+    f = "spice_residual_rmsnorm"
+    T, d, dev = _rows_of(f, x_resid)
+    bf, f32 = torch.bfloat16, torch.float32
+    wide = delta is not None and delta.dtype == f32
+    if (q is None) != (scale is None):
+        raise SpiceError(f"{f}: q and scale are given together")
+    _call_on(dev, f, stream, _addr(f, x_resid, bf, (T, d), dev), None if wide else _addr(f, delta, bf, (T, d), dev),
+             _addr(f, delta, f32, (T, d), dev) if wide else None, _addr(f, weight, bf, (d,), dev), eps, T, d,
+             _addr(f, h, bf, (T, d), dev), _addr(f, q, torch.int8, (T, d), dev), _addr(f, scale, f32, (T,), dev))
+
+
+def spice_quantize_i8_rows(w, q, scale, stream=None) -> None:
+    """w [..., cols] bf16 -> q (int8, same shape) and scale (fp32, shape without the last axis)."""
+    f = "spice_quantize_i8_rows"
+    if w.dim() < 1 or not w.is_cuda:
+        raise SpiceError(f"{f}: expected a CUDA tensor, got shape {tuple(w.shape)} on {w.device}")
+    cols, dev = w.shape[-1], w.device
+    if cols < 1 or cols > 0x7fffffff:
+        raise SpiceError(f"{f}: unsupported row length {cols}")
+    _call_on(dev, f, stream, _addr(f, w, torch.bfloat16, w.shape, dev), w.numel() // cols, cols,
+             _addr(f, q, torch.int8, w.shape, dev), _addr(f, scale, torch.float32, w.shape[:-1], dev))
 
 
 # ------------------------------------------------------------------ convenience wrappers

@@ -1,8 +1,7 @@
 // C ABI of libspice: argument checking, workspace ownership and kernel dispatch.
 #include <new>
 
-#include <nvtx3/nvToolsExt.h>
-
+#include "entry.cuh"
 #include "spice_internal.cuh"
 
 using namespace spice;
@@ -46,17 +45,6 @@ struct spice_ctx {
 };
 
 namespace {
-
-// NVTX range around the host side of an entry point (named after it): a profiler's timeline shows which call enqueued
-// which kernels; without a profiler attached the calls return at once.
-struct Range {
-    explicit Range(const char *name) { nvtxRangePushA(name); }
-    ~Range() { nvtxRangePop(); }
-    Range(const Range &) = delete;
-    Range &operator=(const Range &) = delete;
-};
-
-inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 struct Carver {
     char *base;

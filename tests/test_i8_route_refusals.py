@@ -1,0 +1,50 @@
+"""Host-side checks of the steps next to the layer (residual norm, 8-bit integer rows and products, routing by scores): every
+refusal answers without a device and launches nothing; a call without rows is fine."""
+import pytest
+import torch
+
+from paper_2608_21240_b200 import binding as B
+
+OK, INVALID, SHAPE = 0, 1, 2
+P, Q = 4096, 8192          # 16-byte aligned stand-ins for device addresses: no refused call reads them
+BIG = 1 << 20
+
+
+def norm(x=P, delta=None, delta32=None, weight=P, eps=1e-6, T=1, d=64, h=P, q=P, scale=P):
+    return B.lib().spice_residual_rmsnorm(x, delta, delta32, weight, eps, T, d, h, q, scale, None)
+
+
+def test_residual_rmsnorm_refusals():
+    assert norm(T=0) == OK and norm(T=0, x=None) == OK
+    for bad in (dict(T=-1), dict(d=0), dict(d=12), dict(d=-8), dict(eps=-1.0), dict(eps=float("nan")), dict(h=None, q=None),
+                dict(scale=None), dict(delta=P, delta32=P), dict(x=None), dict(weight=None), dict(x=P + 8), dict(delta=P + 2),
+                dict(delta32=P + 4), dict(weight=P + 2), dict(h=P + 8), dict(q=P + 4), dict(scale=P + 2)):
+        assert norm(**bad) == INVALID, bad
+    assert norm(d=32776) == SHAPE
+
+
+def rows(w=P, n=1, cols=64, q=P, scale=P):
+    return B.lib().spice_quantize_i8_rows(w, n, cols, q, scale, None)
+
+
+def test_quantize_i8_rows_refusals():
+    assert rows(n=0) == OK
+    for bad in (dict(n=-1), dict(cols=0), dict(cols=9), dict(w=None), dict(q=None), dict(scale=None), dict(w=P + 8), dict(q=P + 4),
+                dict(scale=P + 1)):
+        assert rows(**bad) == INVALID, bad
+    assert rows(cols=32776) == SHAPE and rows(n=1 << 31) == SHAPE
+
+
+def test_binding_refuses_host_tensors_and_wrong_shapes():
+    bf, i8, f32 = torch.bfloat16, torch.int8, torch.float32
+    z = lambda *s, dtype: torch.zeros(*s, dtype=dtype)  # noqa: E731
+    with pytest.raises(B.SpiceError):
+        B.spice_residual_rmsnorm(z(2, 8, dtype=bf), z(8, dtype=bf), 1e-6, z(2, 8, dtype=i8), z(2, dtype=f32))
+    with pytest.raises(B.SpiceError):
+        B.spice_quantize_i8_rows(z(2, 8, dtype=bf), z(2, 8, dtype=i8), z(2, dtype=f32))
+    dev = torch.device("cuda", 0)
+    for t, dtype, shape in ((z(2, 8, dtype=bf), bf, (2, 8)), (z(2, 8, dtype=bf), f32, (2, 8)), (z(2, 8, dtype=bf), bf, (2, 4)),
+                            (z(8, 2, dtype=bf).t(), bf, (2, 8))):
+        with pytest.raises(B.SpiceError, match="f: expected a contiguous"):
+            B._addr("f", t, dtype, shape, dev)
+    assert B._addr("f", None, bf, (2, 8), dev) is None
