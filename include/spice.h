@@ -287,6 +287,26 @@ spice_status spice_residual_rmsnorm(spice_bf16 *x_resid, const spice_bf16 *delta
  * rows below 2^31 (SPICE_ERR_UNSUPPORTED_SHAPE above); w 16-byte, q 8-byte aligned. */
 spice_status spice_quantize_i8_rows(const spice_bf16 *w, int64_t rows, int32_t cols, int8_t *q, float *scale, void *stream);
 
+/* Routing by scores, from router logits [T, n_experts] fp32 (e.g. the optional output of spice_route_topk):
+ *     score_e = softmax(logits)_e or 1 / (1 + exp(-logits_e));   key_e = score_e + bias_e
+ *     the top_k experts with the largest keys, in that order, equal keys towards the smaller index -> idx [T, top_k] int32
+ *     gate_k = scale * score_k (without the bias), or with norm_topk scale * score_k / (sum of the winners' scores)
+ * Without a bias (NULL) the order is that of the logits.  bias [n_experts] fp32 balances the load and changes no weight.
+ *   n_groups > 1: the experts form n_groups equal runs of consecutive indices; a group's value is its largest key
+ *   (SPICE_GROUP_MAX) or the sum of its two largest score_e + bias_e (SPICE_GROUP_TOP2; of a group with one available
+ *   expert, that one's); only the experts of the top_groups best groups (equal values towards the smaller index) take part.
+ *   An expert whose logit is NaN or -infinity, or whose bias is, is unavailable: behind every other one, score 0 (it is
+ *   still returned, with gate 0, where too few others are left); a group without an available expert comes last.
+ *   Where the winners' scores sum to 0, norm_topk gives gates of 0.
+ *   Selection compares the exact values: experts that fp32 cannot tell apart are compared in fp64.
+ *   1 <= n_experts <= 1024, n_experts a multiple of n_groups, n_groups <= 32, 1 <= top_groups <= n_groups,
+ *   1 <= top_k <= 32 and at most the experts of top_groups groups (SPICE_ERR_UNSUPPORTED_SHAPE otherwise). */
+enum { SPICE_SCORE_SOFTMAX = 0, SPICE_SCORE_SIGMOID = 1 };
+enum { SPICE_GROUP_MAX = 0, SPICE_GROUP_TOP2 = 1 };
+spice_status spice_route_scored(const float *logits, const float *bias, int32_t T, int32_t n_experts, int32_t top_k,
+                                int32_t score, int32_t n_groups, int32_t top_groups, int32_t group_score, int32_t norm_topk,
+                                float scale, int32_t *idx, float *gate, void *stream);
+
 /* The resident-expert FFN for callers that cannot allocate (the paper has no counterpart: this is
  * a packaging variant of spice_grouped_expert_ffn, not a step of the method).
  *

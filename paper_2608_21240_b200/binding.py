@@ -68,7 +68,8 @@ def lib() -> C.CDLL:
             getattr(L, name).restype = C.c_int
         i32, i64, f32, ptr = C.c_int32, C.c_int64, C.c_float, C.c_void_p
         for name, args in (("spice_residual_rmsnorm", [ptr, ptr, ptr, ptr, f32, i32, i32, ptr, ptr, ptr, ptr]),
-                           ("spice_quantize_i8_rows", [ptr, i64, i32, ptr, ptr, ptr])):
+                           ("spice_quantize_i8_rows", [ptr, i64, i32, ptr, ptr, ptr]),
+                           ("spice_route_scored", [ptr, ptr, i32, i32, i32, i32, i32, i32, i32, i32, f32, ptr, ptr, ptr])):
             getattr(L, name).argtypes, getattr(L, name).restype = args, C.c_int
         L.spice_static_scratch_bytes.restype = C.c_size_t
         L.spice_lore_calibrate.restype = C.c_int
@@ -258,6 +259,8 @@ def spice_moe_layer_fwd_fp8(ctx, weights: "LayerWeightsFp8C", h, conf, T, y, y_c
 
 
 # ---- steps next to the layer: no ctx; shapes are read off the tensors and checked, the call goes to the tensors' device
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
+GROUP_MAX, GROUP_TOP2 = 0, 1
 
 
 def _addr(what: str, t: Optional[torch.Tensor], dtype, shape, dev) -> Optional[int]:
@@ -314,6 +317,18 @@ def spice_quantize_i8_rows(w, q, scale, stream=None) -> None:
         raise SpiceError(f"{f}: unsupported row length {cols}")
     _call_on(dev, f, stream, _addr(f, w, torch.bfloat16, w.shape, dev), w.numel() // cols, cols,
              _addr(f, q, torch.int8, w.shape, dev), _addr(f, scale, torch.float32, w.shape[:-1], dev))
+
+
+def spice_route_scored(logits, idx, gate, bias=None, score=SCORE_SOFTMAX, n_groups=1, top_groups=1, group_score=GROUP_MAX,
+                       norm_topk=True, scale=1.0, stream=None) -> None:
+    """logits [T,N] fp32 (and bias [N] fp32) -> idx [T,K] int32, gate [T,K] fp32."""
+    f = "spice_route_scored"
+    T, N, dev = _rows_of(f, logits)
+    K = _rows_of(f, idx)[1]
+    f32 = torch.float32
+    _call_on(dev, f, stream, _addr(f, logits, f32, (T, N), dev), _addr(f, bias, f32, (N,), dev), T, N, K, score, n_groups,
+             top_groups, group_score, int(norm_topk), scale, _addr(f, idx, torch.int32, (T, K), dev),
+             _addr(f, gate, f32, (T, K), dev))
 
 
 # ------------------------------------------------------------------ convenience wrappers

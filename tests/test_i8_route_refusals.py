@@ -35,6 +35,20 @@ def test_quantize_i8_rows_refusals():
     assert rows(cols=32776) == SHAPE and rows(n=1 << 31) == SHAPE
 
 
+def route(logits=P, bias=None, T=1, N=64, K=6, score=0, G=1, top=1, pair=0, norm=1, scale=1.0, idx=P, gate=P):
+    return B.lib().spice_route_scored(logits, bias, T, N, K, score, G, top, pair, norm, scale, idx, gate, None)
+
+
+def test_route_scored_refusals():
+    assert route(T=0) == OK
+    for bad in (dict(T=-1), dict(score=2), dict(score=-1), dict(pair=2), dict(logits=None), dict(idx=None), dict(gate=None),
+                dict(logits=P + 2), dict(bias=P + 1), dict(idx=P + 2), dict(gate=P + 3)):
+        assert route(**bad) == INVALID, bad
+    for bad in (dict(N=0), dict(N=1025), dict(K=0), dict(K=33), dict(N=4), dict(G=0), dict(G=3), dict(N=66, G=33), dict(G=8, top=0),
+                dict(G=8, top=9), dict(N=16, G=8, top=2)):
+        assert route(**bad) == SHAPE, bad
+
+
 def test_binding_refuses_host_tensors_and_wrong_shapes():
     bf, i8, f32 = torch.bfloat16, torch.int8, torch.float32
     z = lambda *s, dtype: torch.zeros(*s, dtype=dtype)  # noqa: E731
@@ -42,6 +56,8 @@ def test_binding_refuses_host_tensors_and_wrong_shapes():
         B.spice_residual_rmsnorm(z(2, 8, dtype=bf), z(8, dtype=bf), 1e-6, z(2, 8, dtype=i8), z(2, dtype=f32))
     with pytest.raises(B.SpiceError):
         B.spice_quantize_i8_rows(z(2, 8, dtype=bf), z(2, 8, dtype=i8), z(2, dtype=f32))
+    with pytest.raises(B.SpiceError):
+        B.spice_route_scored(z(2, 8, dtype=f32), z(2, 2, dtype=torch.int32), z(2, 2, dtype=f32))
     dev = torch.device("cuda", 0)
     for t, dtype, shape in ((z(2, 8, dtype=bf), bf, (2, 8)), (z(2, 8, dtype=bf), f32, (2, 8)), (z(2, 8, dtype=bf), bf, (2, 4)),
                             (z(8, 2, dtype=bf).t(), bf, (2, 8))):
