@@ -287,6 +287,26 @@ spice_status spice_residual_rmsnorm(spice_bf16 *x_resid, const spice_bf16 *delta
  * rows below 2^31 (SPICE_ERR_UNSUPPORTED_SHAPE above); w 16-byte, q 8-byte aligned. */
 spice_status spice_quantize_i8_rows(const spice_bf16 *w, int64_t rows, int32_t cols, int8_t *q, float *scale, void *stream);
 
+/* Product of 8-bit integer rows with a scale per token and per output channel:
+ *     y[t,j] = ( sum_i x_q[t,i] * w_q[j,i] ) * x_scale[t] * w_scale[j]
+ * The sum is exact (32-bit integers; -128 is allowed), so results do not depend on how it is split.
+ *   x_q [T,k] int8, x_scale [T] fp32, w_q [n,k] int8, w_scale [n] fp32.
+ *   out: the type of y [T,n]: bf16, fp32, or fp32 that is added to.
+ *   device_status: optional device int32 which the caller has set to 0: raised to SPICE_ERR_TIMEOUT when a bounded wait
+ *   inside the kernel expired (the outputs are undefined then).
+ *   k a multiple of 16 up to 131056, n a multiple of 8; n and T up to 2^24 (SPICE_ERR_UNSUPPORTED_SHAPE above).  x_q, w_q,
+ *   w_scale and y 16-byte aligned.  y must not overlap the inputs. */
+enum { SPICE_OUT_BF16 = 0, SPICE_OUT_F32 = 1, SPICE_OUT_F32_ADD = 2 };
+spice_status spice_gemm_i8(const int8_t *x_q, const float *x_scale, const int8_t *w_q, const float *w_scale, int32_t T,
+                           int32_t n, int32_t k, int32_t out, void *y, int32_t *device_status, void *stream);
+
+/* The gate and up products of a SwiGLU FFN with its activation, in the same arithmetic:
+ *     g, u = rows i and inter + i of the product above with w_gate_up_q,   act[t,i] = bf16( g / (1 + exp(-g)) * u )
+ *   w_gate_up_q [2 inter, k] int8: inter gate rows, then inter up rows (the layout of shared_w_gate_up);
+ *   w_scale [2 inter] fp32; act [T, inter] bf16 out.  Everything else as in spice_gemm_i8 with n = inter. */
+spice_status spice_swiglu_i8(const int8_t *x_q, const float *x_scale, const int8_t *w_gate_up_q, const float *w_scale,
+                             int32_t T, int32_t inter, int32_t k, spice_bf16 *act, int32_t *device_status, void *stream);
+
 /* Routing by scores, from router logits [T, n_experts] fp32 (e.g. the optional output of spice_route_topk):
  *     score_e = softmax(logits)_e or 1 / (1 + exp(-logits_e));   key_e = score_e + bias_e
  *     the top_k experts with the largest keys, in that order, equal keys towards the smaller index -> idx [T, top_k] int32

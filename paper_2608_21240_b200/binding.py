@@ -69,6 +69,8 @@ def lib() -> C.CDLL:
         i32, i64, f32, ptr = C.c_int32, C.c_int64, C.c_float, C.c_void_p
         for name, args in (("spice_residual_rmsnorm", [ptr, ptr, ptr, ptr, f32, i32, i32, ptr, ptr, ptr, ptr]),
                            ("spice_quantize_i8_rows", [ptr, i64, i32, ptr, ptr, ptr]),
+                           ("spice_gemm_i8", [ptr, ptr, ptr, ptr, i32, i32, i32, i32, ptr, ptr, ptr]),
+                           ("spice_swiglu_i8", [ptr, ptr, ptr, ptr, i32, i32, i32, ptr, ptr, ptr]),
                            ("spice_route_scored", [ptr, ptr, i32, i32, i32, i32, i32, i32, i32, i32, f32, ptr, ptr, ptr])):
             getattr(L, name).argtypes, getattr(L, name).restype = args, C.c_int
         L.spice_static_scratch_bytes.restype = C.c_size_t
@@ -261,6 +263,7 @@ def spice_moe_layer_fwd_fp8(ctx, weights: "LayerWeightsFp8C", h, conf, T, y, y_c
 # ---- steps next to the layer: no ctx; shapes are read off the tensors and checked, the call goes to the tensors' device
 SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
 GROUP_MAX, GROUP_TOP2 = 0, 1
+OUT_BF16, OUT_F32, OUT_F32_ADD = 0, 1, 2
 
 
 def _addr(what: str, t: Optional[torch.Tensor], dtype, shape, dev) -> Optional[int]:
@@ -317,6 +320,35 @@ def spice_quantize_i8_rows(w, q, scale, stream=None) -> None:
         raise SpiceError(f"{f}: unsupported row length {cols}")
     _call_on(dev, f, stream, _addr(f, w, torch.bfloat16, w.shape, dev), w.numel() // cols, cols,
              _addr(f, q, torch.int8, w.shape, dev), _addr(f, scale, torch.float32, w.shape[:-1], dev))
+
+
+def spice_gemm_i8(x_q, x_scale, w_q, w_scale, y, accumulate=False, device_status=None, stream=None) -> None:
+    """x_q [T,k] int8, x_scale [T] fp32, w_q [n,k] int8, w_scale [n] fp32 -> y [T,n] bf16 or fp32; accumulate: y fp32 is
+    added to.  device_status: zeroed int32 tensor of one element that receives an expired wait."""
+    f = "spice_gemm_i8"
+    T, k, dev = _rows_of(f, x_q)
+    n = _rows_of(f, w_q)[0]
+    i8, f32 = torch.int8, torch.float32
+    out = (OUT_F32_ADD if accumulate else OUT_F32) if y.dtype == f32 else OUT_BF16
+    if accumulate and out == OUT_BF16:
+        raise SpiceError(f"{f}: only an fp32 y is added to")
+    _call_on(dev, f, stream, _addr(f, x_q, i8, (T, k), dev), _addr(f, x_scale, f32, (T,), dev), _addr(f, w_q, i8, (n, k), dev),
+             _addr(f, w_scale, f32, (n,), dev), T, n, k, out, _addr(f, y, torch.bfloat16 if out == OUT_BF16 else f32, (T, n), dev),
+             _addr(f, device_status, torch.int32, (1,), dev))
+
+
+def spice_swiglu_i8(x_q, x_scale, w_gate_up_q, w_scale, act, device_status=None, stream=None) -> None:
+    """x_q [T,k] int8, x_scale [T] fp32, w_gate_up_q [2 inter,k] int8 (gate rows, then up rows), w_scale [2 inter] fp32 ->
+    act [T,inter] bf16."""
+    f = "spice_swiglu_i8"
+    T, k, dev = _rows_of(f, x_q)
+    n2 = _rows_of(f, w_gate_up_q)[0]
+    if n2 % 2:
+        raise SpiceError(f"{f}: w_gate_up_q has an odd number of rows")
+    i8, f32 = torch.int8, torch.float32
+    _call_on(dev, f, stream, _addr(f, x_q, i8, (T, k), dev), _addr(f, x_scale, f32, (T,), dev),
+             _addr(f, w_gate_up_q, i8, (n2, k), dev), _addr(f, w_scale, f32, (n2,), dev), T, n2 // 2, k,
+             _addr(f, act, torch.bfloat16, (T, n2 // 2), dev), _addr(f, device_status, torch.int32, (1,), dev))
 
 
 def spice_route_scored(logits, idx, gate, bias=None, score=SCORE_SOFTMAX, n_groups=1, top_groups=1, group_score=GROUP_MAX,
@@ -388,6 +420,38 @@ def quantize_layer(w: "LayerWeights") -> LayerWeightsFp8:
     hgu, shgu = qz(w.shared_w_gate_up)
     hd, shd = qz(w.shared_w_down)
     return LayerWeightsFp8(w.w_router, sgu, ssgu, sd, ssd, w.slot_of_expert, hgu, shgu, hd, shd, w.lore_A, w.lore_B)
+
+
+@dataclass
+class SharedExpertI8:
+    """Device tensors of the shared expert (or a dense FFN) in 8-bit integers with a scale per output channel."""
+    q_gate_up: torch.Tensor    # [2Is,d] int8
+    s_gate_up: torch.Tensor    # [2Is] fp32
+    q_down: torch.Tensor       # [d,Is] int8
+    s_down: torch.Tensor       # [d] fp32
+
+
+def quantize_shared_i8(w: "LayerWeights") -> SharedExpertI8:
+    """The shared expert of a bf16 weight set in 8-bit integers: two calls of spice_quantize_i8_rows."""
+    def qz(t):
+        q = torch.empty(t.shape, dtype=torch.int8, device=t.device)
+        s = torch.empty(t.shape[:-1], dtype=torch.float32, device=t.device)
+        spice_quantize_i8_rows(t, q, s)
+        return q, s
+    return SharedExpertI8(*qz(w.shared_w_gate_up), *qz(w.shared_w_down))
+
+
+def shared_expert_i8(w: SharedExpertI8, x_q, x_scale, y, accumulate=False, device_status=None, stream=None) -> torch.Tensor:
+    """y (bf16 or fp32, or added to fp32) = the SwiGLU FFN of the 8-bit rows that spice_residual_rmsnorm wrote: three calls
+    (gate/up products with the activation, the activations' 8-bit rows, the down product) and the buffers between them."""
+    T, dev = x_q.shape[0], x_q.device
+    with torch.cuda.stream(stream):
+        act = torch.empty(T, w.q_down.shape[1], dtype=torch.bfloat16, device=dev)
+        q, s = torch.empty_like(act, dtype=torch.int8), torch.empty(T, dtype=torch.float32, device=dev)
+    spice_swiglu_i8(x_q, x_scale, w.q_gate_up, w.s_gate_up, act, device_status, stream)
+    spice_quantize_i8_rows(act, q, s, stream)
+    spice_gemm_i8(q, s, w.q_down, w.s_down, y, accumulate, device_status, stream)
+    return y
 
 
 @dataclass

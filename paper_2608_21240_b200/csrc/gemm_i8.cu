@@ -1,0 +1,520 @@
+// Products of 8-bit integer rows with a scale per token and per output channel, on the 5th-generation tensor cores:
+//
+//   y[t, n] = ( sum_k x[t,k] w[n,k] ) * x_scale[t] * w_scale[n]                        (bf16, fp32, or added to fp32)
+//   SwiGLU:   g, u = the products with the gate and the up rows;   act[t, i] = bf16( g / (1 + e^-g) * u )
+//
+// The sum is an integer and exact (k <= 131056: 2^14 k < 2^31), so neither the order of the additions nor a split of the
+// reduction changes a bit; one rounding when it becomes fp32, one per scale, one to bf16.
+//
+// Two kernels.  Few tokens: every weight byte is used for few products and the call is bound by streaming the weights, so
+// the weight rows are the M operand, the tokens the N operand (as in the fused decode kernel), and the reduction is split
+// over the CTAs of a cluster so that narrow layers still fill the GPU; the cluster adds its partial sums through
+// distributed shared memory, no workspace and no atomics.  Many tokens: pairs of CTAs work on 256 x 256 tiles
+// (cta_group::2: each CTA loads half of either operand), persistent, accumulators double-buffered in TMEM.
+#include <algorithm>
+
+#include "entry.cuh"
+#include "spice_internal.cuh"
+#include "tc_device.cuh"
+
+namespace spice {
+
+namespace {
+
+using namespace tcdev;
+
+constexpr int BK = 128;                 // bytes = elements of the reduction per pipeline stage: one swizzle span
+constexpr int MAX_K = 131056;
+
+struct GemmI8Args {
+    const float *xs, *ws;   // [T], [n] (SwiGLU: [2 inter])
+    void *y;                // [T, n] (SwiGLU: [T, inter])
+    int32_t T, n, k;        // n: columns of y
+    int32_t out;            // SPICE_OUT_*
+    int32_t *status;        // optional
+    // few tokens
+    int32_t split, stages, cols;   // CTAs along the reduction, ring stages, token columns of a tile (multiple of 16)
+    // many tokens
+    int32_t m_tiles, n_tiles;
+};
+
+__device__ __forceinline__ float silu_times(float g, float u) { return g / (1.0f + __expf(-g)) * u; }
+
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+    __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<uint32_t *>(&v);
+}
+
+// four consecutive outputs of one token
+__device__ __forceinline__ void store4(const GemmI8Args &g, size_t at, float4 v) {
+    if (g.out == SPICE_OUT_BF16) {
+        *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(g.y) + at) = make_uint2(pack2(v.x, v.y), pack2(v.z, v.w));
+        return;
+    }
+    float4 *dst = reinterpret_cast<float4 *>(static_cast<float *>(g.y) + at);
+    if (g.out == SPICE_OUT_F32_ADD) {
+        const float4 o = *dst;
+        v = make_float4(o.x + v.x, o.y + v.y, o.z + v.z, o.w + v.w);
+    }
+    *dst = v;
+}
+
+// ------------------------------------------------------------------------------------------------ few tokens
+constexpr int SK_THREADS = 128, SK_MAX_STAGES = 12;
+constexpr int SK_W_BYTES = 128 * BK;
+
+struct SkinnyShared {
+    alignas(8) unsigned long long full[SK_MAX_STAGES], empty[SK_MAX_STAGES], done;
+    uint32_t tmem_base;
+    int abort_flag;
+};
+static_assert(sizeof(SkinnyShared) <= 256, "control block");
+
+__device__ __forceinline__ int4 ld_cluster4(uint32_t cluster_addr) {
+    int4 v;
+    asm volatile("ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(cluster_addr));
+    return v;
+}
+
+// grid: x = row tiles * split (a cluster = one row tile), y = token tiles.  Row tile: 128 weight rows (SwiGLU: 64 gate
+// rows and their 64 up rows).
+template <bool SWIGLU>
+__global__ void __launch_bounds__(SK_THREADS) gemm_i8_skinny_kernel(const __grid_constant__ CUtensorMap map_w,
+                                                                    const __grid_constant__ CUtensorMap map_x, const GemmI8Args g) {
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    unsigned char *ring = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    __shared__ SkinnyShared sh;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    volatile int *abort_flag = &sh.abort_flag;
+    const int split = g.split, rank = blockIdx.x % split, tile = blockIdx.x / split;
+    const int cols = g.cols, stages = g.stages, stage_bytes = SK_W_BYTES + cols * BK;
+    const int n0 = tile * (SWIGLU ? 64 : 128), t0 = blockIdx.y * cols;
+    const int kblocks = (g.k + BK - 1) / BK;
+    const int kb0 = kblocks * rank / split, n_it = kblocks * (rank + 1) / split - kb0;
+    uint32_t tmem_cols = 32;
+    while (tmem_cols < (uint32_t)cols) tmem_cols *= 2;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < stages; ++s) {
+            mbar_init(smem_u32(&sh.full[s]), 1);
+            mbar_init(smem_u32(&sh.empty[s]), 1);
+        }
+        mbar_init(smem_u32(&sh.done), 1);
+        sh.abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem_base)), "r"(tmem_cols));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = sh.tmem_base;
+
+    if (warp == 0 && lane == 0) {
+        int it = 0;
+        for (; it < n_it; ++it) {
+            const int s = it % stages;
+            if (!mbar_wait(smem_u32(&sh.empty[s]), ((it / stages) & 1) ^ 1, abort_flag)) break;
+            const uint32_t full = smem_u32(&sh.full[s]), dst = smem_u32(ring + s * stage_bytes);
+            const int k0 = (kb0 + it) * BK;
+            mbar_expect_tx(full, stage_bytes);
+            if (SWIGLU) {
+                tma_load_2d(dst, &map_w, k0, n0, full);
+                tma_load_2d(dst + SK_W_BYTES / 2, &map_w, k0, g.n + n0, full);
+            } else {
+                tma_load_2d(dst, &map_w, k0, n0, full);
+            }
+            tma_load_2d(dst + SK_W_BYTES, &map_x, k0, t0, full);
+        }
+        // every stage that was armed has landed before the ring is reused or the CTA ends
+        for (int j = it > stages ? it - stages : 0; j < it; ++j) mbar_drain(smem_u32(&sh.full[j % stages]), (j / stages) & 1);
+    } else if (warp == 1 && lane == 0) {
+        const uint32_t idesc = make_idesc_i8(128, cols);
+        for (int it = 0; it < n_it; ++it) {
+            const int s = it % stages;
+            if (!mbar_wait(smem_u32(&sh.full[s]), (it / stages) & 1, abort_flag)) break;
+            tc_fence_after();
+            const uint32_t w0 = smem_u32(ring + s * stage_bytes);
+            const uint64_t dw = make_desc(w0), dx = make_desc(w0 + SK_W_BYTES);
+#pragma unroll
+            for (int k = 0; k < BK / 32; ++k) tc_mma_i8(tmem, dw + 2 * k, dx + 2 * k, idesc, (it | k) ? 1u : 0u);
+            tc_commit(smem_u32(&sh.empty[s]));
+        }
+        tc_commit(smem_u32(&sh.done));
+    }
+    __syncwarp();
+    if (lane == 0) mbar_drain(smem_u32(&sh.done), 0);
+    __syncwarp();
+    tc_fence_after();
+    __syncthreads();   // (the producer has seen its last copies land: the ring is free)
+
+    // ---- sums into shared memory, [token column][128 rows]
+    const int ncol = min(cols, g.T - t0);
+    int32_t *red = reinterpret_cast<int32_t *>(ring);
+    for (int c = 0; c < ncol; c += 16) {
+        uint32_t v[16];
+        tc_ld16(tmem + ((uint32_t)(warp * 32) << 16) + c, v);
+        tc_wait_ld();
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            if (c + j < ncol) red[(c + j) * 128 + warp * 32 + lane] = (int32_t)v[j];
+    }
+    tc_fence_before();
+    if (split > 1) cluster_sync();
+    else __syncthreads();
+    tc_fence_after();
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(tmem_cols));
+
+    // ---- every CTA of the cluster finishes its share of the tile, four rows of a column at a time
+    constexpr int QUADS = SWIGLU ? 16 : 32;
+    const int items = ncol * QUADS;
+    const uint32_t red_s = smem_u32(red);
+    for (int i = items * rank / split + threadIdx.x; i < items * (rank + 1) / split; i += SK_THREADS) {
+        const int c = i / QUADS, row = (i % QUADS) * 4;
+        if (n0 + row >= g.n) continue;
+        int4 a = make_int4(0, 0, 0, 0), b = make_int4(0, 0, 0, 0);
+        for (int r = 0; r < split; ++r) {
+            const uint32_t at = red_s + (uint32_t)(c * 128 + row) * 4;
+            const int4 p = ld_cluster4(map_to_cta(at, (uint32_t)r));
+            a = make_int4(a.x + p.x, a.y + p.y, a.z + p.z, a.w + p.w);
+            if (SWIGLU) {
+                const int4 q = ld_cluster4(map_to_cta(at + 64 * 4, (uint32_t)r));
+                b = make_int4(b.x + q.x, b.y + q.y, b.z + q.z, b.w + q.w);
+            }
+        }
+        const float xs = g.xs[t0 + c];
+        const float4 w4 = *reinterpret_cast<const float4 *>(g.ws + n0 + row);
+        float4 v = make_float4((float)a.x * xs * w4.x, (float)a.y * xs * w4.y, (float)a.z * xs * w4.z, (float)a.w * xs * w4.w);
+        if (SWIGLU) {
+            const float4 u4 = *reinterpret_cast<const float4 *>(g.ws + g.n + n0 + row);
+            v = make_float4(silu_times(v.x, (float)b.x * xs * u4.x), silu_times(v.y, (float)b.y * xs * u4.y),
+                            silu_times(v.z, (float)b.z * xs * u4.z), silu_times(v.w, (float)b.w * xs * u4.w));
+        }
+        store4(g, (size_t)(t0 + c) * g.n + n0 + row, v);
+    }
+    if (threadIdx.x == 0 && sh.abort_flag && g.status) atomicMax(g.status, (int)SPICE_ERR_TIMEOUT);
+    if (split > 1) cluster_sync();   // nobody leaves while a peer reads its sums
+}
+
+// ------------------------------------------------------------------------------------------------ many tokens
+constexpr int PR_THREADS = 192, PR_STAGES = 6;
+constexpr int PR_TILE = 256;                                   // tokens and accumulator columns of a pair's tile
+constexpr int PR_HALF_BYTES = 128 * BK;                        // a CTA's half of one operand
+constexpr int PR_STAGE_BYTES = 2 * PR_HALF_BYTES;
+constexpr int PR_STG_WARP = 32 * 144;                          // an epilogue warp's transposition buffer
+constexpr size_t PR_SMEM = (size_t)PR_STAGES * PR_STAGE_BYTES + 4 * PR_STG_WARP + 1024;
+constexpr int PR_GROUP_M = 16;                                 // token tiles that share a sweep over the weight tiles
+
+struct PairShared {
+    alignas(8) unsigned long long full[PR_STAGES], empty[PR_STAGES], tmem_full[2], tmem_empty[2], mma_drain;
+    uint32_t tmem_base;
+    int abort_flag;
+};
+
+// tile number -> token tile, weight tile: groups of PR_GROUP_M token tiles, within a group the token tile runs fastest, so
+// that pairs working at the same time share both operands in L2
+__device__ __forceinline__ void pair_tile(const GemmI8Args &g, int tile, int &mt, int &nt) {
+    const int per_group = PR_GROUP_M * g.n_tiles;
+    const int grp = tile / per_group, first = grp * PR_GROUP_M;
+    const int width = min(PR_GROUP_M, g.m_tiles - first);
+    const int in = tile - grp * per_group;
+    mt = first + in % width;
+    nt = in / width;
+}
+
+template <bool SWIGLU>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PR_THREADS, 1)
+    gemm_i8_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const GemmI8Args g) {
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    unsigned char *ring = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    unsigned char *stage_base = ring + PR_STAGES * PR_STAGE_BYTES;
+    __shared__ PairShared sh;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    volatile int *abort_flag = &sh.abort_flag;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < PR_STAGES; ++s) {
+            mbar_init(smem_u32(&sh.full[s]), 1);    // used in the even CTA: both CTAs' copies report there
+            mbar_init(smem_u32(&sh.empty[s]), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(smem_u32(&sh.tmem_full[b]), 1);
+            mbar_init(smem_u32(&sh.tmem_empty[b]), 8);   // used in the even CTA: four epilogue warps of either CTA
+        }
+        mbar_init(smem_u32(&sh.mma_drain), 1);
+        sh.abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {   // TMEM: all 512 columns (two 256-column accumulators), in both CTAs
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem_base)), "r"(512));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::);
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();   // both CTAs' barriers exist before either signals the other's
+    tc_fence_after();
+    const uint32_t tmem_base = sh.tmem_base;
+
+    const int n_tiles = g.m_tiles * g.n_tiles;
+    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    const int kblocks = (g.k + BK - 1) / BK;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            uint32_t it = 0;
+            bool ok = true;
+            for (int tile = pair; tile < n_tiles && ok; tile += pairs) {
+                int mt, nt;
+                pair_tile(g, tile, mt, nt);
+                const int x_row = mt * PR_TILE + (int)rank * 128;
+                const int w_row = SWIGLU ? (rank ? g.n : 0) + nt * 128 : nt * PR_TILE + (int)rank * 128;
+                for (int kb = 0; kb < kblocks; ++kb, ++it) {
+                    const int s = it % PR_STAGES;
+                    if (!mbar_wait(smem_u32(&sh.empty[s]), ((it / PR_STAGES) & 1) ^ 1, abort_flag)) { ok = false; break; }
+                    const uint32_t full = map_to_cta(smem_u32(&sh.full[s]), 0);
+                    const uint32_t dst = smem_u32(ring + s * PR_STAGE_BYTES);
+                    if (rank == 0) mbar_expect_tx(smem_u32(&sh.full[s]), 2 * PR_STAGE_BYTES);
+                    tma_load_2d_pair(dst, &map_x, kb * BK, x_row, full);
+                    tma_load_2d_pair(dst + PR_HALF_BYTES, &map_w, kb * BK, w_row, full);
+                }
+            }
+            // a CTA ends when the stages it filled have been read by the MMAs: nothing of it is in flight then, neither a
+            // copy nor a release of a stage (also after an abort, within the limit)
+            for (uint32_t j = (it > PR_STAGES ? it - PR_STAGES : 0); j < it; ++j)
+                mbar_drain(smem_u32(&sh.empty[j % PR_STAGES]), (j / PR_STAGES) & 1);
+        }
+    } else if (warp == 1) {
+        if (rank == 0 && lane == 0) {
+            constexpr uint32_t idesc = make_idesc_i8(256, PR_TILE);
+            uint32_t it = 0, tcount = 0;
+            bool ok = true;
+            for (int tile = pair; tile < n_tiles && ok; tile += pairs, ++tcount) {
+                const int buf = tcount & 1;
+                if (!mbar_wait(smem_u32(&sh.tmem_empty[buf]), ((tcount >> 1) & 1) ^ 1, abort_flag)) break;
+                tc_fence_after();
+                const uint32_t d_tmem = tmem_base + buf * PR_TILE;
+                for (int kb = 0; kb < kblocks; ++kb, ++it) {
+                    const int s = it % PR_STAGES;
+                    if (!mbar_wait(smem_u32(&sh.full[s]), (it / PR_STAGES) & 1, abort_flag)) { ok = false; break; }
+                    tc_fence_after();
+                    const uint32_t a0 = smem_u32(ring + s * PR_STAGE_BYTES);
+                    const uint64_t da = make_desc(a0), db = make_desc(a0 + PR_HALF_BYTES);
+#pragma unroll
+                    for (int k = 0; k < BK / 32; ++k) tc_mma_i8_pair(d_tmem, da + 2 * k, db + 2 * k, idesc, (kb | k) ? 1u : 0u);
+                    tc_commit_pair(smem_u32(&sh.empty[s]));
+                }
+                if (ok) tc_commit_pair(smem_u32(&sh.tmem_full[buf]));
+            }
+            tc_commit_pair_local(smem_u32(&sh.mma_drain));
+            mbar_drain(smem_u32(&sh.mma_drain), 0);
+        }
+    } else {
+        // ---------------- epilogue: warp w owns TMEM lanes 32*(w%4) .. +31 = rows of this CTA's half of the tile
+        const int q = warp & 3;
+        unsigned char *stg = stage_base + (warp - 2) * PR_STG_WARP;
+        uint32_t tcount = 0;
+        for (int tile = pair; tile < n_tiles; tile += pairs, ++tcount) {
+            const int buf = tcount & 1;
+            int mt, nt;
+            pair_tile(g, tile, mt, nt);
+            bool ok = true;
+            if (lane == 0) ok = mbar_wait(smem_u32(&sh.tmem_full[buf]), (tcount >> 1) & 1, abort_flag);
+            ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
+            if (!ok) break;
+            tc_fence_after();
+            const int row0 = mt * PR_TILE + (int)rank * 128 + q * 32;   // token of lane 0
+            const float xs = row0 + lane < g.T ? g.xs[row0 + lane] : 0.0f;
+            const uint32_t tm = tmem_base + buf * PR_TILE + ((uint32_t)(q * 32) << 16);
+            const int col0 = nt * (SWIGLU ? 128 : PR_TILE);
+            // 32 columns at a time: a lane holds one token's; turned through shared memory so that a store covers whole
+            // 16-byte pieces of consecutive columns
+            if (SWIGLU || g.out == SPICE_OUT_BF16) {
+                constexpr int PITCH = 80;   // 64 B of bf16 per row + 16
+#pragma unroll 1
+                for (int c = 0; c < (SWIGLU ? 128 : PR_TILE); c += 32) {
+                    if (col0 + c >= g.n) break;
+                    uint32_t v[32], u[SWIGLU ? 32 : 1];
+                    tc_ld32(tm + c, v);
+                    if constexpr (SWIGLU) tc_ld32(tm + 128 + c, u);
+                    tc_wait_ld();
+                    const float4 *w4 = reinterpret_cast<const float4 *>(g.ws + col0 + c);
+                    const float4 *u4 = reinterpret_cast<const float4 *>(g.ws + (SWIGLU ? g.n : 0) + col0 + c);
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        // (g.n is a multiple of 8: a piece of eight columns is inside or outside)
+                        const float4 w = col0 + c + 4 * j < g.n ? w4[j] : make_float4(0.f, 0.f, 0.f, 0.f);
+                        float a[4] = {(float)(int32_t)v[4 * j] * xs * w.x, (float)(int32_t)v[4 * j + 1] * xs * w.y,
+                                      (float)(int32_t)v[4 * j + 2] * xs * w.z, (float)(int32_t)v[4 * j + 3] * xs * w.w};
+                        if constexpr (SWIGLU) {
+                            const float4 z = col0 + c + 4 * j < g.n ? u4[j] : make_float4(0.f, 0.f, 0.f, 0.f);
+                            a[0] = silu_times(a[0], (float)(int32_t)u[4 * j] * xs * z.x);
+                            a[1] = silu_times(a[1], (float)(int32_t)u[4 * j + 1] * xs * z.y);
+                            a[2] = silu_times(a[2], (float)(int32_t)u[4 * j + 2] * xs * z.z);
+                            a[3] = silu_times(a[3], (float)(int32_t)u[4 * j + 3] * xs * z.w);
+                        }
+                        pk[2 * j] = pack2(a[0], a[1]);
+                        pk[2 * j + 1] = pack2(a[2], a[3]);
+                    }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        *reinterpret_cast<uint4 *>(stg + lane * PITCH + k * 16) = make_uint4(pk[4 * k], pk[4 * k + 1], pk[4 * k + 2], pk[4 * k + 3]);
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int rr = i * 8 + (lane >> 2), part = lane & 3, col = col0 + c + part * 8;
+                        const uint4 val = *reinterpret_cast<const uint4 *>(stg + rr * PITCH + part * 16);
+                        if (row0 + rr < g.T && col < g.n)
+                            *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(g.y) + (size_t)(row0 + rr) * g.n + col) = val;
+                    }
+                    __syncwarp();
+                }
+            } else {
+                constexpr int PITCH = 144;   // 128 B of fp32 per row + 16
+#pragma unroll 1
+                for (int c = 0; c < PR_TILE; c += 32) {
+                    if (col0 + c >= g.n) break;
+                    uint32_t v[32];
+                    tc_ld32(tm + c, v);
+                    tc_wait_ld();
+                    const float4 *w4 = reinterpret_cast<const float4 *>(g.ws + col0 + c);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float4 w = col0 + c + 4 * j < g.n ? w4[j] : make_float4(0.f, 0.f, 0.f, 0.f);
+                        *reinterpret_cast<float4 *>(stg + lane * PITCH + j * 16) =
+                            make_float4((float)(int32_t)v[4 * j] * xs * w.x, (float)(int32_t)v[4 * j + 1] * xs * w.y,
+                                        (float)(int32_t)v[4 * j + 2] * xs * w.z, (float)(int32_t)v[4 * j + 3] * xs * w.w);
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int rr = i * 4 + (lane >> 3), part = lane & 7, col = col0 + c + part * 4;
+                        const float4 val = *reinterpret_cast<const float4 *>(stg + rr * PITCH + part * 16);
+                        if (row0 + rr < g.T && col < g.n) store4(g, (size_t)(row0 + rr) * g.n + col, val);
+                    }
+                    __syncwarp();
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&sh.tmem_empty[buf]), 0));
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (threadIdx.x == 0 && sh.abort_flag && g.status) atomicMax(g.status, (int)SPICE_ERR_TIMEOUT);
+    cluster_sync();   // the pair's MMAs, copies and signals are over in both CTAs
+    tc_fence_after();
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512));
+}
+
+// ------------------------------------------------------------------------------------------------ host side
+// dynamic shared memory limits are raised once per device
+bool prepare_device(int dev) {
+    static std::atomic<bool> done[64];
+    if (done[dev].load(std::memory_order_acquire)) return true;
+    const int most = 227 * 1024 - 1024;
+    bool ok = true;
+    ok &= cudaFuncSetAttribute(gemm_i8_skinny_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) == cudaSuccess;
+    ok &= cudaFuncSetAttribute(gemm_i8_skinny_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) == cudaSuccess;
+    ok &= cudaFuncSetAttribute(gemm_i8_pair_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) == cudaSuccess;
+    ok &= cudaFuncSetAttribute(gemm_i8_pair_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) == cudaSuccess;
+    if (ok) done[dev].store(true, std::memory_order_release);
+    return ok;
+}
+
+template <bool SWIGLU>
+spice_status launch_gemm_i8(GemmI8Args g, const int8_t *x, const int8_t *w, cudaStream_t st) {
+    int dev = 0;
+    const int sms = current_device_sms(&dev);
+    if (sms <= 0 || !prepare_device(dev)) return SPICE_ERR_CUDA;
+    const int w_rows = SWIGLU ? 2 * g.n : g.n;
+    const int kblocks = (g.k + BK - 1) / BK;
+    CUtensorMap map_x, map_w;
+    if (g.T <= 256) {
+        const int tile_n = SWIGLU ? 64 : 128;
+        const int row_tiles = (g.n + tile_n - 1) / tile_n;
+        g.cols = min(256, (g.T + 15) & ~15);
+        const int token_tiles = (g.T + g.cols - 1) / g.cols;
+        const int tiles = row_tiles * token_tiles;
+        g.split = max(1, min(min(8, kblocks), sms / tiles));
+        const int per_cta = (kblocks + g.split - 1) / g.split;
+        const int stage_bytes = SK_W_BYTES + g.cols * BK;
+        g.stages = max(1, min(min(per_cta, SK_MAX_STAGES), (200 * 1024) / stage_bytes));
+        const size_t red = (size_t)min(g.cols, g.T) * 512;
+        // A CTA takes at least the share of shared memory that it takes of TMEM (512 columns against 228 KB with the 1 KB
+        // the system adds): however the CTAs of calls on different streams mix on an SM, no TMEM allocation has to wait,
+        // and a cluster never holds columns that a CTA of another cluster needs to reach its own barrier.
+        int tmem_cols = 32;
+        while (tmem_cols < g.cols) tmem_cols *= 2;
+        const size_t smem = std::max({(size_t)g.stages * stage_bytes + 1024, red + 1024, (size_t)(456 * tmem_cols - 1024)});
+        if (!tc_encode_map2_bytes(&map_w, w, (uint64_t)w_rows, (uint64_t)g.k, tile_n) ||
+            !tc_encode_map2_bytes(&map_x, x, (uint64_t)g.T, (uint64_t)g.k, (uint32_t)g.cols))
+            return SPICE_ERR_CUDA;
+        cudaLaunchConfig_t lc{};
+        lc.gridDim = dim3((unsigned)(row_tiles * g.split), (unsigned)token_tiles, 1);
+        lc.blockDim = dim3(SK_THREADS, 1, 1);
+        lc.dynamicSmemBytes = smem;
+        lc.stream = st;
+        cudaLaunchAttribute at[1];
+        at[0].id = cudaLaunchAttributeClusterDimension;
+        at[0].val.clusterDim.x = (unsigned)g.split;
+        at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+        lc.attrs = at;
+        lc.numAttrs = g.split > 1 ? 1 : 0;
+        return cudaLaunchKernelEx(&lc, gemm_i8_skinny_kernel<SWIGLU>, map_w, map_x, g) == cudaSuccess ? SPICE_OK : SPICE_ERR_CUDA;
+    }
+    g.m_tiles = (g.T + PR_TILE - 1) / PR_TILE;
+    g.n_tiles = SWIGLU ? (g.n + 127) / 128 : (g.n + PR_TILE - 1) / PR_TILE;
+    if ((int64_t)g.m_tiles * g.n_tiles > 0x3fffffff) return SPICE_ERR_UNSUPPORTED_SHAPE;
+    if (!tc_encode_map2_bytes(&map_x, x, (uint64_t)g.T, (uint64_t)g.k, 128) ||
+        !tc_encode_map2_bytes(&map_w, w, (uint64_t)w_rows, (uint64_t)g.k, 128))
+        return SPICE_ERR_CUDA;
+    const int pairs = min(sms / 2, g.m_tiles * g.n_tiles);
+    gemm_i8_pair_kernel<SWIGLU><<<2 * pairs, PR_THREADS, PR_SMEM, st>>>(map_x, map_w, g);
+    return cudaGetLastError() == cudaSuccess ? SPICE_OK : SPICE_ERR_CUDA;
+}
+
+template <bool SWIGLU>
+spice_status call_gemm_i8(const int8_t *x_q, const float *x_scale, const int8_t *w_q, const float *w_scale, int32_t T, int32_t n,
+                          int32_t k, int32_t out, void *y, int32_t *device_status, void *stream) {
+    if (T < 0 || n < 8 || n % 8 || k < 16 || k % 16 ||
+        (out != SPICE_OUT_BF16 && out != SPICE_OUT_F32 && out != SPICE_OUT_F32_ADD))
+        return SPICE_ERR_INVALID_ARG;
+    if (k > MAX_K || n > (1 << 24) || T > (1 << 24)) return SPICE_ERR_UNSUPPORTED_SHAPE;
+    if (T == 0) return SPICE_OK;
+    if (!x_q || !x_scale || !w_q || !w_scale || !y || !aligned16(x_q) || !aligned16(w_q) || !aligned16(w_scale) || !aligned16(y) ||
+        (reinterpret_cast<uintptr_t>(x_scale) & 3u) || (reinterpret_cast<uintptr_t>(device_status) & 3u))
+        return SPICE_ERR_INVALID_ARG;
+    GemmI8Args g{};
+    g.xs = x_scale;
+    g.ws = w_scale;
+    g.y = y;
+    g.T = T;
+    g.n = n;
+    g.k = k;
+    g.out = out;
+    g.status = device_status;
+    return launch_gemm_i8<SWIGLU>(g, x_q, w_q, static_cast<cudaStream_t>(stream));
+}
+
+}  // namespace
+
+}  // namespace spice
+
+using namespace spice;
+
+extern "C" spice_status spice_gemm_i8(const int8_t *x_q, const float *x_scale, const int8_t *w_q, const float *w_scale, int32_t T,
+                                      int32_t n, int32_t k, int32_t out, void *y, int32_t *device_status, void *stream) {
+    Range range_("spice_gemm_i8");
+    return call_gemm_i8<false>(x_q, x_scale, w_q, w_scale, T, n, k, out, y, device_status, stream);
+}
+
+extern "C" spice_status spice_swiglu_i8(const int8_t *x_q, const float *x_scale, const int8_t *w_gate_up_q, const float *w_scale,
+                                        int32_t T, int32_t inter, int32_t k, spice_bf16 *act, int32_t *device_status, void *stream) {
+    Range range_("spice_swiglu_i8");
+    return call_gemm_i8<true>(x_q, x_scale, w_gate_up_q, w_scale, T, inter, k, SPICE_OUT_BF16, act, device_status, stream);
+}

@@ -1,0 +1,130 @@
+"""The steps next to the layer as a decode or prefill step uses them, two layers in a row: residual addition and norm, router
+logits, routing by scores, classification, resident experts in bf16, the shared expert in 8-bit integers added to their sum,
+whose fp32 rows are the next norm's residual.  Against a 64-bit evaluation of the same definitions.
+
+Tolerance: the outputs' own of the layer's parity tests, 1e-2 max |reference| + 1e-3.  What separates the two: bf16 h and
+activations (2^-8 each), 8-bit codes of activations whose bf16 value falls on the other side of a border (one step of
+m / 127 in few of them), all relative to sums of hundreds of terms."""
+import pytest
+import torch
+
+from paper_2608_21240_b200 import binding as B
+from paper_2608_21240_b200 import workloads as W
+from tests._gpu import cfg_of, upload, y_close
+
+pytestmark = pytest.mark.gpu
+f64 = torch.float64
+
+
+def codes64(p):
+    m = p.abs().amax(1, keepdim=True)
+    return torch.round(127 * p / m) * m / 127
+
+
+def silu_acts(x, gate_up):
+    g, u = (x @ gate_up.T).chunk(2, 1)
+    return g / (1 + (-g).exp()) * u
+
+
+def silu_ffn(x, gate_up, down):
+    return silu_acts(x, gate_up) @ down.T
+
+
+def one_layer(L, w, w8, x, delta, weight, conf, bias, route):
+    """One step through the library; x is updated.  Returns the fp32 output rows and what the routing chose."""
+    T, d, K = x.shape[0], x.shape[1], L.cfg.top_k
+    e = lambda *s, t=torch.float32: torch.empty(*s, dtype=t, device="cuda")  # noqa: E731
+    h, q, s = e(T, d, t=torch.bfloat16), e(T, d, t=torch.int8), e(T)
+    B.spice_residual_rmsnorm(x, weight, 1e-6, q, s, h=h, delta=delta)
+    _, _, logits = L.route_topk(h, w.w_router, want_logits=True)
+    idx, gate = e(T, K, t=torch.int32), e(T, K)
+    B.spice_route_scored(logits, idx, gate, bias=bias, **route)
+    cls, slot, counts, _ = L.classify_misses(idx, gate, w.slot_of_expert, conf)
+    y = torch.zeros(T, d, device="cuda")
+    L.grouped_expert_ffn(w, h, idx, gate, cls, slot, y)
+    B.shared_expert_i8(w8, q, s, y, accumulate=True)
+    return y, h, logits, idx, gate, cls, slot
+
+
+@pytest.mark.parametrize("T", [1, 7, 300])
+def test_two_layers_in_a_row(T):
+    wl = W.make_layer("tiny", T, variant=70)
+    s = wl.shape
+    L = B.SpiceLayer(cfg_of(s), T)
+    w = upload(wl)
+    w8 = B.quantize_shared_i8(w)
+    g = torch.Generator(device="cuda").manual_seed(T)
+    rnd = lambda *shape: torch.randn(*shape, device="cuda", generator=g)  # noqa: E731
+    x, weight, bias = rnd(T, s.d).bfloat16(), (1 + 0.1 * rnd(s.d)).bfloat16(), 0.05 * rnd(s.n_experts)
+    conf = torch.from_numpy(wl.conf).cuda()
+    route = dict(score=B.SCORE_SIGMOID, n_groups=4, top_groups=2, group_score=B.GROUP_TOP2, norm_topk=True, scale=2.5)
+    wgu, wd = codes64(w.shared_w_gate_up.to(f64)), codes64(w.shared_w_down.to(f64))
+    delta = None
+    for layer in range(2):
+        before = x.clone()
+        y, h, logits, idx, gate, cls, slot = one_layer(L, w, w8, x, delta, weight, conf, bias, route)
+        torch.cuda.synchronize()
+        # the norm
+        stream = before if delta is None else (before.float() + delta).bfloat16()
+        assert torch.equal(x, stream)
+        p = x.to(f64) * weight.to(f64)
+        r = 1 / (x.to(f64).square().mean(1, keepdim=True) + 1e-6).sqrt()
+        assert ((h.to(f64) - p * r).abs() <= (2.0 ** -8 + 3e-6) * (p * r).abs()).all()
+        # the routing of the logits that the library computed
+        sc = 1 / (1 + (-logits.to(f64)).exp())
+        key = sc + bias.to(f64)
+        G = s.n_experts // 4
+        of = key.view(T, 4, G).sort(dim=2, descending=True).values[:, :, :2].sum(2)
+        keep = torch.zeros_like(of, dtype=torch.bool).scatter_(1, of.sort(dim=1, descending=True, stable=True).indices[:, :2], True)
+        key = torch.where(keep.repeat_interleave(G, 1), key, -torch.inf)
+        ri = key.sort(dim=1, descending=True, stable=True).indices[:, :s.top_k]
+        assert torch.equal(idx.long(), ri)
+        rg = sc.gather(1, ri)
+        rg = 2.5 * rg / rg.sum(1, keepdim=True)
+        assert ((gate - rg).abs() <= 1.1e-5 * rg).all()
+        res = w.slot_of_expert.long()[ri]
+        assert torch.equal(cls == B.HIT, res >= 0) and torch.equal(slot.long(), res)
+        # the experts: resident ones in bf16, the shared one in 8 bits
+        a = silu_acts(codes64(p) * r, wgu)
+        ref = codes64(a.bfloat16().to(f64)) @ wd.T
+        for k in range(s.top_k):
+            for sl in range(s.n_slots):
+                rows = (res[:, k] == sl).nonzero()[:, 0]
+                if len(rows):
+                    ref[rows] += rg[rows, k:k + 1] * silu_ffn(h[rows].to(f64), w.slot_w_gate_up[sl].to(f64), w.slot_w_down[sl].to(f64))
+        err, bound = y_close(y.cpu().numpy(), ref.cpu().numpy())
+        assert err <= bound, (layer, err, bound)
+        delta = y
+    assert L.device_status() == 0
+    L.close()
+
+
+def test_a_captured_step_replays():
+    """The same chain in one graph, replayed on changed inputs, gives what the separate calls give."""
+    T = 5
+    wl = W.make_layer("tiny", T, variant=71)
+    s = wl.shape
+    L = B.SpiceLayer(cfg_of(s), T)
+    w = upload(wl)
+    w8 = B.quantize_shared_i8(w)
+    weight, conf = torch.ones(s.d, dtype=torch.bfloat16, device="cuda"), torch.from_numpy(wl.conf).cuda()
+    bias = torch.zeros(s.n_experts, device="cuda")
+    x, delta = torch.randn(T, s.d, device="cuda").bfloat16(), torch.randn(T, s.d, device="cuda")
+    keep = x.clone()
+    one_layer(L, w, w8, x, delta, weight, conf, bias, {})
+    torch.cuda.synchronize()
+    x.copy_(keep)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = one_layer(L, w, w8, x, delta, weight, conf, bias, {})[0]
+    for i in range(3):
+        fresh = torch.randn(T, s.d, device="cuda").bfloat16()
+        x.copy_(fresh)
+        graph.replay()
+        got, gx = y.clone(), x.clone()
+        x2 = fresh.clone()
+        ref = one_layer(L, w, w8, x2, delta, weight, conf, bias, {})[0]
+        assert torch.equal(gx, x2)
+        # (the routed experts' rows are added in the order of the batch: bitwise equal)
+        assert torch.equal(got, ref)
+    L.close()

@@ -35,6 +35,27 @@ def test_quantize_i8_rows_refusals():
     assert rows(cols=32776) == SHAPE and rows(n=1 << 31) == SHAPE
 
 
+def gemm(x=P, xs=P, w=P, ws=P, T=1, n=64, k=64, out=0, y=P, status=None):
+    return B.lib().spice_gemm_i8(x, xs, w, ws, T, n, k, out, y, status, None)
+
+
+def swiglu(x=P, xs=P, w=P, ws=P, T=1, n=64, k=64, y=P, status=None):
+    return B.lib().spice_swiglu_i8(x, xs, w, ws, T, n, k, y, status, None)
+
+
+@pytest.mark.parametrize("call", [gemm, swiglu])
+def test_product_refusals(call):
+    assert call(T=0) == OK
+    for bad in (dict(T=-1), dict(n=0), dict(n=12), dict(k=0), dict(k=24), dict(k=8), dict(x=None), dict(xs=None), dict(w=None),
+                dict(ws=None), dict(y=None), dict(x=P + 8), dict(w=P + 8), dict(ws=P + 4), dict(y=P + 8), dict(xs=P + 2),
+                dict(status=P + 2)):
+        assert call(**bad) == INVALID, bad
+    for bad in (dict(k=131072), dict(n=(1 << 24) + 8), dict(T=(1 << 24) + 1)):
+        assert call(**bad) == SHAPE, bad
+    if call is gemm:
+        assert call(out=3) == INVALID and call(out=-1) == INVALID
+
+
 def route(logits=P, bias=None, T=1, N=64, K=6, score=0, G=1, top=1, pair=0, norm=1, scale=1.0, idx=P, gate=P):
     return B.lib().spice_route_scored(logits, bias, T, N, K, score, G, top, pair, norm, scale, idx, gate, None)
 
@@ -56,6 +77,10 @@ def test_binding_refuses_host_tensors_and_wrong_shapes():
         B.spice_residual_rmsnorm(z(2, 8, dtype=bf), z(8, dtype=bf), 1e-6, z(2, 8, dtype=i8), z(2, dtype=f32))
     with pytest.raises(B.SpiceError):
         B.spice_quantize_i8_rows(z(2, 8, dtype=bf), z(2, 8, dtype=i8), z(2, dtype=f32))
+    with pytest.raises(B.SpiceError):
+        B.spice_gemm_i8(z(2, 16, dtype=i8), z(2, dtype=f32), z(8, 16, dtype=i8), z(8, dtype=f32), z(2, 8, dtype=bf))
+    with pytest.raises(B.SpiceError):
+        B.spice_swiglu_i8(z(2, 16, dtype=i8), z(2, dtype=f32), z(16, 16, dtype=i8), z(16, dtype=f32), z(2, 8, dtype=bf))
     with pytest.raises(B.SpiceError):
         B.spice_route_scored(z(2, 8, dtype=f32), z(2, 2, dtype=torch.int32), z(2, 2, dtype=f32))
     dev = torch.device("cuda", 0)
