@@ -266,32 +266,41 @@ GROUP_MAX, GROUP_TOP2 = 0, 1
 OUT_BF16, OUT_F32, OUT_F32_ADD = 0, 1, 2
 
 
-def _addr(what: str, t: Optional[torch.Tensor], dtype, shape, dev) -> Optional[int]:
-    """Device address of a tensor of this type and shape on this device (or in pinned host memory); None for None."""
+def _addr(what: str, t: Optional[torch.Tensor], dtype, shape, dev: int) -> Optional[int]:
+    """Address of a tensor of this type and shape on CUDA device `dev` (or in pinned host memory); None for None."""
     if t is None:
         return None
-    if t.dtype != dtype or t.shape != shape or not t.is_contiguous() or not (t.device == dev or t.is_pinned()):
-        raise SpiceError(f"{what}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {dev}, got {t.dtype} "
-                         f"{tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}")
-    return t.data_ptr()
+    if t.dtype is dtype and t.shape == shape and t.is_contiguous() and (t.get_device() == dev or t.is_pinned()):
+        return t.data_ptr()
+    raise SpiceError(f"{what}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on cuda:{dev}, got {t.dtype} "
+                     f"{tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}")
 
 
 def _rows_of(what: str, t: torch.Tensor):
-    """(rows, columns, device) of the 2-D CUDA tensor that gives a call its sizes."""
-    if t.dim() != 2 or not t.is_cuda:
-        raise SpiceError(f"{what}: expected a 2-D CUDA tensor, got shape {tuple(t.shape)} on {t.device}")
-    if t.shape[0] > 0x7fffffff or t.shape[1] > 0x7fffffff:
-        raise SpiceError(f"{what}: too many rows or columns: {tuple(t.shape)}")
-    return t.shape[0], t.shape[1], t.device
+    """(rows, columns, device index) of the 2-D CUDA tensor that gives a call its sizes."""
+    shape = t.shape
+    if len(shape) != 2 or not t.is_cuda:
+        raise SpiceError(f"{what}: expected a 2-D CUDA tensor, got shape {tuple(shape)} on {t.device}")
+    rows, cols = shape
+    if rows > 0x7fffffff or cols > 0x7fffffff:
+        raise SpiceError(f"{what}: too many rows or columns: {tuple(shape)}")
+    return rows, cols, t.get_device()
 
 
-def _call_on(dev: torch.device, name: str, stream, *args) -> None:
-    st = (torch.cuda.current_stream(dev) if stream is None else stream).cuda_stream
-    if dev.index == torch.cuda.current_device():
-        code = getattr(lib(), name)(*args, st)
+# The raw handle of a device's current stream without a Stream object around it (2 us less per call, as much as the launch
+# itself); the public way where this build of torch does not have it.
+_current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+
+
+def _call_on(dev: int, name: str, stream, *args) -> None:
+    """The entry point on the tensors' device, whatever the current one is."""
+    st = _current_raw_stream(dev) if stream is None else stream.cuda_stream
+    f = getattr(_lib or lib(), name)
+    if dev == torch.cuda.current_device():
+        code = f(*args, st)
     else:
         with torch.cuda.device(dev):
-            code = getattr(lib(), name)(*args, st)
+            code = f(*args, st)
     if code != SPICE_OK:
         _check(code, name)
 
@@ -315,7 +324,7 @@ def spice_quantize_i8_rows(w, q, scale, stream=None) -> None:
     f = "spice_quantize_i8_rows"
     if w.dim() < 1 or not w.is_cuda:
         raise SpiceError(f"{f}: expected a CUDA tensor, got shape {tuple(w.shape)} on {w.device}")
-    cols, dev = w.shape[-1], w.device
+    cols, dev = w.shape[-1], w.get_device()
     if cols < 1 or cols > 0x7fffffff:
         raise SpiceError(f"{f}: unsupported row length {cols}")
     _call_on(dev, f, stream, _addr(f, w, torch.bfloat16, w.shape, dev), w.numel() // cols, cols,

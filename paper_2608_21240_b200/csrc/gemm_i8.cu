@@ -38,7 +38,8 @@ struct GemmI8Args {
     int32_t m_tiles, n_tiles;
 };
 
-__device__ __forceinline__ float silu_times(float g, float u) { return g / (1.0f + __expf(-g)) * u; }
+// (fast exponential and quotient: a few 2^-23 for |g| of some units, the result is rounded to bf16 right after)
+__device__ __forceinline__ float silu_times(float g, float u) { return __fdividef(g, 1.0f + __expf(-g)) * u; }
 
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
     __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
@@ -59,16 +60,107 @@ __device__ __forceinline__ void store4(const GemmI8Args &g, size_t at, float4 v)
     *dst = v;
 }
 
+// ------------------------------------------------------------------------------------------------ single tokens
+// Up to 8 tokens: a warp takes a weight row (from two tokens on a pair of rows, which halves the reads of the tokens; with
+// SwiGLU always a gate row and its up row), reads 16 bytes per lane and multiplies with four-wide integer dot products; the
+// tokens come from L1.  No barriers and no tensor memory: at these sizes the chain of latencies of the tensor-core kernel is
+// longer than the whole call.
+constexpr int DOT_THREADS = 256, DOT_MAX_TOKENS = 8;
+
+// WPR warps share the rows: layers with few of them
+template <int TT, bool SWIGLU, int WPR>
+__global__ void __launch_bounds__(DOT_THREADS) gemm_i8_dot_kernel(const int8_t *__restrict__ x, const int8_t *__restrict__ w,
+                                                                  const GemmI8Args g) {
+    constexpr int R = SWIGLU || TT > 1 ? 2 : 1, UN = TT >= 8 ? 2 : 4;
+    constexpr int COLS = SWIGLU ? 1 : R;                       // output columns of a warp
+    __shared__ int32_t part[DOT_THREADS / 32][R * TT];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int row = (blockIdx.x * (DOT_THREADS / 32 / WPR) + warp / WPR) * COLS;
+    const bool in = row < g.n;                                 // (n is a multiple of 8: both columns or none)
+    const int nv = g.k >> 4;
+    const int4 *w0 = reinterpret_cast<const int4 *>(w + (size_t)(in ? row : 0) * g.k);
+    const int4 *w1 = reinterpret_cast<const int4 *>(w + (size_t)((in ? row : 0) + (SWIGLU ? g.n : 1)) * g.k);
+    const int4 *x4 = reinterpret_cast<const int4 *>(x);
+    int32_t acc[R][TT];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int t = 0; t < TT; ++t) acc[r][t] = 0;
+    const int4 zero = make_int4(0, 0, 0, 0);
+    for (int v0 = (warp % WPR) * 32 + lane; v0 < nv; v0 += 32 * WPR * UN) {
+        int4 a[UN][R];
+#pragma unroll
+        for (int u = 0; u < UN; ++u) {
+            const int v = v0 + u * 32 * WPR;
+            a[u][0] = v < nv ? __ldcs(w0 + v) : zero;
+            if (R > 1) a[u][R - 1] = v < nv ? __ldcs(w1 + v) : zero;
+        }
+#pragma unroll
+        for (int u = 0; u < UN; ++u) {
+            const int v = v0 + u * 32 * WPR;
+#pragma unroll
+            for (int t = 0; t < TT; ++t) {
+                const int4 b = v < nv && t < g.T ? __ldg(x4 + (size_t)t * nv + v) : zero;
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    acc[r][t] = __dp4a(a[u][r].x, b.x, acc[r][t]);
+                    acc[r][t] = __dp4a(a[u][r].y, b.y, acc[r][t]);
+                    acc[r][t] = __dp4a(a[u][r].z, b.z, acc[r][t]);
+                    acc[r][t] = __dp4a(a[u][r].w, b.w, acc[r][t]);
+                }
+            }
+        }
+    }
+    int32_t mine[R] = {};   // lane t: token t
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+            const int32_t s = __reduce_add_sync(0xffffffffu, acc[r][t]);
+            if (lane == t) mine[r] = s;
+        }
+    if (WPR > 1) {
+        if (lane < TT)
+#pragma unroll
+            for (int r = 0; r < R; ++r) part[warp][r * TT + lane] = mine[r];
+        __syncthreads();
+        if (warp % WPR) return;
+        if (lane < TT)
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int i = 1; i < WPR; ++i) mine[r] += part[warp + i][r * TT + lane];
+    }
+    if (!in || lane >= g.T) return;
+    const float xs = g.xs[lane];
+    float v[COLS];
+    v[0] = (float)mine[0] * xs * g.ws[row];
+    if (SWIGLU) v[0] = silu_times(v[0], (float)mine[R - 1] * xs * g.ws[row + g.n]);
+    else if (COLS > 1) v[COLS - 1] = (float)mine[R - 1] * xs * g.ws[row + 1];
+    const size_t at = (size_t)lane * g.n + row;
+    if (g.out == SPICE_OUT_BF16) {
+        __nv_bfloat16 *y = static_cast<__nv_bfloat16 *>(g.y) + at;
+        if (COLS > 1) *reinterpret_cast<uint32_t *>(y) = pack2(v[0], v[COLS - 1]);
+        else *y = __float2bfloat16_rn(v[0]);
+    } else {
+        float *y = static_cast<float *>(g.y) + at;
+#pragma unroll
+        for (int i = 0; i < COLS; ++i) y[i] = g.out == SPICE_OUT_F32 ? v[i] : y[i] + v[i];
+    }
+}
+
 // ------------------------------------------------------------------------------------------------ few tokens
-constexpr int SK_THREADS = 128, SK_MAX_STAGES = 12;
+constexpr int SK_THREADS = 256, SK_MAX_STAGES = 12, SK_MAX_SPLIT = 8;
 constexpr int SK_W_BYTES = 128 * BK;
+constexpr int SK_MAX_SMEM = 225 * 1024;
 
 struct SkinnyShared {
     alignas(8) unsigned long long full[SK_MAX_STAGES], empty[SK_MAX_STAGES], done;
     uint32_t tmem_base;
     int abort_flag;
+    alignas(16) float ws[128];   // of the tile's weight rows
+    float xs[256];               // of its tokens
 };
-static_assert(sizeof(SkinnyShared) <= 256, "control block");
 
 __device__ __forceinline__ int4 ld_cluster4(uint32_t cluster_addr) {
     int4 v;
@@ -81,7 +173,7 @@ __device__ __forceinline__ int4 ld_cluster4(uint32_t cluster_addr) {
 template <bool SWIGLU>
 __global__ void __launch_bounds__(SK_THREADS) gemm_i8_skinny_kernel(const __grid_constant__ CUtensorMap map_w,
                                                                     const __grid_constant__ CUtensorMap map_x, const GemmI8Args g) {
-    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    extern __shared__ __align__(16) unsigned char smem_raw[];   // (aligned to 1024 by hand: the swizzled tiles)
     unsigned char *ring = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     __shared__ SkinnyShared sh;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -94,6 +186,14 @@ __global__ void __launch_bounds__(SK_THREADS) gemm_i8_skinny_kernel(const __grid
     uint32_t tmem_cols = 32;
     while (tmem_cols < (uint32_t)cols) tmem_cols *= 2;
 
+    auto load_stage = [&](int it) {
+        const int s = it % stages, k0 = (kb0 + it) * BK;
+        const uint32_t full = smem_u32(&sh.full[s]), dst = smem_u32(ring + s * stage_bytes);
+        mbar_expect_tx(full, stage_bytes);
+        tma_load_2d(dst, &map_w, k0, n0, full);
+        if (SWIGLU) tma_load_2d(dst + SK_W_BYTES / 2, &map_w, k0, g.n + n0, full);
+        tma_load_2d(dst + SK_W_BYTES, &map_x, k0, t0, full);
+    };
     if (threadIdx.x == 0) {
         for (int s = 0; s < stages; ++s) {
             mbar_init(smem_u32(&sh.full[s]), 1);
@@ -102,6 +202,9 @@ __global__ void __launch_bounds__(SK_THREADS) gemm_i8_skinny_kernel(const __grid
         mbar_init(smem_u32(&sh.done), 1);
         sh.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_proxy_async();
+        // the first copies leave before the block is set up: a short call is a chain of latencies
+        for (int it = 0; it < min(stages, n_it); ++it) load_stage(it);
     }
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem_base)), "r"(tmem_cols));
@@ -113,20 +216,10 @@ __global__ void __launch_bounds__(SK_THREADS) gemm_i8_skinny_kernel(const __grid
     const uint32_t tmem = sh.tmem_base;
 
     if (warp == 0 && lane == 0) {
-        int it = 0;
+        int it = min(stages, n_it);
         for (; it < n_it; ++it) {
-            const int s = it % stages;
-            if (!mbar_wait(smem_u32(&sh.empty[s]), ((it / stages) & 1) ^ 1, abort_flag)) break;
-            const uint32_t full = smem_u32(&sh.full[s]), dst = smem_u32(ring + s * stage_bytes);
-            const int k0 = (kb0 + it) * BK;
-            mbar_expect_tx(full, stage_bytes);
-            if (SWIGLU) {
-                tma_load_2d(dst, &map_w, k0, n0, full);
-                tma_load_2d(dst + SK_W_BYTES / 2, &map_w, k0, g.n + n0, full);
-            } else {
-                tma_load_2d(dst, &map_w, k0, n0, full);
-            }
-            tma_load_2d(dst + SK_W_BYTES, &map_x, k0, t0, full);
+            if (!mbar_wait(smem_u32(&sh.empty[it % stages]), ((it / stages) & 1) ^ 1, abort_flag)) break;
+            load_stage(it);
         }
         // every stage that was armed has landed before the ring is reused or the CTA ends
         for (int j = it > stages ? it - stages : 0; j < it; ++j) mbar_drain(smem_u32(&sh.full[j % stages]), (j / stages) & 1);
@@ -145,6 +238,11 @@ __global__ void __launch_bounds__(SK_THREADS) gemm_i8_skinny_kernel(const __grid
         tc_commit(smem_u32(&sh.done));
     }
     __syncwarp();
+    if (threadIdx.x >= 128) {   // the scales arrive while the products run
+        const int r = threadIdx.x - 128, row = SWIGLU ? n0 + (r & 63) : n0 + r;
+        sh.ws[r] = row < g.n ? g.ws[row + (SWIGLU && r >= 64 ? g.n : 0)] : 0.0f;
+        for (int c = r; c < cols; c += 128) sh.xs[c] = t0 + c < g.T ? g.xs[t0 + c] : 0.0f;
+    }
     if (lane == 0) mbar_drain(smem_u32(&sh.done), 0);
     __syncwarp();
     tc_fence_after();
@@ -153,13 +251,14 @@ __global__ void __launch_bounds__(SK_THREADS) gemm_i8_skinny_kernel(const __grid
     // ---- sums into shared memory, [token column][128 rows]
     const int ncol = min(cols, g.T - t0);
     int32_t *red = reinterpret_cast<int32_t *>(ring);
-    for (int c = 0; c < ncol; c += 16) {
+    const int q = warp & 3;   // a warp reads the TMEM lanes of its quarter; the two warps of a quarter share the columns
+    for (int c = (warp >> 2) * 16; c < ncol; c += 32) {
         uint32_t v[16];
-        tc_ld16(tmem + ((uint32_t)(warp * 32) << 16) + c, v);
+        tc_ld16(tmem + ((uint32_t)(q * 32) << 16) + c, v);
         tc_wait_ld();
 #pragma unroll
         for (int j = 0; j < 16; ++j)
-            if (c + j < ncol) red[(c + j) * 128 + warp * 32 + lane] = (int32_t)v[j];
+            if (c + j < ncol) red[(c + j) * 128 + q * 32 + lane] = (int32_t)v[j];
     }
     tc_fence_before();
     if (split > 1) cluster_sync();
@@ -171,24 +270,35 @@ __global__ void __launch_bounds__(SK_THREADS) gemm_i8_skinny_kernel(const __grid
     constexpr int QUADS = SWIGLU ? 16 : 32;
     const int items = ncol * QUADS;
     const uint32_t red_s = smem_u32(red);
+    const int4 *red4 = reinterpret_cast<const int4 *>(red);
+    auto at_own = [](int c, int row) { return c * 32 + row / 4; };
     for (int i = items * rank / split + threadIdx.x; i < items * (rank + 1) / split; i += SK_THREADS) {
         const int c = i / QUADS, row = (i % QUADS) * 4;
         if (n0 + row >= g.n) continue;
         int4 a = make_int4(0, 0, 0, 0), b = make_int4(0, 0, 0, 0);
-        for (int r = 0; r < split; ++r) {
-            const uint32_t at = red_s + (uint32_t)(c * 128 + row) * 4;
-            const int4 p = ld_cluster4(map_to_cta(at, (uint32_t)r));
-            a = make_int4(a.x + p.x, a.y + p.y, a.z + p.z, a.w + p.w);
-            if (SWIGLU) {
-                const int4 q = ld_cluster4(map_to_cta(at + 64 * 4, (uint32_t)r));
-                b = make_int4(b.x + q.x, b.y + q.y, b.z + q.z, b.w + q.w);
+        const uint32_t at = red_s + (uint32_t)(c * 128 + row) * 4;
+        if (split == 1) {
+            a = red4[at_own(c, row)];
+            if (SWIGLU) b = red4[at_own(c, row + 64)];
+        } else {
+            // all loads leave before the first is used: a peer's shared memory is some hundred cycles away
+            int4 p[SK_MAX_SPLIT], u[SWIGLU ? SK_MAX_SPLIT : 1];
+#pragma unroll
+            for (int r = 0; r < SK_MAX_SPLIT; ++r) {
+                p[r] = r < split ? ld_cluster4(map_to_cta(at, (uint32_t)r)) : make_int4(0, 0, 0, 0);
+                if (SWIGLU) u[r] = r < split ? ld_cluster4(map_to_cta(at + 64 * 4, (uint32_t)r)) : make_int4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int r = 0; r < SK_MAX_SPLIT; ++r) {
+                a = make_int4(a.x + p[r].x, a.y + p[r].y, a.z + p[r].z, a.w + p[r].w);
+                if (SWIGLU) b = make_int4(b.x + u[r].x, b.y + u[r].y, b.z + u[r].z, b.w + u[r].w);
             }
         }
-        const float xs = g.xs[t0 + c];
-        const float4 w4 = *reinterpret_cast<const float4 *>(g.ws + n0 + row);
+        const float xs = sh.xs[c];
+        const float4 w4 = *reinterpret_cast<const float4 *>(&sh.ws[row]);
         float4 v = make_float4((float)a.x * xs * w4.x, (float)a.y * xs * w4.y, (float)a.z * xs * w4.z, (float)a.w * xs * w4.w);
         if (SWIGLU) {
-            const float4 u4 = *reinterpret_cast<const float4 *>(g.ws + g.n + n0 + row);
+            const float4 u4 = *reinterpret_cast<const float4 *>(&sh.ws[64 + row]);
             v = make_float4(silu_times(v.x, (float)b.x * xs * u4.x), silu_times(v.y, (float)b.y * xs * u4.y),
                             silu_times(v.z, (float)b.z * xs * u4.z), silu_times(v.w, (float)b.w * xs * u4.w));
         }
@@ -199,18 +309,20 @@ __global__ void __launch_bounds__(SK_THREADS) gemm_i8_skinny_kernel(const __grid
 }
 
 // ------------------------------------------------------------------------------------------------ many tokens
-constexpr int PR_THREADS = 192, PR_STAGES = 6;
+constexpr int PR_THREADS = 320, PR_STAGES = 6, PR_EPI_WARPS = 8;
 constexpr int PR_TILE = 256;                                   // tokens and accumulator columns of a pair's tile
 constexpr int PR_HALF_BYTES = 128 * BK;                        // a CTA's half of one operand
 constexpr int PR_STAGE_BYTES = 2 * PR_HALF_BYTES;
-constexpr int PR_STG_WARP = 32 * 144;                          // an epilogue warp's transposition buffer
-constexpr size_t PR_SMEM = (size_t)PR_STAGES * PR_STAGE_BYTES + 4 * PR_STG_WARP + 1024;
+constexpr int PR_PITCH = 80;                                   // 64 B of a row's outputs + 16: 16-byte accesses do not collide
+constexpr int PR_STG_WARP = 32 * PR_PITCH;                     // an epilogue warp's transposition buffer
+constexpr size_t PR_SMEM = (size_t)PR_STAGES * PR_STAGE_BYTES + PR_EPI_WARPS * PR_STG_WARP + 1024;
 constexpr int PR_GROUP_M = 16;                                 // token tiles that share a sweep over the weight tiles
 
 struct PairShared {
     alignas(8) unsigned long long full[PR_STAGES], empty[PR_STAGES], tmem_full[2], tmem_empty[2], mma_drain;
     uint32_t tmem_base;
     int abort_flag;
+    alignas(16) float ws[2][PR_TILE];   // channel scales of the tile (SwiGLU: gate, then up), per accumulator buffer
 };
 
 // tile number -> token tile, weight tile: groups of PR_GROUP_M token tiles, within a group the token tile runs fastest, so
@@ -227,7 +339,7 @@ __device__ __forceinline__ void pair_tile(const GemmI8Args &g, int tile, int &mt
 template <bool SWIGLU>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PR_THREADS, 1)
     gemm_i8_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const GemmI8Args g) {
-    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    extern __shared__ __align__(16) unsigned char smem_raw[];   // (aligned to 1024 by hand: the swizzled tiles)
     unsigned char *ring = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     unsigned char *stage_base = ring + PR_STAGES * PR_STAGE_BYTES;
     __shared__ PairShared sh;
@@ -242,7 +354,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PR_THREADS, 1)
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(smem_u32(&sh.tmem_full[b]), 1);
-            mbar_init(smem_u32(&sh.tmem_empty[b]), 8);   // used in the even CTA: four epilogue warps of either CTA
+            mbar_init(smem_u32(&sh.tmem_empty[b]), 2 * PR_EPI_WARPS);   // used in the even CTA: the epilogue warps of both
         }
         mbar_init(smem_u32(&sh.mma_drain), 1);
         sh.abort_flag = 0;
@@ -312,45 +424,50 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PR_THREADS, 1)
             mbar_drain(smem_u32(&sh.mma_drain), 0);
         }
     } else {
-        // ---------------- epilogue: warp w owns TMEM lanes 32*(w%4) .. +31 = rows of this CTA's half of the tile
-        const int q = warp & 3;
+        // ---------------- epilogue: warp w reads TMEM lanes 32*(w%4) .. +31 = rows of this CTA's half of the tile; the two
+        // warps of a quarter take alternate pieces of 64 bytes
+        const int q = warp & 3, c_first = warp >= 6 ? 32 : 0;
         unsigned char *stg = stage_base + (warp - 2) * PR_STG_WARP;
         uint32_t tcount = 0;
+        bool gave_up = false;   // after an expired wait a warp only keeps the others' barriers
         for (int tile = pair; tile < n_tiles; tile += pairs, ++tcount) {
             const int buf = tcount & 1;
             int mt, nt;
             pair_tile(g, tile, mt, nt);
-            bool ok = true;
-            if (lane == 0) ok = mbar_wait(smem_u32(&sh.tmem_full[buf]), (tcount >> 1) & 1, abort_flag);
-            ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
-            if (!ok) break;
-            tc_fence_after();
             const int row0 = mt * PR_TILE + (int)rank * 128 + q * 32;   // token of lane 0
-            const float xs = row0 + lane < g.T ? g.xs[row0 + lane] : 0.0f;
-            const uint32_t tm = tmem_base + buf * PR_TILE + ((uint32_t)(q * 32) << 16);
             const int col0 = nt * (SWIGLU ? 128 : PR_TILE);
-            // 32 columns at a time: a lane holds one token's; turned through shared memory so that a store covers whole
+            // scales come while the tile is still being multiplied; the barrier of the epilogue warps also keeps a buffer
+            // from being overwritten while a warp is two tiles behind
+            const float xs = row0 + lane < g.T ? g.xs[row0 + lane] : 0.0f;
+            const int wc = threadIdx.x - 64, wcol = col0 + (SWIGLU ? wc & 127 : wc);
+            sh.ws[buf][wc] = wcol < g.n ? g.ws[wcol + (SWIGLU && wc >= 128 ? g.n : 0)] : 0.0f;
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+            bool ok = true;
+            if (lane == 0 && !gave_up) ok = mbar_wait(smem_u32(&sh.tmem_full[buf]), (tcount >> 1) & 1, abort_flag);
+            ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
+            gave_up |= !ok;
+            if (gave_up) continue;
+            tc_fence_after();
+            const uint32_t tm = tmem_base + buf * PR_TILE + ((uint32_t)(q * 32) << 16);
+            const float4 *w4 = reinterpret_cast<const float4 *>(sh.ws[buf]), *u4 = w4 + 32;
+            // 64 bytes of outputs at a time: a lane holds one token's; turned through shared memory so that a store covers whole
             // 16-byte pieces of consecutive columns
             if (SWIGLU || g.out == SPICE_OUT_BF16) {
-                constexpr int PITCH = 80;   // 64 B of bf16 per row + 16
 #pragma unroll 1
-                for (int c = 0; c < (SWIGLU ? 128 : PR_TILE); c += 32) {
+                for (int c = c_first; c < (SWIGLU ? 128 : PR_TILE); c += 64) {
                     if (col0 + c >= g.n) break;
                     uint32_t v[32], u[SWIGLU ? 32 : 1];
                     tc_ld32(tm + c, v);
                     if constexpr (SWIGLU) tc_ld32(tm + 128 + c, u);
                     tc_wait_ld();
-                    const float4 *w4 = reinterpret_cast<const float4 *>(g.ws + col0 + c);
-                    const float4 *u4 = reinterpret_cast<const float4 *>(g.ws + (SWIGLU ? g.n : 0) + col0 + c);
                     uint32_t pk[16];
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        // (g.n is a multiple of 8: a piece of eight columns is inside or outside)
-                        const float4 w = col0 + c + 4 * j < g.n ? w4[j] : make_float4(0.f, 0.f, 0.f, 0.f);
+                        const float4 w = w4[c / 4 + j];
                         float a[4] = {(float)(int32_t)v[4 * j] * xs * w.x, (float)(int32_t)v[4 * j + 1] * xs * w.y,
                                       (float)(int32_t)v[4 * j + 2] * xs * w.z, (float)(int32_t)v[4 * j + 3] * xs * w.w};
                         if constexpr (SWIGLU) {
-                            const float4 z = col0 + c + 4 * j < g.n ? u4[j] : make_float4(0.f, 0.f, 0.f, 0.f);
+                            const float4 z = u4[c / 4 + j];
                             a[0] = silu_times(a[0], (float)(int32_t)u[4 * j] * xs * z.x);
                             a[1] = silu_times(a[1], (float)(int32_t)u[4 * j + 1] * xs * z.y);
                             a[2] = silu_times(a[2], (float)(int32_t)u[4 * j + 2] * xs * z.z);
@@ -361,38 +478,36 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PR_THREADS, 1)
                     }
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
-                        *reinterpret_cast<uint4 *>(stg + lane * PITCH + k * 16) = make_uint4(pk[4 * k], pk[4 * k + 1], pk[4 * k + 2], pk[4 * k + 3]);
+                        *reinterpret_cast<uint4 *>(stg + lane * PR_PITCH + k * 16) = make_uint4(pk[4 * k], pk[4 * k + 1], pk[4 * k + 2], pk[4 * k + 3]);
                     __syncwarp();
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int rr = i * 8 + (lane >> 2), part = lane & 3, col = col0 + c + part * 8;
-                        const uint4 val = *reinterpret_cast<const uint4 *>(stg + rr * PITCH + part * 16);
+                        const uint4 val = *reinterpret_cast<const uint4 *>(stg + rr * PR_PITCH + part * 16);
                         if (row0 + rr < g.T && col < g.n)
                             *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(g.y) + (size_t)(row0 + rr) * g.n + col) = val;
                     }
                     __syncwarp();
                 }
             } else {
-                constexpr int PITCH = 144;   // 128 B of fp32 per row + 16
 #pragma unroll 1
-                for (int c = 0; c < PR_TILE; c += 32) {
+                for (int c = c_first / 2; c < PR_TILE; c += 32) {
                     if (col0 + c >= g.n) break;
-                    uint32_t v[32];
-                    tc_ld32(tm + c, v);
+                    uint32_t v[16];
+                    tc_ld16(tm + c, v);
                     tc_wait_ld();
-                    const float4 *w4 = reinterpret_cast<const float4 *>(g.ws + col0 + c);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float4 w = col0 + c + 4 * j < g.n ? w4[j] : make_float4(0.f, 0.f, 0.f, 0.f);
-                        *reinterpret_cast<float4 *>(stg + lane * PITCH + j * 16) =
+                    for (int j = 0; j < 4; ++j) {
+                        const float4 w = w4[c / 4 + j];
+                        *reinterpret_cast<float4 *>(stg + lane * PR_PITCH + j * 16) =
                             make_float4((float)(int32_t)v[4 * j] * xs * w.x, (float)(int32_t)v[4 * j + 1] * xs * w.y,
                                         (float)(int32_t)v[4 * j + 2] * xs * w.z, (float)(int32_t)v[4 * j + 3] * xs * w.w);
                     }
                     __syncwarp();
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int rr = i * 4 + (lane >> 3), part = lane & 7, col = col0 + c + part * 4;
-                        const float4 val = *reinterpret_cast<const float4 *>(stg + rr * PITCH + part * 16);
+                    for (int i = 0; i < 4; ++i) {
+                        const int rr = i * 8 + (lane >> 2), part = lane & 3, col = col0 + c + part * 4;
+                        const float4 val = *reinterpret_cast<const float4 *>(stg + rr * PR_PITCH + part * 16);
                         if (row0 + rr < g.T && col < g.n) store4(g, (size_t)(row0 + rr) * g.n + col, val);
                     }
                     __syncwarp();
@@ -416,14 +531,23 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PR_THREADS, 1)
 bool prepare_device(int dev) {
     static std::atomic<bool> done[64];
     if (done[dev].load(std::memory_order_acquire)) return true;
-    const int most = 227 * 1024 - 1024;
     bool ok = true;
-    ok &= cudaFuncSetAttribute(gemm_i8_skinny_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) == cudaSuccess;
-    ok &= cudaFuncSetAttribute(gemm_i8_skinny_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) == cudaSuccess;
-    ok &= cudaFuncSetAttribute(gemm_i8_pair_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) == cudaSuccess;
-    ok &= cudaFuncSetAttribute(gemm_i8_pair_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, most) == cudaSuccess;
+    ok &= cudaFuncSetAttribute(gemm_i8_skinny_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, SK_MAX_SMEM) == cudaSuccess;
+    ok &= cudaFuncSetAttribute(gemm_i8_skinny_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, SK_MAX_SMEM) == cudaSuccess;
+    ok &= cudaFuncSetAttribute(gemm_i8_pair_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PR_SMEM) == cudaSuccess;
+    ok &= cudaFuncSetAttribute(gemm_i8_pair_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PR_SMEM) == cudaSuccess;
     if (ok) done[dev].store(true, std::memory_order_release);
     return ok;
+}
+
+template <int TT, bool SWIGLU>
+void launch_dot(const GemmI8Args &g, const int8_t *x, const int8_t *w, int sms, cudaStream_t st) {
+    constexpr int COLS = SWIGLU || TT == 1 ? 1 : 2;
+    const int warps = g.n / COLS;
+    if (warps < 32 * sms && g.k >= 2048)   // too few warps to keep enough bytes in flight
+        gemm_i8_dot_kernel<TT, SWIGLU, 4><<<(warps + 1) / 2, DOT_THREADS, 0, st>>>(x, w, g);
+    else
+        gemm_i8_dot_kernel<TT, SWIGLU, 1><<<(warps + 7) / 8, DOT_THREADS, 0, st>>>(x, w, g);
 }
 
 template <bool SWIGLU>
@@ -433,17 +557,43 @@ spice_status launch_gemm_i8(GemmI8Args g, const int8_t *x, const int8_t *w, cuda
     if (sms <= 0 || !prepare_device(dev)) return SPICE_ERR_CUDA;
     const int w_rows = SWIGLU ? 2 * g.n : g.n;
     const int kblocks = (g.k + BK - 1) / BK;
+    const int64_t weights = (int64_t)w_rows * g.k;
+    // The dot products' reads of the tokens grow with their number, the tensor cores' do not matter up to 64 of them.
+    // 2048 x 2816, 5632 x 2048, 11264 x 2048, 3584 x 20480, 40960 x 3584 weights, us with dot products / tensor cores:
+    // 1 token 3.5/7.0, 4.7/8.5, 6.1/9.9, 15/17, 29/27;  4 tokens 4.2/7.5, 4.9/8.4, 8.2/10, 27/18, 31/28;
+    // 8 tokens 4.8/7.7, 7.2/8.6, 11/10, 50/18, 40/28
+    if (g.T == 1 || (g.T <= 4 && weights <= (48 << 20)) || (g.T <= DOT_MAX_TOKENS && weights <= (16 << 20))) {
+        if (g.T == 1) launch_dot<1, SWIGLU>(g, x, w, sms, st);
+        else if (g.T == 2) launch_dot<2, SWIGLU>(g, x, w, sms, st);
+        else if (g.T <= 4) launch_dot<4, SWIGLU>(g, x, w, sms, st);
+        else launch_dot<8, SWIGLU>(g, x, w, sms, st);
+        return cudaGetLastError() == cudaSuccess ? SPICE_OK : SPICE_ERR_CUDA;
+    }
     CUtensorMap map_x, map_w;
-    if (g.T <= 256) {
-        const int tile_n = SWIGLU ? 64 : 128;
-        const int row_tiles = (g.n + tile_n - 1) / tile_n;
-        g.cols = min(256, (g.T + 15) & ~15);
-        const int token_tiles = (g.T + g.cols - 1) / g.cols;
-        const int tiles = row_tiles * token_tiles;
-        g.split = max(1, min(min(8, kblocks), sms / tiles));
+    g.m_tiles = (g.T + PR_TILE - 1) / PR_TILE;
+    g.n_tiles = SWIGLU ? (g.n + 127) / 128 : (g.n + PR_TILE - 1) / PR_TILE;
+    if ((int64_t)g.m_tiles * g.n_tiles > 0x3fffffff) return SPICE_ERR_UNSUPPORTED_SHAPE;
+    const int tile_n = SWIGLU ? 64 : 128;
+    const int row_tiles = (g.n + tile_n - 1) / tile_n;
+    g.cols = ((g.T <= 128 ? g.T : (g.T + 1) / 2) + 15) & ~15;
+    const int token_tiles = (g.T + g.cols - 1) / g.cols;
+    const int tiles = row_tiles * token_tiles;
+    // Up to 256 tokens either tensor-core kernel can be the faster one: in ns, a start, a term for the sums that pass through
+    // shared memory and the bytes that the CTAs bring in at 12 TB/s, against a start and 300 ns per 128 of the reduction for
+    // every round of the pairs over their tiles.  Measured, few-token kernel / pairs, us: 128 tokens 2048 x 2816 12.3 / 13.6,
+    // 5632 x 2048 (SwiGLU) 13.7 / 12.2, 3584 x 20480 22 / 54, 40960 x 3584 (SwiGLU) 35 / 39, 512 x 512 8.0 / 7.4;  256 tokens
+    // 14.0 / 13.7, 13.7 / 12.3, 30 / 54, 58 / 40, 8.0 / 7.5.
+    const int64_t rounds = ((int64_t)g.m_tiles * g.n_tiles + sms / 2 - 1) / (sms / 2);
+    const int64_t few_ns = 5500 + 40 * g.cols + (int64_t)tiles * kblocks * (SK_W_BYTES + g.cols * BK) / 12000;
+    const int64_t pair_ns = 7000 + rounds * kblocks * 300 + (rounds - 1) * 2000;
+    if (g.T <= 256 && few_ns <= pair_ns) {
+        // split the reduction until two CTAs per SM are busy, three stages each at least
+        g.split = max(1, std::min({SK_MAX_SPLIT, 2 * sms / tiles, kblocks / 3}));
+        int per_sm = (tiles * g.split + sms - 1) / sms;
+        per_sm = std::max(g.split > 1 ? 2 : 1, std::min(per_sm, 3));   // (clusters pack badly with one CTA per SM)
         const int per_cta = (kblocks + g.split - 1) / g.split;
         const int stage_bytes = SK_W_BYTES + g.cols * BK;
-        g.stages = max(1, min(min(per_cta, SK_MAX_STAGES), (200 * 1024) / stage_bytes));
+        g.stages = max(1, min(min(per_cta, SK_MAX_STAGES), (228 / per_sm - 4) * 1024 / stage_bytes));
         const size_t red = (size_t)min(g.cols, g.T) * 512;
         // A CTA takes at least the share of shared memory that it takes of TMEM (512 columns against 228 KB with the 1 KB
         // the system adds): however the CTAs of calls on different streams mix on an SM, no TMEM allocation has to wait,
@@ -467,13 +617,10 @@ spice_status launch_gemm_i8(GemmI8Args g, const int8_t *x, const int8_t *w, cuda
         lc.numAttrs = g.split > 1 ? 1 : 0;
         return cudaLaunchKernelEx(&lc, gemm_i8_skinny_kernel<SWIGLU>, map_w, map_x, g) == cudaSuccess ? SPICE_OK : SPICE_ERR_CUDA;
     }
-    g.m_tiles = (g.T + PR_TILE - 1) / PR_TILE;
-    g.n_tiles = SWIGLU ? (g.n + 127) / 128 : (g.n + PR_TILE - 1) / PR_TILE;
-    if ((int64_t)g.m_tiles * g.n_tiles > 0x3fffffff) return SPICE_ERR_UNSUPPORTED_SHAPE;
     if (!tc_encode_map2_bytes(&map_x, x, (uint64_t)g.T, (uint64_t)g.k, 128) ||
         !tc_encode_map2_bytes(&map_w, w, (uint64_t)w_rows, (uint64_t)g.k, 128))
         return SPICE_ERR_CUDA;
-    const int pairs = min(sms / 2, g.m_tiles * g.n_tiles);
+    const int pairs = max(1, min(sms / 2, g.m_tiles * g.n_tiles));
     gemm_i8_pair_kernel<SWIGLU><<<2 * pairs, PR_THREADS, PR_SMEM, st>>>(map_x, map_w, g);
     return cudaGetLastError() == cudaSuccess ? SPICE_OK : SPICE_ERR_CUDA;
 }

@@ -10,13 +10,14 @@
 // score 0, so a row that a mask leaves nothing still yields valid expert ids with gates of 0.
 //
 // Selection is a comparison of real numbers; fp32 scores decide it wherever two of them are further apart than their
-// error bound.  A row in which two neighbours of the order (or the last group that stays and the first that does not) are
-// nearer than that is decided by the same formulas in fp64 (slow_row; about one row in a thousand at 256 experts).
-// Where the order is that of the logits nothing is rounded and the first answer stands.
+// error bound.  Where two neighbours of the order are nearer than that, every expert that could be among the winners is
+// evaluated by the same formulas in fp64, one per lane, and ranked (slow_row, a row at a time, where more than 32 could
+// be); so are the groups where the last one that stays and the first that does not are that close.  Where the order is
+// that of the logits nothing is rounded and the first answer stands.
 //
-// One warp per token; keys live in registers as integers that order like the floats, a round of the selection is one
-// warp-wide integer maximum for the key and one minimum for the index.  Bytes are few (4 N per token): the bound is the
-// issue of the K + 1 rounds.
+// One warp per token.  Keys live in registers as integers that order like the floats: a round of the selection is one
+// warp-wide integer maximum, a ballot and a shuffle.  With groups, the keys pass through shared memory and only those of
+// the groups that stay are read back.  Bytes are few (4 N per token): the bound is the issue of instructions.
 #include "entry.cuh"
 #include "spice_internal.cuh"
 
@@ -32,7 +33,7 @@ struct RouteArgs {
     const float *bias;     // [N] or null
     int32_t *idx;          // [T, K]
     float *gate;           // [T, K]
-    int32_t T, N, K, n_groups, top_groups, norm_topk;
+    int32_t T, N, K, n_groups, top_groups, norm_topk, sigmoid, pair;
     uint32_t size_magic;   // ceil(2^32 / (N / n_groups)): e / size as a high product (exact for e < 1024); 0 for size 1
     float scale;
 };
@@ -71,66 +72,89 @@ __device__ __forceinline__ void warp_best64(unsigned long long &key, int &e) {
     }
 }
 
-// The selection of one row in fp64, for rows whose fp32 scores are too close to call.  key: [N] doubles of this warp in
-// shared memory.  Returns the winners, lane k holding the k-th.
-template <bool SIGMOID, bool PAIR>
-__device__ __noinline__ int slow_row(const RouteArgs &a, const float *l, double *key, int lane) {
-    const double ninf = -(double)INFINITY;
-    double m = ninf, s = 0.0;
-    if (!SIGMOID) {
+// What the groups' values are made of, for the n_groups groups of `size` keys in shared memory: lane g gets group g's.
+template <typename F>
+__device__ __forceinline__ F group_value(const RouteArgs &a, const F *keys, int size, int lane) {
+    // `width` lanes share a group: each looks at every width-th member, then they merge
+    const int G = a.n_groups, width = 32 >> (32 - __clz(G - 1));
+    const int g = lane / width;
+    F b0 = -(F)INFINITY, b1 = b0;   // the two largest
+    if (g < G) {
+        for (int j = lane & (width - 1); j < size; j += width) {
+            const F x = keys[g * size + j];
+            b1 = max(b1, min(b0, x));
+            b0 = max(b0, x);
+        }
+    }
+    for (int o = width >> 1; o > 0; o >>= 1) {
+        const F o0 = __shfl_xor_sync(FULL, b0, o), o1 = __shfl_xor_sync(FULL, b1, o);
+        b1 = max(max(b1, o1), min(b0, o0));
+        b0 = max(b0, o0);
+    }
+    const F value = a.pair && b1 > -(F)INFINITY ? b0 + b1 : b0;
+    return __shfl_sync(FULL, value, (lane * width) & 31);
+}
+
+// Rank of lane's key among those of lanes 0..n-1 (equal keys: the smaller `tag` first).
+template <typename F>
+__device__ __forceinline__ int rank_of(F key, int tag, int n) {
+    int rank = 0;
+    for (int j = 0; j < n; ++j) {
+        const F k = __shfl_sync(FULL, key, j);
+        const int t = __shfl_sync(FULL, tag, j);
+        rank += k > key || (k == key && t < tag) ? 1 : 0;
+    }
+    return rank;
+}
+
+// fp64 scores of a row: softmax's largest logit and sum, then any expert's key
+struct Score64 {
+    double m, s;
+    __device__ __noinline__ Score64(const RouteArgs &a, const float *l, int lane) : m(-(double)INFINITY), s(0.0) {
+        if (a.sigmoid) return;
         for (int e = lane; e < a.N; e += 32)
-            if (l[e] > -INFINITY) m = fmax(m, (double)l[e]);
+            if (available(a, l, e)) m = fmax(m, (double)l[e]);
         for (int o = 16; o > 0; o >>= 1) m = fmax(m, __shfl_xor_sync(FULL, m, o));
         for (int e = lane; e < a.N; e += 32)
-            if (l[e] > -INFINITY) s += (double)l[e] == m ? 1.0 : exp((double)l[e] - m);
+            if (available(a, l, e)) s += (double)l[e] == m ? 1.0 : exp((double)l[e] - m);
         for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(FULL, s, o);
     }
-    for (int e = lane; e < a.N; e += 32) {
+    static __device__ __forceinline__ bool available(const RouteArgs &a, const float *l, int e) {
+        return l[e] > -INFINITY && (!a.bias || a.bias[e] > -INFINITY);   // NaN compares false
+    }
+    __device__ __noinline__ double key(const RouteArgs &a, const float *l, int e) const {
+        if (!available(a, l, e)) return -(double)INFINITY;
         const double v = l[e];
-        const double sc = SIGMOID ? 1.0 / (1.0 + exp(-v)) : (v == m ? 1.0 : exp(v - m)) / s;
-        const double k = sc + (a.bias ? (double)a.bias[e] : 0.0);
-        key[e] = v > ninf && k > ninf ? k : ninf;
+        const double sc = a.sigmoid ? 1.0 / (1.0 + exp(-v)) : (v == m ? 1.0 : exp(v - m)) / s;
+        return sc + (a.bias ? (double)a.bias[e] : 0.0);
     }
+};
+
+// The groups that stay, in fp64.  keys: [N] doubles of this warp in shared memory.
+__device__ __noinline__ uint32_t slow_groups(const RouteArgs &a, const float *l, double *keys, int size, int lane) {
+    const Score64 sc(a, l, lane);
     __syncwarp();
-    uint32_t open = FULL;
-    const int size = a.N / a.n_groups;
-    if (a.n_groups > 1) {
-        unsigned long long gk = 0;   // lane g: the value of group g
-        if (lane < a.n_groups) {
-            double b0 = ninf, b1 = ninf;
-            for (int j = 0; j < size; ++j) {
-                const double v = key[lane * size + j];
-                if (v > b0) {
-                    b1 = b0;
-                    b0 = v;
-                } else if (v > b1) {
-                    b1 = v;
-                }
-            }
-            gk = ordered64(PAIR && b1 > ninf ? b0 + b1 : b0);
-        }
-        open = 0;
-        for (int i = 0; i < a.top_groups; ++i) {
-            unsigned long long k = gk;
-            int g = lane;
-            warp_best64(k, g);
-            open |= 1u << g;
-            if (lane == g) gk = 0;
-        }
-    }
-    if (!a.bias) {   // the winners' order is that of the logits (fp64 scores of large ones may coincide)
-        __syncwarp();
-        for (int e = lane; e < a.N; e += 32) key[e] = l[e] > -INFINITY ? (double)l[e] : ninf;
-        __syncwarp();
-    }
+    for (int e = lane; e < a.N; e += 32) keys[e] = sc.key(a, l, e);
+    __syncwarp();
+    const double v = group_value<double>(a, keys, size, lane);
+    const int rank = rank_of<double>(v, lane, a.n_groups);
+    return __ballot_sync(FULL, lane < a.n_groups && rank < a.top_groups);
+}
+
+// The winners of one row in fp64 among the experts of the open groups, round by round: rows in which more than 32 experts
+// could be among them (many equal keys).  Returns lane k's winner k.
+__device__ __noinline__ int slow_row(const RouteArgs &a, const float *l, double *keys, uint32_t open, int lane) {
+    const Score64 sc(a, l, lane);
+    __syncwarp();
+    for (int e = lane; e < a.N; e += 32) keys[e] = sc.key(a, l, e);
     int mine = 0;
     for (int i = 0; i < a.K; ++i) {
+        __syncwarp();
         unsigned long long k = 0;
         int e = a.N;
         for (int j = lane; j < a.N; j += 32) {
-            if (a.n_groups > 1 && !((open >> group_of(a, j)) & 1u)) continue;
-            const double v = key[j];
-            if (v != v) continue;   // taken
+            const double v = keys[j];
+            if (v != v || !((open >> group_of(a, j)) & 1u)) continue;   // NaN: taken
             const unsigned long long kj = ordered64(v);
             if (kj > k) {
                 k = kj;
@@ -139,17 +163,28 @@ __device__ __noinline__ int slow_row(const RouteArgs &a, const float *l, double 
         }
         warp_best64(k, e);
         if (lane == i) mine = e;
-        __syncwarp();
-        if (lane == 0) key[e] = __longlong_as_double(0x7ff8000000000000ll);
-        __syncwarp();
+        if (lane == 0) keys[e] = __longlong_as_double(0x7ff8000000000000ll);
     }
+    __syncwarp();
     return mine;
 }
 
-// V: experts per lane (e = lane + 32 i)
-template <int V, bool SIGMOID, bool PAIR>
+// fast exponential and sigmoid: the keys' error bound covers them (the gates use the accurate functions)
+__device__ __forceinline__ float fast_exp(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x * 1.4426950408889634f));
+    return y;
+}
+__device__ __forceinline__ float fast_sigmoid(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(1.0f + fast_exp(-x)));
+    return y;
+}
+
+// V: experts per lane (e = lane + 32 i).  VS: keys per lane in the selection, those of the groups that stay
+template <int V, int VS>
 __global__ void __launch_bounds__(WARPS * 32) route_scored_kernel(const RouteArgs a) {
-    extern __shared__ double sh_keys[];   // [WARPS][N], also the fp32 values of a row's groups
+    extern __shared__ double sh_keys[];   // with groups or a bias: [WARPS][N] doubles, also the fp32 keys; then the open groups
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const long long t = (long long)blockIdx.x * WARPS + warp;
     if (t >= a.T) return;   // warp-uniform; no block-wide barrier below
@@ -157,19 +192,21 @@ __global__ void __launch_bounds__(WARPS * 32) route_scored_kernel(const RouteArg
     double *shd = sh_keys + (size_t)warp * a.N;
     float *shf = reinterpret_cast<float *>(shd);
     const int N = a.N, K = a.K;
+    const bool grouped = a.n_groups > 1, by_score = a.bias != nullptr || a.pair;   // else everything goes by the logits
 
-    float v[V], b[V];
+    float v[V], b[V];   // (b: only with a bias)
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         const int e = lane + 32 * i;
         v[i] = e < N ? l[e] : -INFINITY;
         b[i] = a.bias && e < N ? a.bias[e] : 0.0f;
-        if (!(v[i] > -INFINITY) || !(b[i] > -INFINITY)) v[i] = -INFINITY;   // NaN too
     }
-    // ---- scores
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+        if (!(v[i] > -INFINITY) || !(b[i] > -INFINITY)) v[i] = -INFINITY;   // NaN too
+    // ---- scores and keys
     float m = -INFINITY, inv = 1.0f;
-    const bool by_score = a.bias != nullptr || PAIR;   // else everything goes by the logits
-    if (!SIGMOID) {
+    if (!a.sigmoid) {
         uint32_t top = 0;
 #pragma unroll
         for (int i = 0; i < V; ++i) top = max(top, ordered(v[i]));
@@ -177,107 +214,141 @@ __global__ void __launch_bounds__(WARPS * 32) route_scored_kernel(const RouteArg
         if (by_score || !a.norm_topk) {
             float s = 0.0f;
 #pragma unroll
-            for (int i = 0; i < V; ++i) s += v[i] == m ? (m > -INFINITY ? 1.0f : 0.0f) : expf(v[i] - m);
+            for (int i = 0; i < V; ++i) s += v[i] == m ? (m > -INFINITY ? 1.0f : 0.0f) : fast_exp(v[i] - m);
             s = warp_add(s);
             inv = s > 0.0f ? 1.0f / s : 0.0f;
         }
     }
+    // Two keys nearer than tol (plus the rounding of score + bias) are not told apart.  A sigmoid score is off by at most
+    // s (1 - s) (1.2 |x| + 2) 2^-23 from the exponential and 1.5 * 2^-23 s from sum and reciprocal: below 3.5e-7.  A
+    // softmax score by (1.2 |x| + 2) 2^-23 e^x / sum, with |x| e^x < 0.37, and the V + 5 additions and the quotient: below
+    // (13 + V) / 2 * 2^-23 of the largest score.
+    const float tol = a.sigmoid ? 1e-6f : (13 + V) * 1.2e-7f * inv;
     uint32_t key[V];
-    float tol = 0.0f;    // keys nearer than this (plus their own rounding) are not told apart
-    if (by_score) {
-        // expf within 2 ulp, its argument and the sums and quotients behind it: below (13 + V) half ulps of the score
-        tol = SIGMOID ? 2e-6f : (13 + V) * 1.2e-7f * inv;
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const float sc = SIGMOID ? 1.0f / (1.0f + expf(-v[i])) : (v[i] == m ? 1.0f : expf(v[i] - m)) * inv;
-            const float val = v[i] > -INFINITY ? sc + b[i] : -INFINITY;
-            const int e = lane + 32 * i;
-            key[i] = e < N ? ordered(a.bias ? val : v[i]) : 0u;
-            if (PAIR && e < N) shf[e] = val;
+    for (int i = 0; i < V; ++i) {
+        const int e = lane + 32 * i;
+        float val = v[i];
+        if (by_score && v[i] > -INFINITY)
+            val = (a.sigmoid ? fast_sigmoid(v[i]) : (v[i] == m ? 1.0f : fast_exp(v[i] - m)) * inv) + b[i];
+        if (grouped && e < N) shf[e] = val;
+        key[i] = e < N ? ordered(a.bias ? val : v[i]) : 0u;
+    }
+    // ---- groups: only the keys of those that stay are read back (in the order of the experts)
+    uint32_t sel[VS], open = FULL;
+    int count = N;
+    const int size = N / a.n_groups;
+    int32_t *list = reinterpret_cast<int32_t *>(sh_keys + (size_t)WARPS * N) + warp * 32;
+    if (grouped) {
+        __syncwarp();
+        const int G = a.n_groups;
+        const float mine = group_value<float>(a, shf, size, lane);
+        const int rank = rank_of<float>(mine, lane, G);
+        open = __ballot_sync(FULL, lane < G && rank < a.top_groups);
+        if (by_score && a.top_groups < G) {
+            const float in = __shfl_sync(FULL, mine, __ffs(__ballot_sync(FULL, lane < G && rank == a.top_groups - 1)) - 1);
+            const float out = __shfl_sync(FULL, mine, __ffs(__ballot_sync(FULL, lane < G && rank == a.top_groups)) - 1);
+            if (out > -INFINITY && in - out <= 2.0f * tol + 2.4e-7f * (fabsf(in) + fabsf(out))) {   // warp-uniform
+                open = slow_groups(a, l, shd, size, lane);
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < V; ++i)   // the fp32 keys again: the doubles lay over them
+                    if (lane + 32 * i < N) shf[lane + 32 * i] = unordered(key[i]);
+            } else if (a.pair && !a.bias) {
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < V; ++i)   // the winners go by the logits
+                    if (lane + 32 * i < N) shf[lane + 32 * i] = v[i];
+            }
+        } else if (a.pair && !a.bias) {
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (lane + 32 * i < N) shf[lane + 32 * i] = v[i];
+        }
+        if ((open >> lane) & 1u) list[__popc(open & ((1u << lane) - 1u))] = lane;
+        __syncwarp();
+        count = a.top_groups * size;
+#pragma unroll
+        for (int i = 0; i < VS; ++i) {
+            const int c = lane + 32 * i;
+            sel[i] = 0u;
+            if (c < count) {
+                const int og = group_of(a, c);
+                sel[i] = ordered(shf[list[og] * size + c - og * size]);
+            }
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < V; ++i) key[i] = lane + 32 * i < N ? ordered(v[i]) : 0u;
+        for (int i = 0; i < VS; ++i) sel[i] = i < V ? key[i < V ? i : 0] : 0u;
     }
-    bool close = false;
-    // ---- groups
-    if (a.n_groups > 1) {
-        const int G = a.n_groups, size = N / G;
-        if (!PAIR) {
-#pragma unroll
-            for (int i = 0; i < V; ++i)
-                if (lane + 32 * i < N) shf[lane + 32 * i] = unordered(key[i]);
-        }
-        __syncwarp();
-        // `width` lanes share a group: each looks at every width-th member, then they merge
-        const int width = G <= 1 ? 32 : 32 >> (32 - __clz(G - 1));
-        const int g = lane / width;
-        float b0 = -INFINITY, b1 = -INFINITY;
-        if (g < G) {
-            for (int j = lane & (width - 1); j < size; j += width) {
-                const float x = shf[g * size + j];
-                if (PAIR) b1 = fmaxf(b1, fminf(b0, x));
-                b0 = fmaxf(b0, x);
-            }
-        }
-        for (int o = width >> 1; o > 0; o >>= 1) {
-            const float o0 = __shfl_xor_sync(FULL, b0, o);
-            if (PAIR) {
-                const float o1 = __shfl_xor_sync(FULL, b1, o);
-                b1 = fmaxf(fmaxf(b1, o1), fminf(b0, o0));
-            }
-            b0 = fmaxf(b0, o0);
-        }
-        const float value = PAIR && b1 > -INFINITY ? b0 + b1 : b0;
-        const float mine = __shfl_sync(FULL, value, (lane * width) & 31);   // lane g: group g
-        uint32_t gk = lane < G ? ordered(mine) : 0u, open = 0, last = 0;
-        for (int i = 0; i < a.top_groups; ++i) {
-            last = __reduce_max_sync(FULL, gk);
-            const int best = __ffs(__ballot_sync(FULL, gk == last)) - 1;
-            open |= 1u << best;
-            if (lane == best) gk = 0u;
-        }
-        if (by_score && a.top_groups < G) {
-            const float in = unordered(last), out = unordered(__reduce_max_sync(FULL, gk));
-            if (out > -INFINITY && in - out <= 2.0f * tol + 2.4e-7f * (fabsf(in) + fabsf(out))) close = true;
-        }
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int e = lane + 32 * i;
-            if (e < N && !((open >> group_of(a, e)) & 1u)) key[i] = 0u;
-        }
-    }
-    // ---- winners: lane k keeps the k-th
+    // ---- winners: lane k keeps the k-th, its place among the candidates and its key
     int win = 0;
-    uint32_t before = 0;
-    const bool check = a.bias != nullptr;
-    const int rounds = K + (check ? 1 : 0);
-    for (int k = 0; k < rounds; ++k) {
-        uint32_t best = key[0];
+    uint32_t won = 0u;
+    auto round = [&](int k) {
+        uint32_t best = sel[0];
+        int at = lane;
 #pragma unroll
-        for (int i = 1; i < V; ++i) best = max(best, key[i]);
-        best = __reduce_max_sync(FULL, best);
-        int at = N;
-#pragma unroll
-        for (int i = V - 1; i >= 0; --i)
-            if (key[i] == best) at = lane + 32 * i;
-        at = __reduce_min_sync(FULL, at);
-        if (check && best != 0u) {
-            const float cur = unordered(best);
-            if (k > 0 && cur > -INFINITY) {
-                const float prev = unordered(before);
-                if (prev - cur <= tol + 1.2e-7f * (fabsf(prev) + fabsf(cur))) close = true;
+        for (int i = 1; i < VS; ++i)
+            if (sel[i] > best) {
+                best = sel[i];
+                at = lane + 32 * i;
             }
-            before = best;
+        const uint32_t top = __reduce_max_sync(FULL, best);
+        at = __reduce_min_sync(FULL, best == top ? at : 0x7fffffff);   // equal keys: the smaller index
+        if (lane == k) {
+            win = at;
+            won = top;
         }
-        if (k == lane && k < K) win = at;
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (lane + 32 * i == at) key[i] = 0u;
+        for (int i = 0; i < VS; ++i)
+            if (at == lane + 32 * i) sel[i] = 0u;
+        return top;
+    };
+    // whether a key is not told apart from the one before it in the order
+    auto near = [&](uint32_t before, uint32_t after) {
+        const float x = unordered(before), y = unordered(after);
+        return after != 0u && y > -INFINITY && x - y <= tol + 1.2e-7f * (fabsf(x) + fabsf(y));
+    };
+    for (int k = 0; k < K; ++k) round(k);
+    int have = K;
+    bool close = false, many = false;
+    if (a.bias) {
+        // the first that is left is a possible winner too if the K-th is not told apart from it, and so on
+        const uint32_t last = __shfl_sync(FULL, won, K - 1), before = __shfl_up_sync(FULL, won, 1);
+        close = __any_sync(FULL, lane > 0 && lane < K && near(before, won));
+        while (true) {
+            if (have == 32) {   // no lane left: are there more?
+                uint32_t best = 0u;
+#pragma unroll
+                for (int i = 0; i < VS; ++i) best = max(best, sel[i]);
+                many = near(last, __reduce_max_sync(FULL, best));
+                close |= many;
+                break;
+            }
+            if (!near(last, round(have))) break;
+            close = true;
+            ++have;
+        }
+    }
+    if (grouped && lane < have) {
+        const int og = group_of(a, win);
+        win = list[og] * size + win - og * size;
     }
     if (close) {   // warp-uniform
-        __syncwarp();
-        win = slow_row<SIGMOID, PAIR>(a, l, shd, lane);
+        if (many) {
+            win = slow_row(a, l, shd, open, lane);
+        } else {
+            const Score64 sc(a, l, lane);
+            const double k64 = lane < have ? sc.key(a, l, win) : 0.0;
+            const int rank = rank_of<double>(k64, win, have);
+            // lane `rank` takes this lane's expert
+            int32_t *order = reinterpret_cast<int32_t *>(shf);
+            __syncwarp();
+            if (lane < have) order[rank] = win;
+            __syncwarp();
+            win = lane < K ? order[lane] : 0;
+        }
     }
     // ---- gates
     float x = -INFINITY, g = 0.0f;
@@ -289,16 +360,16 @@ __global__ void __launch_bounds__(WARPS * 32) route_scored_kernel(const RouteArg
     if (a.norm_topk) {
         // relative to the winners' largest, so that a row of tiny scores keeps its ratios:
         // softmax: e^(x - M); sigmoid: e^(min(x,0) - M) / (1 + e^-|x|)
-        const float y = SIGMOID ? fminf(x, 0.0f) : x;
+        const float y = a.sigmoid ? fminf(x, 0.0f) : x;
         const float M = unordered(__reduce_max_sync(FULL, ordered(y)));
         if (has) {
             g = y == M ? 1.0f : expf(y - M);
-            if (SIGMOID) g /= 1.0f + expf(-fabsf(x));
+            if (a.sigmoid) g = __fdividef(g, 1.0f + expf(-fabsf(x)));
         }
         const float s = warp_add(g);
-        g = s > 0.0f ? g / s : 0.0f;
+        g = s > 0.0f ? __fdividef(g, s) : 0.0f;
     } else if (has) {
-        g = SIGMOID ? 1.0f / (1.0f + expf(-x)) : (x == m ? 1.0f : expf(x - m)) * inv;
+        g = a.sigmoid ? __fdividef(1.0f, 1.0f + expf(-x)) : (x == m ? 1.0f : expf(x - m)) * inv;
     }
     if (lane < K) {
         a.idx[(size_t)t * K + lane] = win;
@@ -306,17 +377,11 @@ __global__ void __launch_bounds__(WARPS * 32) route_scored_kernel(const RouteArg
     }
 }
 
-template <bool SIGMOID, bool PAIR>
-spice_status launch_route_scored(const RouteArgs &a, cudaStream_t st) {
-    const unsigned grid = ((unsigned)a.T + WARPS - 1) / WARPS;
-    const size_t smem = (size_t)WARPS * a.N * sizeof(double);   // at most 32 KB
-    const int v = (a.N + 31) / 32;
-    if (v <= 2) route_scored_kernel<2, SIGMOID, PAIR><<<grid, WARPS * 32, smem, st>>>(a);
-    else if (v <= 4) route_scored_kernel<4, SIGMOID, PAIR><<<grid, WARPS * 32, smem, st>>>(a);
-    else if (v <= 8) route_scored_kernel<8, SIGMOID, PAIR><<<grid, WARPS * 32, smem, st>>>(a);
-    else if (v <= 16) route_scored_kernel<16, SIGMOID, PAIR><<<grid, WARPS * 32, smem, st>>>(a);
-    else route_scored_kernel<32, SIGMOID, PAIR><<<grid, WARPS * 32, smem, st>>>(a);
-    return cudaGetLastError() == cudaSuccess ? SPICE_OK : SPICE_ERR_CUDA;
+template <int V>
+void launch_route_scored(const RouteArgs &a, int vs, unsigned grid, size_t smem, cudaStream_t st) {
+    if (V >= 8 && vs <= V / 4) route_scored_kernel<V, (V >= 8 ? V / 4 : V)><<<grid, WARPS * 32, smem, st>>>(a);
+    else if (V >= 4 && vs <= V / 2) route_scored_kernel<V, (V >= 4 ? V / 2 : V)><<<grid, WARPS * 32, smem, st>>>(a);
+    else route_scored_kernel<V, V><<<grid, WARPS * 32, smem, st>>>(a);
 }
 
 }  // namespace
@@ -340,10 +405,17 @@ extern "C" spice_status spice_route_scored(const float *logits, const float *bia
     if (!logits || !idx || !gate || !aligned4(logits) || !aligned4(bias) || !aligned4(idx) || !aligned4(gate))
         return SPICE_ERR_INVALID_ARG;
     const uint32_t size = (uint32_t)(n_experts / n_groups);
-    const RouteArgs a{logits, bias, idx, gate, T, n_experts, top_k, n_groups, top_groups, norm_topk,
+    const int pair = n_groups > 1 && group_score == SPICE_GROUP_TOP2;
+    const RouteArgs a{logits, bias, idx, gate, T, n_experts, top_k, n_groups, top_groups, norm_topk, score == SPICE_SCORE_SIGMOID, pair,
                       size > 1 ? (uint32_t)((0x100000000ull + size - 1) / size) : 0u, scale};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const bool pair = n_groups > 1 && group_score == SPICE_GROUP_TOP2;
-    if (score == SPICE_SCORE_SIGMOID) return pair ? launch_route_scored<true, true>(a, st) : launch_route_scored<true, false>(a, st);
-    return pair ? launch_route_scored<false, true>(a, st) : launch_route_scored<false, false>(a, st);
+    const unsigned grid = ((unsigned)T + WARPS - 1) / WARPS;
+    const size_t smem = n_groups > 1 || bias ? (size_t)WARPS * (n_experts * sizeof(double) + 32 * sizeof(int32_t)) : 0;   // up to 33 KB
+    const int v = (n_experts + 31) / 32, vs = (int)(top_groups * size + 31) / 32;
+    if (v <= 2) launch_route_scored<2>(a, vs, grid, smem, st);
+    else if (v <= 4) launch_route_scored<4>(a, vs, grid, smem, st);
+    else if (v <= 8) launch_route_scored<8>(a, vs, grid, smem, st);
+    else if (v <= 16) launch_route_scored<16>(a, vs, grid, smem, st);
+    else launch_route_scored<32>(a, vs, grid, smem, st);
+    return cudaGetLastError() == cudaSuccess ? SPICE_OK : SPICE_ERR_CUDA;
 }

@@ -31,7 +31,7 @@ struct RowArgs {
     int8_t *q;                    // [T, d] or null
     float *scale;                 // [T], with q
     int d;
-    float eps;
+    float eps, inv_d;
 };
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
@@ -39,30 +39,82 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return *reinterpret_cast<uint32_t *>(&b);
 }
 
-// Normaliser of one row's codes: multiplying by f (a power of two) brings the largest magnitude into [1, 2).
+// What turns the values of a row with largest magnitude m into codes
 struct CodeScale {
-    float f, inv, mn;
-    __device__ __forceinline__ explicit CodeScale(float m) {
-        const int e = (int)(__float_as_uint(m) >> 23);               // biased exponent of m >= 0
-        f = __uint_as_float((uint32_t)min(max(254 - e, 1), 253) << 23);   // 2^(127 - e): at most 2^126
-        mn = m * f;
-        inv = m > 0.0f ? 127.0f / mn : 0.0f;
+    float m, c;   // c = 127 / m within 2^-23; 0 where m is not well inside fp32's range
+    __device__ __forceinline__ explicit CodeScale(float largest) {
+        m = largest;
+        float r = __fdividef(1.0f, m);
+        r = fmaf(r, fmaf(-m, r, 1.0f), r);
+        c = m > 0x1p-100f && m < 0x1p100f ? 127.0f * r : 0.0f;
     }
 };
 
-// nearest integer to 127 p / m, ties to even, exactly (see the top of the file).  The fp32 quotient is off by at most
-// 127 * 2^-22.9 < 2e-5.
-__device__ __forceinline__ int code_of(float p, const CodeScale &c) {
-    const float pn = p * c.f;
-    const float u = pn * c.inv;
-    float k = rintf(u);
-    if (fabsf(u - k) > 0.4999f) {
-        const float a = floorf(fabsf(u));
-        const float lhs = 254.0f * fabsf(pn), rhs = (2.0f * a + 1.0f) * c.mn;
-        const float up = lhs > rhs || (lhs == rhs && ((int)a & 1)) ? 1.0f : 0.0f;
-        k = copysignf(a + up, u);
+// nearest integer to 127 p / m, ties to even, exactly, for |127 p / m| between the integers a and a + 1: both products have
+// at most 24 significant bits.  (Weights meet this often: a value of half the row's largest is a tie at 63.5.)
+__device__ __forceinline__ float round_at_border(float p, float m, float a, bool odd) {
+    const float lhs = 254.0f * fabsf(p), rhs = (2.0f * a + 1.0f) * m;
+    return copysignf(a + (lhs > rhs || (lhs == rhs && odd) ? 1.0f : 0.0f), p);
+}
+
+// the codes of a row at the ends of fp32's range: m is brought into [1, 2) by a power of two first
+__device__ __noinline__ float code_scaled(float p, float m) {
+    if (!(m > 0.0f)) return 0.0f;
+    const int e = (int)(__float_as_uint(m) >> 23);                                    // biased exponent
+    const float f = __uint_as_float((uint32_t)min(max(254 - e, 1), 253) << 23);       // 2^(127 - e): at most 2^126
+    const float mn = m * f, pn = p * f;
+    const float u = pn * (127.0f / mn);
+    const float k = rintf(u);
+    const float a = floorf(fabsf(u));
+    return fabsf(u - k) > 0.4999f ? round_at_border(pn, mn, a, (int)a & 1) : k;
+}
+
+// Codes of 8 values as packed bytes.  p c + 1.5 * 2^23 in one rounding is the nearest integer to p c, its low byte the code;
+// p c is off by at most 127 * 2^-23 < 1.6e-5 from the quotient.  Where one of the values lies within 2e-5 of a border they
+// are looked at once more.
+__device__ __forceinline__ uint2 codes_of(const float (&p)[8], const CodeScale &c) {
+    constexpr float MAGIC = 12582912.0f;
+    uint32_t k[8];
+    float off = c.c > 0.0f ? 0.0f : 1.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float s = __fmaf_rn(p[j], c.c, MAGIC);
+        off = fmaxf(off, fabsf(__fmaf_rn(p[j], c.c, MAGIC - s)));
+        k[j] = __float_as_uint(s);
     }
-    return (int)k;
+    if (off > 0.49998f) {
+        if (c.c > 0.0f) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float n = __uint_as_float(k[j]) - MAGIC;      // the nearest integer; the other side of the border is n +- 1
+                const float d = __fmaf_rn(p[j], c.c, -n);
+                if (fabsf(d) > 0.49998f) {
+                    const bool outer = n != 0.0f && (d > 0.0f) != (n > 0.0f);   // n is the one further from 0
+                    k[j] = __float_as_uint(round_at_border(p[j], c.m, fabsf(n) - (outer ? 1.0f : 0.0f), ((k[j] & 1u) != 0u) != outer) + MAGIC);
+                }
+            }
+        } else {
+#pragma unroll 1
+            for (int j = 0; j < 8; ++j) {
+                float v = p[0];
+#pragma unroll
+                for (int i = 1; i < 8; ++i) v = i == j ? p[i] : v;
+                const uint32_t code = __float_as_uint(code_scaled(v, c.m) + MAGIC);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) k[i] = i == j ? code : k[i];
+            }
+        }
+    }
+    const uint32_t a = __byte_perm(k[0], k[1], 0x0040), b = __byte_perm(k[2], k[3], 0x0040);
+    const uint32_t d = __byte_perm(k[4], k[5], 0x0040), e = __byte_perm(k[6], k[7], 0x0040);
+    return make_uint2(__byte_perm(a, b, 0x5410), __byte_perm(d, e, 0x5410));
+}
+
+// the larger magnitude; a NaN on either side stays
+__device__ __forceinline__ float max_abs_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(fabsf(b)));
+    return r;
 }
 
 __device__ __forceinline__ float warp_sum_xor(float v) {
@@ -71,10 +123,16 @@ __device__ __forceinline__ float warp_sum_xor(float v) {
     return v;
 }
 
+// threads of a block: what its registers leave room for
+template <int V, int MODE>
+constexpr int most_threads() {
+    return V <= 2 || (V == 4 && MODE == NO_NORM) ? 1024 : 512;
+}
+
 // One row per group of threads: a warp (WIDE = false, several rows per block) or the whole block.  A thread holds V
 // vectors of 8 elements, `step` threads apart.
 template <int V, int MODE, bool WIDE>
-__global__ void __launch_bounds__(WIDE ? 512 : 256) rows_i8_kernel(const RowArgs a, const size_t rows) {
+__global__ void __launch_bounds__(WIDE ? most_threads<V, MODE>() : 256) rows_i8_kernel(const RowArgs a, const size_t rows) {
     __shared__ float sh_sum[32];
     __shared__ uint32_t sh_max[32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -102,8 +160,11 @@ __global__ void __launch_bounds__(WIDE ? 512 : 256) rows_i8_kernel(const RowArgs
         if (MODE != NO_NORM) wt[v] = in ? *reinterpret_cast<const uint4 *>(a.weight + (size_t)i * 8) : make_uint4(0, 0, 0, 0);
     }
 
+    constexpr bool KEEP = MODE != NO_NORM && V <= 2;   // the products stay in registers
+    float kept[KEEP ? V : 1][8];
     float sum = 0.0f;
-    uint32_t big = 0;   // bits of |p|: magnitudes order like integers, infinities and NaN on top
+    float top = 0.0f;       // largest |p|
+    uint32_t top16 = 0;     // NO_NORM: the same of the bits of two bf16 at a time (they order like the values)
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         uint32_t *x = reinterpret_cast<uint32_t *>(&xs[v]);
@@ -112,20 +173,32 @@ __global__ void __launch_bounds__(WIDE ? 512 : 256) rows_i8_kernel(const RowArgs
         const float *d32 = reinterpret_cast<const float *>(&df[MODE == DELTA_F32 ? 2 * v : 0]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            if (MODE == DELTA_BF16) x[j] = pack_bf16(bf_lo(x[j]) + bf_lo(d16[j]), bf_hi(x[j]) + bf_hi(d16[j]));
+            if (MODE == DELTA_BF16) {   // (a sum of two bf16 rounds to bf16 the same directly and by way of fp32)
+                const __nv_bfloat162 s = __hadd2(*reinterpret_cast<const __nv_bfloat162 *>(&x[j]),
+                                                 *reinterpret_cast<const __nv_bfloat162 *>(&d16[j]));
+                x[j] = *reinterpret_cast<const uint32_t *>(&s);
+            }
             if (MODE == DELTA_F32) x[j] = pack_bf16(bf_lo(x[j]) + d32[2 * j], bf_hi(x[j]) + d32[2 * j + 1]);
             const float lo = bf_lo(x[j]), hi = bf_hi(x[j]);
             if (MODE == NO_NORM) {
-                big = max(big, max(__float_as_uint(lo) & 0x7fffffffu, __float_as_uint(hi) & 0x7fffffffu));
+                top16 = __vmaxu2(top16, x[j] & 0x7fff7fffu);
             } else {
                 sum = fmaf(lo, lo, sum);
                 sum = fmaf(hi, hi, sum);
-                big = max(big, max(__float_as_uint(lo * bf_lo(w[j])) & 0x7fffffffu, __float_as_uint(hi * bf_hi(w[j])) & 0x7fffffffu));
+                const float p0 = lo * bf_lo(w[j]), p1 = hi * bf_hi(w[j]);
+                top = max_abs_nan(top, p0);
+                top = max_abs_nan(top, p1);
+                if (KEEP) {
+                    kept[KEEP ? v : 0][2 * j] = p0;
+                    kept[KEEP ? v : 0][2 * j + 1] = p1;
+                }
             }
         }
         const int i = i0 + v * step;
         if ((MODE == DELTA_BF16 || MODE == DELTA_F32) && i < nv) *reinterpret_cast<uint4 *>(a.x + base + (size_t)i * 8) = xs[v];
     }
+    // as bits: magnitudes order like integers, infinities and NaN on top
+    uint32_t big = MODE == NO_NORM ? max(top16 << 16, top16 & 0xffff0000u) : __float_as_uint(top) & 0x7fffffffu;
     big = __reduce_max_sync(0xffffffffu, big);
     if (MODE != NO_NORM) sum = warp_sum_xor(sum);
     if (WIDE) {
@@ -140,8 +213,9 @@ __global__ void __launch_bounds__(WIDE ? 512 : 256) rows_i8_kernel(const RowArgs
     const bool finite = big < 0x7f800000u;
     float r = 1.0f;
     if (MODE != NO_NORM) {
-        const float mean = sum / (float)a.d + a.eps;
-        r = 1.0f / sqrtf(mean);
+        const float mean = sum * a.inv_d + a.eps;
+        r = rsqrtf(mean);
+        r = r * (1.5f - 0.5f * mean * r * r);   // (one Newton step: within an ulp)
         if (finite && !(mean >= 0x1p-60f && mean < INFINITY)) {   // (the same for the whole row)
             // squares at the ends of fp32's range: once more, of scaled values
             const float S = mean < 1.0f ? 0x1p64f : 0x1p-100f;
@@ -163,7 +237,7 @@ __global__ void __launch_bounds__(WIDE ? 512 : 256) rows_i8_kernel(const RowArgs
                 __syncthreads();
                 s2 = warp_sum_xor(lane < nw ? sh_sum[lane] : 0.0f);
             }
-            r = S / sqrtf(s2 / (float)a.d + a.eps * S * S);
+            r = S / sqrtf(s2 * a.inv_d + a.eps * S * S);
         }
     }
     const float m = __uint_as_float(big);
@@ -179,20 +253,16 @@ __global__ void __launch_bounds__(WIDE ? 512 : 256) rows_i8_kernel(const RowArgs
         if (i >= nv) break;
         const uint32_t *x = reinterpret_cast<const uint32_t *>(&xs[v]);
         const uint32_t *w = reinterpret_cast<const uint32_t *>(&wt[MODE != NO_NORM ? v : 0]);
-        uint32_t hv[4], qv[2] = {0u, 0u};
+        float p[8];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            float lo = bf_lo(x[j]), hi = bf_hi(x[j]);
-            if (MODE != NO_NORM) {
-                lo *= bf_lo(w[j]);
-                hi *= bf_hi(w[j]);
-                hv[j] = pack_bf16(lo * r, hi * r);
-            }
-            if (a.q && codes)
-                qv[j >> 1] |= ((uint32_t)(code_of(lo, cs) & 0xff) | (uint32_t)(code_of(hi, cs) & 0xff) << 8) << (16 * (j & 1));
+            p[2 * j] = KEEP ? kept[KEEP ? v : 0][2 * j] : MODE == NO_NORM ? bf_lo(x[j]) : bf_lo(x[j]) * bf_lo(w[j]);
+            p[2 * j + 1] = KEEP ? kept[KEEP ? v : 0][2 * j + 1] : MODE == NO_NORM ? bf_hi(x[j]) : bf_hi(x[j]) * bf_hi(w[j]);
         }
-        if (MODE != NO_NORM && a.h) *reinterpret_cast<uint4 *>(a.h + base + (size_t)i * 8) = make_uint4(hv[0], hv[1], hv[2], hv[3]);
-        if (a.q) *reinterpret_cast<uint2 *>(a.q + base + (size_t)i * 8) = make_uint2(qv[0], qv[1]);
+        if (MODE != NO_NORM && a.h)
+            *reinterpret_cast<uint4 *>(a.h + base + (size_t)i * 8) = make_uint4(pack_bf16(p[0] * r, p[1] * r), pack_bf16(p[2] * r, p[3] * r),
+                                                                              pack_bf16(p[4] * r, p[5] * r), pack_bf16(p[6] * r, p[7] * r));
+        if (a.q) *reinterpret_cast<uint2 *>(a.q + base + (size_t)i * 8) = codes ? codes_of(p, cs) : make_uint2(0u, 0u);
     }
 }
 
@@ -212,11 +282,16 @@ spice_status launch_rows(const RowArgs &a, size_t rows, cudaStream_t st) {
         rows_i8_kernel<V, MODE, false><<<(unsigned)((rows + wpb - 1) / wpb), wpb * 32, 0, st>>>(a, rows);
     };
     using std::integral_constant;
+    // Few rows: a vector per thread, the shortest chain.  Many: more per thread, so that what a thread does beside its data
+    // (reductions, the row's scale) is spread over more of it, as long as enough warps stay resident.
+    // 16 rows of 2048: norm 2.1 / 2.2 / 2.5 us with 1 / 2 / 4; 4096 rows of 2048: norm 14.5 / 13.8 / 15.1 us; 40960 rows of
+    // 3584: quantiser 160 / 110 / 87 / 111 us with 1 / 2 / 4 / 8.
+    const int want = rows < 1024 ? 1 : MODE == NO_NORM ? 4 : 2;
     if (nv <= 32) narrow(integral_constant<int, 1>{});
     else if (nv <= 64) narrow(integral_constant<int, 2>{});
-    else if (nv <= 512) wide(integral_constant<int, 1>{});
-    else if (nv <= 1024) wide(integral_constant<int, 2>{});
-    else if (nv <= 2048) wide(integral_constant<int, 4>{});
+    else if (want <= 1 && nv <= 1024) wide(integral_constant<int, 1>{});
+    else if (want <= 2 && nv <= 2048) wide(integral_constant<int, 2>{});
+    else if (nv <= 4 * most_threads<4, MODE>()) wide(integral_constant<int, 4>{});
     else wide(integral_constant<int, 8>{});
     return cudaGetLastError() == cudaSuccess ? SPICE_OK : SPICE_ERR_CUDA;
 }
@@ -239,7 +314,7 @@ extern "C" spice_status spice_residual_rmsnorm(spice_bf16 *x_resid, const spice_
         !aligned16(h) || (reinterpret_cast<uintptr_t>(q) & 7u) || (reinterpret_cast<uintptr_t>(scale) & 3u))
         return SPICE_ERR_INVALID_ARG;
     const RowArgs a{reinterpret_cast<__nv_bfloat16 *>(x_resid), reinterpret_cast<const __nv_bfloat16 *>(delta), delta_f32,
-                    reinterpret_cast<const __nv_bfloat16 *>(weight), reinterpret_cast<__nv_bfloat16 *>(h), q, scale, d, eps};
+                    reinterpret_cast<const __nv_bfloat16 *>(weight), reinterpret_cast<__nv_bfloat16 *>(h), q, scale, d, eps, 1.0f / (float)d};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (delta) return launch_rows<DELTA_BF16>(a, (size_t)T, st);
     if (delta_f32) return launch_rows<DELTA_F32>(a, (size_t)T, st);
@@ -256,6 +331,6 @@ extern "C" spice_status spice_quantize_i8_rows(const spice_bf16 *w, int64_t rows
         return SPICE_ERR_INVALID_ARG;
     // (the kernel only reads x in this mode)
     const RowArgs a{const_cast<__nv_bfloat16 *>(reinterpret_cast<const __nv_bfloat16 *>(w)), nullptr, nullptr, nullptr, nullptr,
-                    q, scale, cols, 0.0f};
+                    q, scale, cols, 0.0f, 0.0f};
     return launch_rows<NO_NORM>(a, (size_t)rows, static_cast<cudaStream_t>(stream));
 }

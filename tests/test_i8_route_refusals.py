@@ -83,9 +83,8 @@ def test_binding_refuses_host_tensors_and_wrong_shapes():
         B.spice_swiglu_i8(z(2, 16, dtype=i8), z(2, dtype=f32), z(16, 16, dtype=i8), z(16, dtype=f32), z(2, 8, dtype=bf))
     with pytest.raises(B.SpiceError):
         B.spice_route_scored(z(2, 8, dtype=f32), z(2, 2, dtype=torch.int32), z(2, 2, dtype=f32))
-    dev = torch.device("cuda", 0)
     for t, dtype, shape in ((z(2, 8, dtype=bf), bf, (2, 8)), (z(2, 8, dtype=bf), f32, (2, 8)), (z(2, 8, dtype=bf), bf, (2, 4)),
                             (z(8, 2, dtype=bf).t(), bf, (2, 8))):
         with pytest.raises(B.SpiceError, match="f: expected a contiguous"):
-            B._addr("f", t, dtype, shape, dev)
-    assert B._addr("f", None, bf, (2, 8), dev) is None
+            B._addr("f", t, dtype, shape, 0)
+    assert B._addr("f", None, bf, (2, 8), 0) is None
