@@ -6,7 +6,8 @@
 // The sum is an integer and exact (k <= 131056: 2^14 k < 2^31), so neither the order of the additions nor a split of the
 // reduction changes a bit; one rounding when it becomes fp32, one per scale, one to bf16.
 //
-// Two kernels.  Few tokens: every weight byte is used for few products and the call is bound by streaming the weights, so
+// Three kernels.  A handful of tokens: straight from global memory into registers, the shortest chain of latencies.  Few
+// tokens: every weight byte is used for few products and the call is bound by streaming the weights, so
 // the weight rows are the M operand, the tokens the N operand (as in the fused decode kernel), and the reduction is split
 // over the CTAs of a cluster so that narrow layers still fill the GPU; the cluster adds its partial sums through
 // distributed shared memory, no workspace and no atomics.  Many tokens: pairs of CTAs work on 256 x 256 tiles
@@ -60,92 +61,86 @@ __device__ __forceinline__ void store4(const GemmI8Args &g, size_t at, float4 v)
     *dst = v;
 }
 
-// ------------------------------------------------------------------------------------------------ single tokens
-// Up to 8 tokens: a warp takes a weight row (from two tokens on a pair of rows, which halves the reads of the tokens; with
-// SwiGLU always a gate row and its up row), reads 16 bytes per lane and multiplies with four-wide integer dot products; the
-// tokens come from L1.  No barriers and no tensor memory: at these sizes the chain of latencies of the tensor-core kernel is
-// longer than the whole call.
-constexpr int DOT_THREADS = 256, DOT_MAX_TOKENS = 8;
-
-// WPR warps share the rows: layers with few of them
-template <int TT, bool SWIGLU, int WPR>
-__global__ void __launch_bounds__(DOT_THREADS) gemm_i8_dot_kernel(const int8_t *__restrict__ x, const int8_t *__restrict__ w,
-                                                                  const GemmI8Args g) {
-    constexpr int R = SWIGLU || TT > 1 ? 2 : 1, UN = TT >= 8 ? 2 : 4;
-    constexpr int COLS = SWIGLU ? 1 : R;                       // output columns of a warp
-    __shared__ int32_t part[DOT_THREADS / 32][R * TT];
+// ------------------------------------------------------------------------------------------------ a handful of tokens
+// A block multiplies 16 weight rows (SwiGLU: 8 gate rows and their up rows) with all tokens; its warps share the reduction
+// in pieces of 64.  The weights go from global memory straight into the registers of warp-wide 16 x 8 x 32 products: a lane
+// reads 16 consecutive bytes of its row, and since both operands are read alike, the order of the reduction inside a piece
+// does not matter.  The call is over before the tensor-memory kernel has its first tile (descriptors, barriers, TMEM and the
+// cluster's sums are a chain of some 6 us).  What limits it is the reads of the tokens, which every block repeats.
+constexpr int FEW_MAX_TOKENS = 32;
+template <int NT, int NW, int UN, bool DEAL, bool SWIGLU>
+__global__ void __launch_bounds__(NW * 32) gemm_i8_few_kernel(const int8_t *__restrict__ x, const int8_t *__restrict__ w,
+                                                              const GemmI8Args g) {
+    __shared__ int32_t red[NW][NT * 8][16 + 4];   // (padded: the 8 rows of a warp's store fall into different banks)
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int row = (blockIdx.x * (DOT_THREADS / 32 / WPR) + warp / WPR) * COLS;
-    const bool in = row < g.n;                                 // (n is a multiple of 8: both columns or none)
-    const int nv = g.k >> 4;
-    const int4 *w0 = reinterpret_cast<const int4 *>(w + (size_t)(in ? row : 0) * g.k);
-    const int4 *w1 = reinterpret_cast<const int4 *>(w + (size_t)((in ? row : 0) + (SWIGLU ? g.n : 1)) * g.k);
+    const int gq = lane >> 2, c = lane & 3;
+    const int n0 = blockIdx.x * (SWIGLU ? 8 : 16);
+    const int r0 = n0 + gq, r1 = SWIGLU ? g.n + n0 + gq : n0 + gq + 8;
+    const bool in1 = SWIGLU || n0 + 8 < g.n;                             // (n is a multiple of 8)
+    const int4 *w0 = reinterpret_cast<const int4 *>(w + (size_t)r0 * g.k);
+    const int4 *w1 = reinterpret_cast<const int4 *>(w + (size_t)(in1 ? r1 : r0) * g.k);
     const int4 *x4 = reinterpret_cast<const int4 *>(x);
-    int32_t acc[R][TT];
+    const int nv = g.k >> 4, pieces = (nv + 3) >> 2;
+    // DEAL: pieces are dealt out one at a time, so that every warp has the same share of a short reduction; of a long one a
+    // warp takes UN pieces side by side, whole lines of DRAM (8 tokens, 2048 x 2816: 3.4 against 4.0 us; 3584 x 20480: 19.1
+    // against 15.9).
+    int32_t acc[NT][4];
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+    for (int i = 0; i < NT; ++i)
 #pragma unroll
-        for (int t = 0; t < TT; ++t) acc[r][t] = 0;
+        for (int j = 0; j < 4; ++j) acc[i][j] = 0;
     const int4 zero = make_int4(0, 0, 0, 0);
-    for (int v0 = (warp % WPR) * 32 + lane; v0 < nv; v0 += 32 * WPR * UN) {
-        int4 a[UN][R];
+    for (int p0 = DEAL ? warp : warp * UN; p0 < pieces; p0 += NW * UN) {
+        int4 a0[UN], a1[UN], b[UN][NT];
 #pragma unroll
         for (int u = 0; u < UN; ++u) {
-            const int v = v0 + u * 32 * WPR;
-            a[u][0] = v < nv ? __ldcs(w0 + v) : zero;
-            if (R > 1) a[u][R - 1] = v < nv ? __ldcs(w1 + v) : zero;
+            const int v = (p0 + u * (DEAL ? NW : 1)) * 4 + c;
+            a0[u] = v < nv ? __ldcs(w0 + v) : zero;
+            a1[u] = v < nv ? __ldcs(w1 + v) : zero;
         }
 #pragma unroll
         for (int u = 0; u < UN; ++u) {
-            const int v = v0 + u * 32 * WPR;
+            const int v = (p0 + u * (DEAL ? NW : 1)) * 4 + c;
 #pragma unroll
-            for (int t = 0; t < TT; ++t) {
-                const int4 b = v < nv && t < g.T ? __ldg(x4 + (size_t)t * nv + v) : zero;
+            for (int i = 0; i < NT; ++i) b[u][i] = v < nv && i * 8 + gq < g.T ? __ldg(x4 + (size_t)(i * 8 + gq) * nv + v) : zero;
+        }
 #pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    acc[r][t] = __dp4a(a[u][r].x, b.x, acc[r][t]);
-                    acc[r][t] = __dp4a(a[u][r].y, b.y, acc[r][t]);
-                    acc[r][t] = __dp4a(a[u][r].z, b.z, acc[r][t]);
-                    acc[r][t] = __dp4a(a[u][r].w, b.w, acc[r][t]);
-                }
+        for (int u = 0; u < UN; ++u)
+#pragma unroll
+            for (int i = 0; i < NT; ++i) {
+                asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                             : "+r"(acc[i][0]), "+r"(acc[i][1]), "+r"(acc[i][2]), "+r"(acc[i][3])
+                             : "r"(a0[u].x), "r"(a1[u].x), "r"(a0[u].y), "r"(a1[u].y), "r"(b[u][i].x), "r"(b[u][i].y));
+                asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                             : "+r"(acc[i][0]), "+r"(acc[i][1]), "+r"(acc[i][2]), "+r"(acc[i][3])
+                             : "r"(a0[u].z), "r"(a1[u].z), "r"(a0[u].w), "r"(a1[u].w), "r"(b[u][i].z), "r"(b[u][i].w));
             }
-        }
     }
-    int32_t mine[R] = {};   // lane t: token t
 #pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int t = 0; t < TT; ++t) {
-            const int32_t s = __reduce_add_sync(0xffffffffu, acc[r][t]);
-            if (lane == t) mine[r] = s;
-        }
-    if (WPR > 1) {
-        if (lane < TT)
-#pragma unroll
-            for (int r = 0; r < R; ++r) part[warp][r * TT + lane] = mine[r];
-        __syncthreads();
-        if (warp % WPR) return;
-        if (lane < TT)
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-                for (int i = 1; i < WPR; ++i) mine[r] += part[warp + i][r * TT + lane];
+    for (int i = 0; i < NT; ++i) {   // rows gq, gq + 8 x tokens 2c, 2c + 1
+        red[warp][i * 8 + 2 * c][gq] = acc[i][0];
+        red[warp][i * 8 + 2 * c + 1][gq] = acc[i][1];
+        red[warp][i * 8 + 2 * c][gq + 8] = acc[i][2];
+        red[warp][i * 8 + 2 * c + 1][gq + 8] = acc[i][3];
     }
-    if (!in || lane >= g.T) return;
-    const float xs = g.xs[lane];
-    float v[COLS];
-    v[0] = (float)mine[0] * xs * g.ws[row];
-    if (SWIGLU) v[0] = silu_times(v[0], (float)mine[R - 1] * xs * g.ws[row + g.n]);
-    else if (COLS > 1) v[COLS - 1] = (float)mine[R - 1] * xs * g.ws[row + 1];
-    const size_t at = (size_t)lane * g.n + row;
-    if (g.out == SPICE_OUT_BF16) {
-        __nv_bfloat16 *y = static_cast<__nv_bfloat16 *>(g.y) + at;
-        if (COLS > 1) *reinterpret_cast<uint32_t *>(y) = pack2(v[0], v[COLS - 1]);
-        else *y = __float2bfloat16_rn(v[0]);
-    } else {
-        float *y = static_cast<float *>(g.y) + at;
+    __syncthreads();
+    constexpr int ROWS = SWIGLU ? 8 : 16;
+    for (int i = threadIdx.x; i < g.T * ROWS; i += NW * 32) {
+        const int t = i / ROWS, r = i % ROWS;
+        if (n0 + r >= g.n) continue;
+        int32_t s = 0, u = 0;
 #pragma unroll
-        for (int i = 0; i < COLS; ++i) y[i] = g.out == SPICE_OUT_F32 ? v[i] : y[i] + v[i];
+        for (int q = 0; q < NW; ++q) {
+            s += red[q][t][r];
+            if (SWIGLU) u += red[q][t][r + 8];
+        }
+        const float xs = g.xs[t];
+        float v = (float)s * xs * g.ws[n0 + r];
+        if (SWIGLU) v = silu_times(v, (float)u * xs * g.ws[g.n + n0 + r]);
+        const size_t at = (size_t)t * g.n + n0 + r;
+        if (g.out == SPICE_OUT_BF16) static_cast<__nv_bfloat16 *>(g.y)[at] = __float2bfloat16_rn(v);
+        else if (g.out == SPICE_OUT_F32) static_cast<float *>(g.y)[at] = v;
+        else static_cast<float *>(g.y)[at] += v;
     }
 }
 
@@ -540,14 +535,10 @@ bool prepare_device(int dev) {
     return ok;
 }
 
-template <int TT, bool SWIGLU>
-void launch_dot(const GemmI8Args &g, const int8_t *x, const int8_t *w, int sms, cudaStream_t st) {
-    constexpr int COLS = SWIGLU || TT == 1 ? 1 : 2;
-    const int warps = g.n / COLS;
-    if (warps < 32 * sms && g.k >= 2048)   // too few warps to keep enough bytes in flight
-        gemm_i8_dot_kernel<TT, SWIGLU, 4><<<(warps + 1) / 2, DOT_THREADS, 0, st>>>(x, w, g);
-    else
-        gemm_i8_dot_kernel<TT, SWIGLU, 1><<<(warps + 7) / 8, DOT_THREADS, 0, st>>>(x, w, g);
+template <int NT, int NW, int UN, bool SWIGLU>
+void launch_few(const GemmI8Args &g, const int8_t *x, const int8_t *w, int blocks, cudaStream_t st) {
+    if (NT >= 4 || (g.k + 63) / 64 <= NW * UN) gemm_i8_few_kernel<NT, NW, UN, true, SWIGLU><<<blocks, NW * 32, 0, st>>>(x, w, g);
+    else gemm_i8_few_kernel<NT, NW, UN, (NT >= 4), SWIGLU><<<blocks, NW * 32, 0, st>>>(x, w, g);
 }
 
 template <bool SWIGLU>
@@ -558,15 +549,16 @@ spice_status launch_gemm_i8(GemmI8Args g, const int8_t *x, const int8_t *w, cuda
     const int w_rows = SWIGLU ? 2 * g.n : g.n;
     const int kblocks = (g.k + BK - 1) / BK;
     const int64_t weights = (int64_t)w_rows * g.k;
-    // The dot products' reads of the tokens grow with their number, the tensor cores' do not matter up to 64 of them.
-    // 2048 x 2816, 5632 x 2048, 11264 x 2048, 3584 x 20480, 40960 x 3584 weights, us with dot products / tensor cores:
-    // 1 token 3.5/7.0, 4.7/8.5, 6.1/9.9, 15/17, 29/27;  4 tokens 4.2/7.5, 4.9/8.4, 8.2/10, 27/18, 31/28;
-    // 8 tokens 4.8/7.7, 7.2/8.6, 11/10, 50/18, 40/28
-    if (g.T == 1 || (g.T <= 4 && weights <= (48 << 20)) || (g.T <= DOT_MAX_TOKENS && weights <= (16 << 20))) {
-        if (g.T == 1) launch_dot<1, SWIGLU>(g, x, w, sms, st);
-        else if (g.T == 2) launch_dot<2, SWIGLU>(g, x, w, sms, st);
-        else if (g.T <= 4) launch_dot<4, SWIGLU>(g, x, w, sms, st);
-        else launch_dot<8, SWIGLU>(g, x, w, sms, st);
+    // Up to a few MB of weights the short start wins, beyond that the reads of the tokens cost more than it saves.
+    // 2048 x 2816, 5632 x 2048, 11264 x 2048, 3584 x 20480, 40960 x 3584 weights, us with this kernel / the tensor-memory one:
+    // 8 tokens 3.4/7.4, 4.7/8.5, 6.5/10, 16/18, 26/27;  16 tokens 4.5/7.6, 4.9/8.7, 8.0/10, 20/18, 35/27;
+    // 32 tokens 6.7/8.2, 6.3/9.3, 10.5/11, 33/19, 46/28
+    if (g.T <= 8 || (g.T <= 16 && weights <= (48 << 20)) || (g.T <= FEW_MAX_TOKENS && weights <= (24 << 20))) {
+        const int blocks = (g.n + (SWIGLU ? 7 : 15)) / (SWIGLU ? 8 : 16);
+        const bool wide = blocks < 2 * sms;   // few blocks: sixteen warps in each, enough bytes in flight
+        if (g.T <= 8) wide ? launch_few<1, 16, 4, SWIGLU>(g, x, w, blocks, st) : launch_few<1, 8, 4, SWIGLU>(g, x, w, blocks, st);
+        else if (g.T <= 16) wide ? launch_few<2, 16, 4, SWIGLU>(g, x, w, blocks, st) : launch_few<2, 8, 4, SWIGLU>(g, x, w, blocks, st);
+        else launch_few<4, 8, 2, SWIGLU>(g, x, w, blocks, st);
         return cudaGetLastError() == cudaSuccess ? SPICE_OK : SPICE_ERR_CUDA;
     }
     CUtensorMap map_x, map_w;
