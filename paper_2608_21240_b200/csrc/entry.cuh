@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include <atomic>
+#include <utility>
 
 namespace spice {
 
@@ -33,6 +34,32 @@ inline int current_device_sms(int *device_out = nullptr) {
         sms[dev].store(n, std::memory_order_relaxed);
     }
     return n;
+}
+
+// Launches a kernel that may be set up while the kernel before it in the stream still drains: such a kernel calls
+// grid_dependency() before its first access to global memory, which returns when everything before it is complete and
+// visible, and lets its own successor be set up as soon as all its blocks run.  Stream order, as the caller sees it, is
+// that of any launch; back to back, a call starts about a microsecond sooner.
+template <typename... P, typename... A>
+inline bool launch_early(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, int cluster, A &&...args) {
+    cudaLaunchConfig_t lc{};
+    lc.gridDim = grid;
+    lc.blockDim = dim3((unsigned)threads, 1, 1);
+    lc.dynamicSmemBytes = smem;
+    lc.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = (unsigned)cluster;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    lc.attrs = at;
+    lc.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&lc, kernel, std::forward<A>(args)...) == cudaSuccess;
+}
+__device__ __forceinline__ void grid_dependency() {
+    asm volatile("griddepcontrol.launch_dependents;");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 }  // namespace spice

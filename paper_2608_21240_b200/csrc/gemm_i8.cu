@@ -89,6 +89,7 @@ __global__ void __launch_bounds__(NW * 32) gemm_i8_few_kernel(const int8_t *__re
     for (int i = 0; i < NT; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[i][j] = 0;
+    grid_dependency();
     const int4 zero = make_int4(0, 0, 0, 0);
     for (int p0 = DEAL ? warp : warp * UN; p0 < pieces; p0 += NW * UN) {
         int4 a0[UN], a1[UN], b[UN][NT];
@@ -198,6 +199,7 @@ __global__ void __launch_bounds__(SK_THREADS) gemm_i8_skinny_kernel(const __grid
         sh.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_proxy_async();
+        grid_dependency();
         // the first copies leave before the block is set up: a short call is a chain of latencies
         for (int it = 0; it < min(stages, n_it); ++it) load_stage(it);
     }
@@ -209,6 +211,7 @@ __global__ void __launch_bounds__(SK_THREADS) gemm_i8_skinny_kernel(const __grid
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = sh.tmem_base;
+    grid_dependency();
 
     if (warp == 0 && lane == 0) {
         int it = min(stages, n_it);
@@ -332,7 +335,7 @@ __device__ __forceinline__ void pair_tile(const GemmI8Args &g, int tile, int &mt
 }
 
 template <bool SWIGLU>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PR_THREADS, 1)
+__global__ void __launch_bounds__(PR_THREADS, 1)
     gemm_i8_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const GemmI8Args g) {
     extern __shared__ __align__(16) unsigned char smem_raw[];   // (aligned to 1024 by hand: the swizzled tiles)
     unsigned char *ring = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -364,6 +367,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PR_THREADS, 1)
     cluster_sync();   // both CTAs' barriers exist before either signals the other's
     tc_fence_after();
     const uint32_t tmem_base = sh.tmem_base;
+    grid_dependency();
 
     const int n_tiles = g.m_tiles * g.n_tiles;
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
@@ -536,9 +540,10 @@ bool prepare_device(int dev) {
 }
 
 template <int NT, int NW, int UN, bool SWIGLU>
-void launch_few(const GemmI8Args &g, const int8_t *x, const int8_t *w, int blocks, cudaStream_t st) {
-    if (NT >= 4 || (g.k + 63) / 64 <= NW * UN) gemm_i8_few_kernel<NT, NW, UN, true, SWIGLU><<<blocks, NW * 32, 0, st>>>(x, w, g);
-    else gemm_i8_few_kernel<NT, NW, UN, (NT >= 4), SWIGLU><<<blocks, NW * 32, 0, st>>>(x, w, g);
+bool launch_few(const GemmI8Args &g, const int8_t *x, const int8_t *w, int blocks, cudaStream_t st) {
+    auto *kernel = NT >= 4 || (g.k + 63) / 64 <= NW * UN ? gemm_i8_few_kernel<NT, NW, UN, true, SWIGLU>
+                                                          : gemm_i8_few_kernel<NT, NW, UN, (NT >= 4), SWIGLU>;
+    return launch_early(kernel, dim3((unsigned)blocks), NW * 32, 0, st, 1, x, w, g);
 }
 
 template <bool SWIGLU>
@@ -556,10 +561,10 @@ spice_status launch_gemm_i8(GemmI8Args g, const int8_t *x, const int8_t *w, cuda
     if (g.T <= 8 || (g.T <= 16 && weights <= (48 << 20)) || (g.T <= FEW_MAX_TOKENS && weights <= (24 << 20))) {
         const int blocks = (g.n + (SWIGLU ? 7 : 15)) / (SWIGLU ? 8 : 16);
         const bool wide = blocks < 2 * sms;   // few blocks: sixteen warps in each, enough bytes in flight
-        if (g.T <= 8) wide ? launch_few<1, 16, 4, SWIGLU>(g, x, w, blocks, st) : launch_few<1, 8, 4, SWIGLU>(g, x, w, blocks, st);
-        else if (g.T <= 16) wide ? launch_few<2, 16, 4, SWIGLU>(g, x, w, blocks, st) : launch_few<2, 8, 4, SWIGLU>(g, x, w, blocks, st);
-        else launch_few<4, 8, 2, SWIGLU>(g, x, w, blocks, st);
-        return cudaGetLastError() == cudaSuccess ? SPICE_OK : SPICE_ERR_CUDA;
+        const bool ok = g.T <= 8 ? (wide ? launch_few<1, 16, 4, SWIGLU>(g, x, w, blocks, st) : launch_few<1, 8, 4, SWIGLU>(g, x, w, blocks, st))
+                        : g.T <= 16 ? (wide ? launch_few<2, 16, 4, SWIGLU>(g, x, w, blocks, st) : launch_few<2, 8, 4, SWIGLU>(g, x, w, blocks, st))
+                        : launch_few<4, 8, 2, SWIGLU>(g, x, w, blocks, st);
+        return ok ? SPICE_OK : SPICE_ERR_CUDA;
     }
     CUtensorMap map_x, map_w;
     g.m_tiles = (g.T + PR_TILE - 1) / PR_TILE;
@@ -596,25 +601,14 @@ spice_status launch_gemm_i8(GemmI8Args g, const int8_t *x, const int8_t *w, cuda
         if (!tc_encode_map2_bytes(&map_w, w, (uint64_t)w_rows, (uint64_t)g.k, tile_n) ||
             !tc_encode_map2_bytes(&map_x, x, (uint64_t)g.T, (uint64_t)g.k, (uint32_t)g.cols))
             return SPICE_ERR_CUDA;
-        cudaLaunchConfig_t lc{};
-        lc.gridDim = dim3((unsigned)(row_tiles * g.split), (unsigned)token_tiles, 1);
-        lc.blockDim = dim3(SK_THREADS, 1, 1);
-        lc.dynamicSmemBytes = smem;
-        lc.stream = st;
-        cudaLaunchAttribute at[1];
-        at[0].id = cudaLaunchAttributeClusterDimension;
-        at[0].val.clusterDim.x = (unsigned)g.split;
-        at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-        lc.attrs = at;
-        lc.numAttrs = g.split > 1 ? 1 : 0;
-        return cudaLaunchKernelEx(&lc, gemm_i8_skinny_kernel<SWIGLU>, map_w, map_x, g) == cudaSuccess ? SPICE_OK : SPICE_ERR_CUDA;
+        return launch_early(gemm_i8_skinny_kernel<SWIGLU>, dim3((unsigned)(row_tiles * g.split), (unsigned)token_tiles, 1), SK_THREADS, smem,
+                            st, g.split, map_w, map_x, g) ? SPICE_OK : SPICE_ERR_CUDA;
     }
     if (!tc_encode_map2_bytes(&map_x, x, (uint64_t)g.T, (uint64_t)g.k, 128) ||
         !tc_encode_map2_bytes(&map_w, w, (uint64_t)w_rows, (uint64_t)g.k, 128))
         return SPICE_ERR_CUDA;
     const int pairs = max(1, min(sms / 2, g.m_tiles * g.n_tiles));
-    gemm_i8_pair_kernel<SWIGLU><<<2 * pairs, PR_THREADS, PR_SMEM, st>>>(map_x, map_w, g);
-    return cudaGetLastError() == cudaSuccess ? SPICE_OK : SPICE_ERR_CUDA;
+    return launch_early(gemm_i8_pair_kernel<SWIGLU>, dim3(2 * (unsigned)pairs), PR_THREADS, PR_SMEM, st, 2, map_x, map_w, g) ? SPICE_OK : SPICE_ERR_CUDA;
 }
 
 template <bool SWIGLU>

@@ -187,6 +187,7 @@ __global__ void __launch_bounds__(WARPS * 32) route_scored_kernel(const RouteArg
     extern __shared__ double sh_keys[];   // with groups or a bias: [WARPS][N] doubles, also the fp32 keys; then the open groups
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const long long t = (long long)blockIdx.x * WARPS + warp;
+    grid_dependency();
     if (t >= a.T) return;   // warp-uniform; no block-wide barrier below
     const float *l = a.logits + (size_t)t * a.N;
     double *shd = sh_keys + (size_t)warp * a.N;
@@ -378,10 +379,10 @@ __global__ void __launch_bounds__(WARPS * 32) route_scored_kernel(const RouteArg
 }
 
 template <int V>
-void launch_route_scored(const RouteArgs &a, int vs, unsigned grid, size_t smem, cudaStream_t st) {
-    if (V >= 8 && vs <= V / 4) route_scored_kernel<V, (V >= 8 ? V / 4 : V)><<<grid, WARPS * 32, smem, st>>>(a);
-    else if (V >= 4 && vs <= V / 2) route_scored_kernel<V, (V >= 4 ? V / 2 : V)><<<grid, WARPS * 32, smem, st>>>(a);
-    else route_scored_kernel<V, V><<<grid, WARPS * 32, smem, st>>>(a);
+bool launch_route_scored(const RouteArgs &a, int vs, unsigned grid, size_t smem, cudaStream_t st) {
+    auto *kernel = V >= 8 && vs <= V / 4 ? route_scored_kernel<V, (V >= 8 ? V / 4 : V)>
+                   : V >= 4 && vs <= V / 2 ? route_scored_kernel<V, (V >= 4 ? V / 2 : V)> : route_scored_kernel<V, V>;
+    return launch_early(kernel, dim3(grid), WARPS * 32, smem, st, 1, a);
 }
 
 }  // namespace
@@ -412,10 +413,8 @@ extern "C" spice_status spice_route_scored(const float *logits, const float *bia
     const unsigned grid = ((unsigned)T + WARPS - 1) / WARPS;
     const size_t smem = n_groups > 1 || bias ? (size_t)WARPS * (n_experts * sizeof(double) + 32 * sizeof(int32_t)) : 0;   // up to 33 KB
     const int v = (n_experts + 31) / 32, vs = (int)(top_groups * size + 31) / 32;
-    if (v <= 2) launch_route_scored<2>(a, vs, grid, smem, st);
-    else if (v <= 4) launch_route_scored<4>(a, vs, grid, smem, st);
-    else if (v <= 8) launch_route_scored<8>(a, vs, grid, smem, st);
-    else if (v <= 16) launch_route_scored<16>(a, vs, grid, smem, st);
-    else launch_route_scored<32>(a, vs, grid, smem, st);
-    return cudaGetLastError() == cudaSuccess ? SPICE_OK : SPICE_ERR_CUDA;
+    const bool ok = v <= 2 ? launch_route_scored<2>(a, vs, grid, smem, st) : v <= 4 ? launch_route_scored<4>(a, vs, grid, smem, st)
+                    : v <= 8 ? launch_route_scored<8>(a, vs, grid, smem, st) : v <= 16 ? launch_route_scored<16>(a, vs, grid, smem, st)
+                    : launch_route_scored<32>(a, vs, grid, smem, st);
+    return ok ? SPICE_OK : SPICE_ERR_CUDA;
 }

@@ -138,6 +138,7 @@ __global__ void __launch_bounds__(WIDE ? most_threads<V, MODE>() : 256) rows_i8_
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int nw = blockDim.x >> 5;
     const size_t row = WIDE ? blockIdx.x : (size_t)blockIdx.x * nw + warp;
+    grid_dependency();
     if (!WIDE && row >= rows) return;
     const int i0 = WIDE ? threadIdx.x : lane, step = WIDE ? blockDim.x : 32;
     const int nv = a.d >> 3;
@@ -271,15 +272,16 @@ constexpr int MAX_COLS = 32768;   // 512 threads x 8 vectors x 8 elements: what 
 template <int MODE>
 spice_status launch_rows(const RowArgs &a, size_t rows, cudaStream_t st) {
     const int nv = a.d >> 3;
+    bool ok = false;
     auto wide = [&](auto v) {
         constexpr int V = decltype(v)::value;
         const int threads = ((nv + V - 1) / V + 31) & ~31;
-        rows_i8_kernel<V, MODE, true><<<(unsigned)rows, threads, 0, st>>>(a, rows);
+        ok = launch_early(rows_i8_kernel<V, MODE, true>, dim3((unsigned)rows), threads, 0, st, 1, a, rows);
     };
     auto narrow = [&](auto v) {
         constexpr int V = decltype(v)::value;
         const int wpb = rows < 8 * 296 ? 4 : 8;
-        rows_i8_kernel<V, MODE, false><<<(unsigned)((rows + wpb - 1) / wpb), wpb * 32, 0, st>>>(a, rows);
+        ok = launch_early(rows_i8_kernel<V, MODE, false>, dim3((unsigned)((rows + wpb - 1) / wpb)), wpb * 32, 0, st, 1, a, rows);
     };
     using std::integral_constant;
     // Few rows: a vector per thread, the shortest chain.  Many: more per thread, so that what a thread does beside its data
@@ -293,7 +295,7 @@ spice_status launch_rows(const RowArgs &a, size_t rows, cudaStream_t st) {
     else if (want <= 2 && nv <= 2048) wide(integral_constant<int, 2>{});
     else if (nv <= 4 * most_threads<4, MODE>()) wide(integral_constant<int, 4>{});
     else wide(integral_constant<int, 8>{});
-    return cudaGetLastError() == cudaSuccess ? SPICE_OK : SPICE_ERR_CUDA;
+    return ok ? SPICE_OK : SPICE_ERR_CUDA;
 }
 
 }  // namespace
