@@ -40,18 +40,24 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 }
 
 // What turns the values of a row with largest magnitude m into codes
+template <bool CHECK>
 struct CodeScale {
-    float m, c;   // c = 127 / m within 2^-23; 0 where m is not well inside fp32's range
+    float m, c;   // c = 127 / m, within 2^-23 or (without CHECK) rounded up; 0 where m is not well inside fp32's range
     __device__ __forceinline__ explicit CodeScale(float largest) {
         m = largest;
-        float r = __fdividef(1.0f, m);
-        r = fmaf(r, fmaf(-m, r, 1.0f), r);
-        c = m > 0x1p-100f && m < 0x1p100f ? 127.0f * r : 0.0f;
+        c = 0.0f;
+        if (!(m > 0x1p-100f && m < 0x1p100f)) return;
+        if (CHECK) {
+            c = __fdividef(1.0f, m);
+            c = 127.0f * fmaf(c, fmaf(-m, c, 1.0f), c);
+        } else {
+            c = __fdiv_ru(127.0f, m);
+        }
     }
 };
 
 // nearest integer to 127 p / m, ties to even, exactly, for |127 p / m| between the integers a and a + 1: both products have
-// at most 24 significant bits.  (Weights meet this often: a value of half the row's largest is a tie at 63.5.)
+// at most 24 significant bits.
 __device__ __forceinline__ float round_at_border(float p, float m, float a, bool odd) {
     const float lhs = 254.0f * fabsf(p), rhs = (2.0f * a + 1.0f) * m;
     return copysignf(a + (lhs > rhs || (lhs == rhs && odd) ? 1.0f : 0.0f), p);
@@ -69,21 +75,46 @@ __device__ __noinline__ float code_scaled(float p, float m) {
     return fabsf(u - k) > 0.4999f ? round_at_border(pn, mn, a, (int)a & 1) : k;
 }
 
-// Codes of 8 values as packed bytes.  p c + 1.5 * 2^23 in one rounding is the nearest integer to p c, its low byte the code;
-// p c is off by at most 127 * 2^-23 < 1.6e-5 from the quotient.  Where one of the values lies within 2e-5 of a border they
-// are looked at once more.
-__device__ __forceinline__ uint2 codes_of(const float (&p)[8], const CodeScale &c) {
+// two fp32 operations in one instruction
+__device__ __forceinline__ uint64_t pair2(float lo, float hi) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
+// Codes of 8 values as packed bytes.  p c + 1.5 * 2^23 in one rounding is the nearest integer to p c, its low byte the code.
+// CHECK (products of two bf16): p c is off by at most 127 * 2^-23 < 1.6e-5 from the quotient; where one of the values lies
+// within 2e-5 of a border they are looked at once more.
+// Without (bf16 values): the answer is exact as it is.  With p = P 2^t, m = M and integers 128 <= P, M < 256, the quotient
+// 127 P 2^t / M is at least 2^t / (2 M) > 2^t * 0.0019 away from every border it does not lie on, and p c is off by
+// 2^t * 3.1e-5 at most.  It lies on a border only where 254 P 2^t = (2 k + 1) M: 127 then divides M, c is a power of two
+// and p c exact, or 127 divides 2 k + 1, the border is 63.5 (half of the row's largest, a frequent value), and c, rounded
+// up, takes it to 64, the even side.
+template <bool CHECK>
+__device__ __forceinline__ uint2 codes_of(const float (&p)[8], const CodeScale<CHECK> &c) {
     constexpr float MAGIC = 12582912.0f;
     uint32_t k[8];
     float off = c.c > 0.0f ? 0.0f : 1.0f;
+    const uint64_t c2 = pair2(c.c, c.c), magic2 = pair2(MAGIC, MAGIC), minus2 = pair2(-1.0f, -1.0f);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const float s = __fmaf_rn(p[j], c.c, MAGIC);
-        off = fmaxf(off, fabsf(__fmaf_rn(p[j], c.c, MAGIC - s)));
-        k[j] = __float_as_uint(s);
+    for (int j = 0; j < 8; j += 2) {
+        const uint64_t p2 = pair2(p[j], p[j + 1]);
+        const uint64_t s2 = fma2(p2, c2, magic2);
+        if (CHECK) {
+            const uint64_t d2 = fma2(p2, c2, fma2(s2, minus2, magic2));
+            off = fmaxf(off, fabsf(__uint_as_float((uint32_t)d2)));
+            off = fmaxf(off, fabsf(__uint_as_float((uint32_t)(d2 >> 32))));
+        }
+        k[j] = (uint32_t)s2;
+        k[j + 1] = (uint32_t)(s2 >> 32);
     }
     if (off > 0.49998f) {
-        if (c.c > 0.0f) {
+        if (CHECK && c.c > 0.0f) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float n = __uint_as_float(k[j]) - MAGIC;      // the nearest integer; the other side of the border is n +- 1
@@ -124,15 +155,15 @@ __device__ __forceinline__ float warp_sum_xor(float v) {
 }
 
 // threads of a block: what its registers leave room for
-template <int V, int MODE>
+template <int V>
 constexpr int most_threads() {
-    return V <= 2 || (V == 4 && MODE == NO_NORM) ? 1024 : 512;
+    return V <= 2 ? 1024 : 512;
 }
 
 // One row per group of threads: a warp (WIDE = false, several rows per block) or the whole block.  A thread holds V
 // vectors of 8 elements, `step` threads apart.
 template <int V, int MODE, bool WIDE>
-__global__ void __launch_bounds__(WIDE ? most_threads<V, MODE>() : 256) rows_i8_kernel(const RowArgs a, const size_t rows) {
+__global__ void __launch_bounds__(WIDE ? most_threads<V>() : 256) rows_i8_kernel(const RowArgs a, const size_t rows) {
     __shared__ float sh_sum[32];
     __shared__ uint32_t sh_max[32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -247,7 +278,7 @@ __global__ void __launch_bounds__(WIDE ? most_threads<V, MODE>() : 256) rows_i8_
         constexpr float C = 1.0f / 127.0f;
         a.scale[row] = !codes ? __uint_as_float(0x7fffffffu) : m == 0.0f ? 1.0f : m > 1.0f ? (m * C) * r : m * (r * C);
     }
-    const CodeScale cs(finite ? m : 0.0f);
+    const CodeScale<MODE != NO_NORM> cs(finite ? m : 0.0f);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         const int i = i0 + v * step;
@@ -263,7 +294,7 @@ __global__ void __launch_bounds__(WIDE ? most_threads<V, MODE>() : 256) rows_i8_
         if (MODE != NO_NORM && a.h)
             *reinterpret_cast<uint4 *>(a.h + base + (size_t)i * 8) = make_uint4(pack_bf16(p[0] * r, p[1] * r), pack_bf16(p[2] * r, p[3] * r),
                                                                               pack_bf16(p[4] * r, p[5] * r), pack_bf16(p[6] * r, p[7] * r));
-        if (a.q) *reinterpret_cast<uint2 *>(a.q + base + (size_t)i * 8) = codes ? codes_of(p, cs) : make_uint2(0u, 0u);
+        if (a.q) *reinterpret_cast<uint2 *>(a.q + base + (size_t)i * 8) = codes ? codes_of<MODE != NO_NORM>(p, cs) : make_uint2(0u, 0u);
     }
 }
 
@@ -286,14 +317,14 @@ spice_status launch_rows(const RowArgs &a, size_t rows, cudaStream_t st) {
     using std::integral_constant;
     // Few rows: a vector per thread, the shortest chain.  Many: more per thread, so that what a thread does beside its data
     // (reductions, the row's scale) is spread over more of it, as long as enough warps stay resident.
-    // 16 rows of 2048: norm 2.1 / 2.2 / 2.5 us with 1 / 2 / 4; 4096 rows of 2048: norm 14.5 / 13.8 / 15.1 us; 40960 rows of
-    // 3584: quantiser 160 / 110 / 87 / 111 us with 1 / 2 / 4 / 8.
+    // 16 rows of 2048: norm 1.7 / 1.8 / 2.3 us with 1 / 2 / 4; 4096 rows of 2048: norm 14.5 / 13.5 / 14.8 us; 40960 rows of
+    // 3584: quantiser 111 / 90 / 67 us; 333 rows of 2816: 2.46 / 2.46 / 2.55.
     const int want = rows < 1024 ? 1 : MODE == NO_NORM ? 4 : 2;
     if (nv <= 32) narrow(integral_constant<int, 1>{});
     else if (nv <= 64) narrow(integral_constant<int, 2>{});
     else if (want <= 1 && nv <= 1024) wide(integral_constant<int, 1>{});
     else if (want <= 2 && nv <= 2048) wide(integral_constant<int, 2>{});
-    else if (nv <= 4 * most_threads<4, MODE>()) wide(integral_constant<int, 4>{});
+    else if (nv <= 2048) wide(integral_constant<int, 4>{});
     else wide(integral_constant<int, 8>{});
     return ok ? SPICE_OK : SPICE_ERR_CUDA;
 }
