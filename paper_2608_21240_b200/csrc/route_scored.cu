@@ -15,8 +15,8 @@
 // be); so are the groups where the last one that stays and the first that does not are that close.  Where the order is
 // that of the logits nothing is rounded and the first answer stands.
 //
-// One warp per token.  Keys live in registers as integers that order like the floats: a round of the selection is one
-// warp-wide integer maximum, a ballot and a shuffle.  With groups, the keys pass through shared memory and only those of
+// One warp per token.  Keys live in registers; a round of the selection is one warp-wide maximum of the keys and one minimum of
+// the places that hold it (NaN marks a key that is out of the race: it is no maximum and equals nothing).  With groups, the keys pass through shared memory and only those of
 // the groups that stay are read back.  Bytes are few (4 N per token): the bound is the issue of instructions.
 #include "entry.cuh"
 #include "spice_internal.cuh"
@@ -38,14 +38,13 @@ struct RouteArgs {
     float scale;
 };
 
-// integers in the order of the floats; 0 is below every float and marks what is out of the race
-__device__ __forceinline__ uint32_t ordered(float v) {
-    const uint32_t b = __float_as_uint(v);
-    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+// the largest of a warp's values, NaN only where all are
+__device__ __forceinline__ float warp_max(float v) {
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
 }
-__device__ __forceinline__ float unordered(uint32_t k) {
-    return __uint_as_float(k ^ ((k & 0x80000000u) ? 0x80000000u : 0xffffffffu));
-}
+__device__ __forceinline__ float none() { return __uint_as_float(0x7fffffffu); }
 __device__ __forceinline__ unsigned long long ordered64(double v) {
     const long long b = __double_as_longlong(v);
     return (unsigned long long)b ^ ((unsigned long long)(b >> 63) | 0x8000000000000000ull);
@@ -208,10 +207,9 @@ __global__ void __launch_bounds__(WARPS * 32) route_scored_kernel(const RouteArg
     // ---- scores and keys
     float m = -INFINITY, inv = 1.0f;
     if (!a.sigmoid) {
-        uint32_t top = 0;
 #pragma unroll
-        for (int i = 0; i < V; ++i) top = max(top, ordered(v[i]));
-        m = unordered(__reduce_max_sync(FULL, top));
+        for (int i = 0; i < V; ++i) m = fmaxf(m, v[i]);
+        m = warp_max(m);
         if (by_score || !a.norm_topk) {
             float s = 0.0f;
 #pragma unroll
@@ -225,7 +223,7 @@ __global__ void __launch_bounds__(WARPS * 32) route_scored_kernel(const RouteArg
     // softmax score by (1.2 |x| + 2) 2^-23 e^x / sum, with |x| e^x < 0.37, and the V + 5 additions and the quotient: below
     // (13 + V) / 2 * 2^-23 of the largest score.
     const float tol = a.sigmoid ? 1e-6f : (13 + V) * 1.2e-7f * inv;
-    uint32_t key[V];
+    float key[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         const int e = lane + 32 * i;
@@ -233,10 +231,11 @@ __global__ void __launch_bounds__(WARPS * 32) route_scored_kernel(const RouteArg
         if (by_score && v[i] > -INFINITY)
             val = (a.sigmoid ? fast_sigmoid(v[i]) : (v[i] == m ? 1.0f : fast_exp(v[i] - m)) * inv) + b[i];
         if (grouped && e < N) shf[e] = val;
-        key[i] = e < N ? ordered(a.bias ? val : v[i]) : 0u;
+        key[i] = e < N ? (a.bias ? val : v[i]) : none();
     }
     // ---- groups: only the keys of those that stay are read back (in the order of the experts)
-    uint32_t sel[VS], open = FULL;
+    float sel[VS];
+    uint32_t open = FULL;
     int count = N;
     const int size = N / a.n_groups;
     int32_t *list = reinterpret_cast<int32_t *>(sh_keys + (size_t)WARPS * N) + warp * 32;
@@ -244,28 +243,23 @@ __global__ void __launch_bounds__(WARPS * 32) route_scored_kernel(const RouteArg
         __syncwarp();
         const int G = a.n_groups;
         const float mine = group_value<float>(a, shf, size, lane);
-        const int rank = rank_of<float>(mine, lane, G);
-        open = __ballot_sync(FULL, lane < G && rank < a.top_groups);
-        if (by_score && a.top_groups < G) {
-            const float in = __shfl_sync(FULL, mine, __ffs(__ballot_sync(FULL, lane < G && rank == a.top_groups - 1)) - 1);
-            const float out = __shfl_sync(FULL, mine, __ffs(__ballot_sync(FULL, lane < G && rank == a.top_groups)) - 1);
-            if (out > -INFINITY && in - out <= 2.0f * tol + 2.4e-7f * (fabsf(in) + fabsf(out))) {   // warp-uniform
-                open = slow_groups(a, l, shd, size, lane);
-                __syncwarp();
-#pragma unroll
-                for (int i = 0; i < V; ++i)   // the fp32 keys again: the doubles lay over them
-                    if (lane + 32 * i < N) shf[lane + 32 * i] = unordered(key[i]);
-            } else if (a.pair && !a.bias) {
-                __syncwarp();
-#pragma unroll
-                for (int i = 0; i < V; ++i)   // the winners go by the logits
-                    if (lane + 32 * i < N) shf[lane + 32 * i] = v[i];
-            }
-        } else if (a.pair && !a.bias) {
+        float left = lane < G ? mine : none(), in = 0.0f;
+        open = 0u;
+        for (int i = 0; i < a.top_groups; ++i) {
+            in = warp_max(left);
+            const int best = __ffs(__ballot_sync(FULL, left == in)) - 1;
+            open |= 1u << best;
+            if (lane == best) left = none();
+        }
+        const float out = by_score ? warp_max(left) : none();   // the best that does not stay (none: NaN)
+        const bool call = out > -INFINITY && in - out <= 2.0f * tol + 2.4e-7f * (fabsf(in) + fabsf(out));   // warp-uniform
+        if (call) open = slow_groups(a, l, shd, size, lane);
+        if (call || (a.pair && !a.bias)) {
+            // the winners' keys again: the doubles lay over them; or, without a bias, the logits in the place of the scores
             __syncwarp();
 #pragma unroll
             for (int i = 0; i < V; ++i)
-                if (lane + 32 * i < N) shf[lane + 32 * i] = v[i];
+                if (lane + 32 * i < N) shf[lane + 32 * i] = key[i];
         }
         if ((open >> lane) & 1u) list[__popc(open & ((1u << lane) - 1u))] = lane;
         __syncwarp();
@@ -273,57 +267,53 @@ __global__ void __launch_bounds__(WARPS * 32) route_scored_kernel(const RouteArg
 #pragma unroll
         for (int i = 0; i < VS; ++i) {
             const int c = lane + 32 * i;
-            sel[i] = 0u;
+            sel[i] = none();
             if (c < count) {
                 const int og = group_of(a, c);
-                sel[i] = ordered(shf[list[og] * size + c - og * size]);
+                sel[i] = shf[list[og] * size + c - og * size];
             }
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < VS; ++i) sel[i] = i < V ? key[i < V ? i : 0] : 0u;
+        for (int i = 0; i < VS; ++i) sel[i] = i < V ? key[i < V ? i : 0] : none();
     }
     // ---- winners: lane k keeps the k-th, its place among the candidates and its key
     int win = 0;
-    uint32_t won = 0u;
+    float won = none();
     auto round = [&](int k) {
-        uint32_t best = sel[0];
-        int at = lane;
+        float best = sel[0];
 #pragma unroll
-        for (int i = 1; i < VS; ++i)
-            if (sel[i] > best) {
-                best = sel[i];
-                at = lane + 32 * i;
-            }
-        const uint32_t top = __reduce_max_sync(FULL, best);
-        at = __reduce_min_sync(FULL, best == top ? at : 0x7fffffff);   // equal keys: the smaller index
+        for (int i = 1; i < VS; ++i) best = fmaxf(best, sel[i]);
+        const float top = warp_max(best);
+        int at = 0x7fffffff;
+#pragma unroll
+        for (int i = VS - 1; i >= 0; --i)
+            if (sel[i] == top) at = lane + 32 * i;
+        at = __reduce_min_sync(FULL, at);   // equal keys: the smaller index
         if (lane == k) {
             win = at;
             won = top;
         }
 #pragma unroll
         for (int i = 0; i < VS; ++i)
-            if (at == lane + 32 * i) sel[i] = 0u;
+            if (at == lane + 32 * i) sel[i] = none();
         return top;
     };
-    // whether a key is not told apart from the one before it in the order
-    auto near = [&](uint32_t before, uint32_t after) {
-        const float x = unordered(before), y = unordered(after);
-        return after != 0u && y > -INFINITY && x - y <= tol + 1.2e-7f * (fabsf(x) + fabsf(y));
-    };
+    // whether a key is not told apart from the one before it in the order (NaN: there is none)
+    auto near = [&](float x, float y) { return y > -INFINITY && x - y <= tol + 1.2e-7f * (fabsf(x) + fabsf(y)); };
     for (int k = 0; k < K; ++k) round(k);
     int have = K;
     bool close = false, many = false;
     if (a.bias) {
         // the first that is left is a possible winner too if the K-th is not told apart from it, and so on
-        const uint32_t last = __shfl_sync(FULL, won, K - 1), before = __shfl_up_sync(FULL, won, 1);
+        const float last = __shfl_sync(FULL, won, K - 1), before = __shfl_up_sync(FULL, won, 1);
         close = __any_sync(FULL, lane > 0 && lane < K && near(before, won));
         while (true) {
             if (have == 32) {   // no lane left: are there more?
-                uint32_t best = 0u;
+                float best = sel[0];
 #pragma unroll
-                for (int i = 0; i < VS; ++i) best = max(best, sel[i]);
-                many = near(last, __reduce_max_sync(FULL, best));
+                for (int i = 1; i < VS; ++i) best = fmaxf(best, sel[i]);
+                many = near(last, warp_max(best));
                 close |= many;
                 break;
             }
@@ -362,7 +352,7 @@ __global__ void __launch_bounds__(WARPS * 32) route_scored_kernel(const RouteArg
         // relative to the winners' largest, so that a row of tiny scores keeps its ratios:
         // softmax: e^(x - M); sigmoid: e^(min(x,0) - M) / (1 + e^-|x|)
         const float y = a.sigmoid ? fminf(x, 0.0f) : x;
-        const float M = unordered(__reduce_max_sync(FULL, ordered(y)));
+        const float M = warp_max(y);
         if (has) {
             g = y == M ? 1.0f : expf(y - M);
             if (a.sigmoid) g = __fdividef(g, 1.0f + expf(-fabsf(x)));
