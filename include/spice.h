@@ -263,7 +263,9 @@ spice_status spice_moe_layer_fwd_fp8(spice_ctx *ctx, const spice_layer_weights_f
  * spice_ctx or a workspace; the GPU is the calling thread's current device; all of them can be captured into a graph.
  * Used together: spice_residual_rmsnorm -> h, (q, scale);  spice_route_topk(h) -> logits;  spice_route_scored -> idx, gate
  * for spice_classify_misses and spice_grouped_expert_ffn;  spice_swiglu_i8(q) -> act;  spice_quantize_i8_rows(act);
- * spice_gemm_i8 -> y fp32 (SPICE_OUT_F32_ADD: into the sum of the routed experts), the next norm's delta_f32. */
+ * spice_gemm_i8 -> y fp32 (SPICE_OUT_F32_ADD: into the sum of the routed experts), the next norm's delta_f32.
+ * A call's kernel may be set up while the kernel before it in the stream drains; it touches no memory before that one is
+ * complete, so the caller sees ordinary stream order.  Outputs may not overlap inputs unless a call says so. */
 
 /* Residual addition and root-mean-square norm, for every token t:
  *     s = bf16(x_resid + delta) (added in fp32),   x_resid <- s,   r = 1 / sqrt(mean_j s_j^2 + eps)
@@ -272,7 +274,7 @@ spice_status spice_moe_layer_fwd_fp8(spice_ctx *ctx, const spice_layer_weights_f
  * so q_j * scale stands for the normalised value before its rounding to bf16.  The codes do not depend on r and are
  * rounded exactly.
  *   x_resid [T,d] bf16, in/out (only read without a delta).  delta [T,d] bf16 or delta_f32 [T,d] fp32: one of them, or
- *   neither (the norm of the stream as it is); it must not overlap x_resid.  weight [d] bf16.  eps >= 0.
+ *   neither (the norm of the stream as it is).  weight [d] bf16.  eps >= 0.
  *   h [T,d] bf16 out, q [T,d] int8 out with scale [T] fp32 out: either may be NULL, not both.
  *   A row of zeros has codes 0 and scale 1.  A row with a value that is not finite (or a product s_j * weight_j, or
  *   r, beyond fp32) has codes 0 and scale NaN; its h is what the formula gives.
@@ -295,7 +297,7 @@ spice_status spice_quantize_i8_rows(const spice_bf16 *w, int64_t rows, int32_t c
  *   device_status: optional device int32 which the caller has set to 0: raised to SPICE_ERR_TIMEOUT when a bounded wait
  *   inside the kernel expired (the outputs are undefined then).
  *   k a multiple of 16 up to 131056, n a multiple of 8; n and T up to 2^24 (SPICE_ERR_UNSUPPORTED_SHAPE above).  x_q, w_q,
- *   w_scale and y 16-byte aligned.  y must not overlap the inputs. */
+ *   w_scale and y 16-byte aligned. */
 enum { SPICE_OUT_BF16 = 0, SPICE_OUT_F32 = 1, SPICE_OUT_F32_ADD = 2 };
 spice_status spice_gemm_i8(const int8_t *x_q, const float *x_scale, const int8_t *w_q, const float *w_scale, int32_t T,
                            int32_t n, int32_t k, int32_t out, void *y, int32_t *device_status, void *stream);
@@ -315,8 +317,9 @@ spice_status spice_swiglu_i8(const int8_t *x_q, const float *x_scale, const int8
  *   n_groups > 1: the experts form n_groups equal runs of consecutive indices; a group's value is its largest key
  *   (SPICE_GROUP_MAX) or the sum of its two largest score_e + bias_e (SPICE_GROUP_TOP2; of a group with one available
  *   expert, that one's); only the experts of the top_groups best groups (equal values towards the smaller index) take part.
- *   An expert whose logit is NaN or -infinity, or whose bias is, is unavailable: behind every other one, score 0 (it is
- *   still returned, with gate 0, where too few others are left); a group without an available expert comes last.
+ *   An expert whose logit is NaN or -infinity, or whose bias is, is unavailable: behind every other one, with score 0 and
+ *   no part in the softmax (it is still returned, with gate 0, where too few others are left); a group without an available
+ *   expert comes last.  Logits of +infinity share a softmax equally.
  *   Where the winners' scores sum to 0, norm_topk gives gates of 0.
  *   Selection compares the exact values: experts that fp32 cannot tell apart are compared in fp64.
  *   1 <= n_experts <= 1024, n_experts a multiple of n_groups, n_groups <= 32, 1 <= top_groups <= n_groups,

@@ -39,7 +39,8 @@ inline int current_device_sms(int *device_out = nullptr) {
 // Launches a kernel that may be set up while the kernel before it in the stream still drains: such a kernel calls
 // grid_dependency() before its first access to global memory, which returns when everything before it is complete and
 // visible, and lets its own successor be set up as soon as all its blocks run.  Stream order, as the caller sees it, is
-// that of any launch; back to back, a call starts about a microsecond sooner.
+// that of any launch; back to back, a call starts about a microsecond sooner.  (What such a kernel reads may still be
+// written while it already runs, so it does not read it as constant for its lifetime: no __ldg, no __restrict__ on inputs.)
 template <typename... P, typename... A>
 inline bool launch_early(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, int cluster, A &&...args) {
     cudaLaunchConfig_t lc{};

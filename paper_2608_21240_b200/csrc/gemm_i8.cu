@@ -13,6 +13,7 @@
 // distributed shared memory, no workspace and no atomics.  Many tokens: pairs of CTAs work on 256 x 256 tiles
 // (cta_group::2: each CTA loads half of either operand), persistent, accumulators double-buffered in TMEM.
 #include <algorithm>
+#include <mutex>
 
 #include "entry.cuh"
 #include "spice_internal.cuh"
@@ -34,7 +35,7 @@ struct GemmI8Args {
     int32_t out;            // SPICE_OUT_*
     int32_t *status;        // optional
     // few tokens
-    int32_t split, stages, cols;   // CTAs along the reduction, ring stages, token columns of a tile (multiple of 16)
+    int32_t split, stages, cols;   // CTAs (pairs) along the reduction; ring stages, token columns of a tile (multiple of 16)
     // many tokens
     int32_t m_tiles, n_tiles;
 };
@@ -69,7 +70,7 @@ __device__ __forceinline__ void store4(const GemmI8Args &g, size_t at, float4 v)
 // cluster's sums are a chain of some 6 us).  What limits it is the reads of the tokens, which every block repeats.
 constexpr int FEW_MAX_TOKENS = 32;
 template <int NT, int NW, int UN, bool DEAL, bool SWIGLU>
-__global__ void __launch_bounds__(NW * 32) gemm_i8_few_kernel(const int8_t *__restrict__ x, const int8_t *__restrict__ w,
+__global__ void __launch_bounds__(NW * 32) gemm_i8_few_kernel(const int8_t *x, const int8_t *w,
                                                               const GemmI8Args g) {
     __shared__ int32_t red[NW][NT * 8][16 + 4];   // (padded: the 8 rows of a warp's store fall into different banks)
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -103,7 +104,7 @@ __global__ void __launch_bounds__(NW * 32) gemm_i8_few_kernel(const int8_t *__re
         for (int u = 0; u < UN; ++u) {
             const int v = (p0 + u * (DEAL ? NW : 1)) * 4 + c;
 #pragma unroll
-            for (int i = 0; i < NT; ++i) b[u][i] = v < nv && i * 8 + gq < g.T ? __ldg(x4 + (size_t)(i * 8 + gq) * nv + v) : zero;
+            for (int i = 0; i < NT; ++i) b[u][i] = v < nv && i * 8 + gq < g.T ? x4[(size_t)(i * 8 + gq) * nv + v] : zero;
         }
 #pragma unroll
         for (int u = 0; u < UN; ++u)
@@ -313,6 +314,7 @@ constexpr int PR_HALF_BYTES = 128 * BK;                        // a CTA's half o
 constexpr int PR_STAGE_BYTES = 2 * PR_HALF_BYTES;
 constexpr int PR_PITCH = 80;                                   // 64 B of a row's outputs + 16: 16-byte accesses do not collide
 constexpr int PR_STG_WARP = 32 * PR_PITCH;                     // an epilogue warp's transposition buffer
+static_assert(PR_TILE * 128 * 4 <= PR_STAGES * PR_STAGE_BYTES, "the sums fit in the ring");
 constexpr size_t PR_SMEM = (size_t)PR_STAGES * PR_STAGE_BYTES + PR_EPI_WARPS * PR_STG_WARP + 1024;
 constexpr int PR_GROUP_M = 16;                                 // token tiles that share a sweep over the weight tiles
 
@@ -334,7 +336,79 @@ __device__ __forceinline__ void pair_tile(const GemmI8Args &g, int tile, int &mt
     nt = in / width;
 }
 
-template <bool SWIGLU>
+// A warp's part of a tile: 32 tokens (row0 ..), 64 bytes of outputs at a time, every other piece of the columns [first, last).
+// load(c, v): the integer sums of columns c .. of this lane's token.  A lane holds one token's outputs; they are turned
+// through shared memory so that a store covers whole 16-byte pieces of consecutive columns.
+template <bool SWIGLU, typename Load>
+__device__ __forceinline__ void pair_store(const GemmI8Args &g, int row0, float xs, int col0, int first, int last, const float *ws,
+                                           unsigned char *stg, int lane, Load load) {
+    const float4 *w4 = reinterpret_cast<const float4 *>(ws), *u4 = w4 + 32;
+    if (SWIGLU || g.out == SPICE_OUT_BF16) {
+#pragma unroll 1
+        for (int c = first; c < last; c += 64) {
+            if (col0 + c >= g.n) break;
+            uint32_t v[32], u[SWIGLU ? 32 : 1];
+            load(c, v);
+            if constexpr (SWIGLU) load(128 + c, u);
+            tc_wait_ld();
+            uint32_t pk[16];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float4 w = w4[c / 4 + j];
+                float a[4] = {(float)(int32_t)v[4 * j] * xs * w.x, (float)(int32_t)v[4 * j + 1] * xs * w.y,
+                              (float)(int32_t)v[4 * j + 2] * xs * w.z, (float)(int32_t)v[4 * j + 3] * xs * w.w};
+                if constexpr (SWIGLU) {
+                    const float4 z = u4[c / 4 + j];
+                    a[0] = silu_times(a[0], (float)(int32_t)u[4 * j] * xs * z.x);
+                    a[1] = silu_times(a[1], (float)(int32_t)u[4 * j + 1] * xs * z.y);
+                    a[2] = silu_times(a[2], (float)(int32_t)u[4 * j + 2] * xs * z.z);
+                    a[3] = silu_times(a[3], (float)(int32_t)u[4 * j + 3] * xs * z.w);
+                }
+                pk[2 * j] = pack2(a[0], a[1]);
+                pk[2 * j + 1] = pack2(a[2], a[3]);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                *reinterpret_cast<uint4 *>(stg + lane * PR_PITCH + k * 16) = make_uint4(pk[4 * k], pk[4 * k + 1], pk[4 * k + 2], pk[4 * k + 3]);
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int rr = i * 8 + (lane >> 2), part = lane & 3, col = col0 + c + part * 8;
+                const uint4 val = *reinterpret_cast<const uint4 *>(stg + rr * PR_PITCH + part * 16);
+                if (row0 + rr < g.T && col < g.n)
+                    *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(g.y) + (size_t)(row0 + rr) * g.n + col) = val;
+            }
+            __syncwarp();
+        }
+    } else {
+#pragma unroll 1
+        for (int c = first; c < last; c += (c & 16) ? 48 : 16) {   // (the same 32 columns as above, 16 at a time)
+            if (col0 + c >= g.n) break;
+            uint32_t v[16];
+            load(c, v);
+            tc_wait_ld();
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float4 w = w4[c / 4 + j];
+                *reinterpret_cast<float4 *>(stg + lane * PR_PITCH + j * 16) =
+                    make_float4((float)(int32_t)v[4 * j] * xs * w.x, (float)(int32_t)v[4 * j + 1] * xs * w.y,
+                                (float)(int32_t)v[4 * j + 2] * xs * w.z, (float)(int32_t)v[4 * j + 3] * xs * w.w);
+            }
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int rr = i * 8 + (lane >> 2), part = lane & 3, col = col0 + c + part * 4;
+                const float4 val = *reinterpret_cast<const float4 *>(stg + rr * PR_PITCH + part * 16);
+                if (row0 + rr < g.T && col < g.n) store4(g, (size_t)(row0 + rr) * g.n + col, val);
+            }
+            __syncwarp();
+        }
+    }
+}
+
+// SPLIT: the reduction of a tile is shared by the g.split pairs of a cluster (one tile per cluster): each pair leaves its sums in
+// its shared memory and finishes its share of the columns with those of the others.
+template <bool SWIGLU, bool SPLIT>
 __global__ void __launch_bounds__(PR_THREADS, 1)
     gemm_i8_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const GemmI8Args g) {
     extern __shared__ __align__(16) unsigned char smem_raw[];   // (aligned to 1024 by hand: the swizzled tiles)
@@ -342,7 +416,8 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
     unsigned char *stage_base = ring + PR_STAGES * PR_STAGE_BYTES;
     __shared__ PairShared sh;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = cluster_rank();
+    const uint32_t rank = cluster_rank() & 1u, part = SPLIT ? cluster_rank() >> 1 : 0u, leader = 2 * part;
+    const uint32_t pair_mask = 3u << leader;
     volatile int *abort_flag = &sh.abort_flag;
 
     if (threadIdx.x == 0) {
@@ -370,8 +445,10 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
     grid_dependency();
 
     const int n_tiles = g.m_tiles * g.n_tiles;
-    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-    const int kblocks = (g.k + BK - 1) / BK;
+    const int pair = SPLIT ? blockIdx.x / (2 * g.split) : blockIdx.x >> 1, pairs = SPLIT ? n_tiles : gridDim.x >> 1;
+    const int all_blocks = (g.k + BK - 1) / BK;
+    const int kb0 = SPLIT ? all_blocks * (int)part / g.split : 0;
+    const int kblocks = SPLIT ? all_blocks * ((int)part + 1) / g.split - kb0 : all_blocks;
 
     if (warp == 0) {
         if (lane == 0) {
@@ -385,11 +462,11 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
                 for (int kb = 0; kb < kblocks; ++kb, ++it) {
                     const int s = it % PR_STAGES;
                     if (!mbar_wait(smem_u32(&sh.empty[s]), ((it / PR_STAGES) & 1) ^ 1, abort_flag)) { ok = false; break; }
-                    const uint32_t full = map_to_cta(smem_u32(&sh.full[s]), 0);
+                    const uint32_t full = map_to_cta(smem_u32(&sh.full[s]), leader);
                     const uint32_t dst = smem_u32(ring + s * PR_STAGE_BYTES);
                     if (rank == 0) mbar_expect_tx(smem_u32(&sh.full[s]), 2 * PR_STAGE_BYTES);
-                    tma_load_2d_pair(dst, &map_x, kb * BK, x_row, full);
-                    tma_load_2d_pair(dst + PR_HALF_BYTES, &map_w, kb * BK, w_row, full);
+                    tma_load_2d_pair(dst, &map_x, (kb0 + kb) * BK, x_row, full);
+                    tma_load_2d_pair(dst + PR_HALF_BYTES, &map_w, (kb0 + kb) * BK, w_row, full);
                 }
             }
             // a CTA ends when the stages it filled have been read by the MMAs: nothing of it is in flight then, neither a
@@ -415,14 +492,14 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
                     const uint64_t da = make_desc(a0), db = make_desc(a0 + PR_HALF_BYTES);
 #pragma unroll
                     for (int k = 0; k < BK / 32; ++k) tc_mma_i8_pair(d_tmem, da + 2 * k, db + 2 * k, idesc, (kb | k) ? 1u : 0u);
-                    tc_commit_pair(smem_u32(&sh.empty[s]));
+                    tc_commit_pair(smem_u32(&sh.empty[s]), pair_mask);
                 }
-                if (ok) tc_commit_pair(smem_u32(&sh.tmem_full[buf]));
+                if (ok) tc_commit_pair(smem_u32(&sh.tmem_full[buf]), pair_mask);
             }
             tc_commit_pair_local(smem_u32(&sh.mma_drain));
             mbar_drain(smem_u32(&sh.mma_drain), 0);
         }
-    } else {
+    } else if (!SPLIT) {
         // ---------------- epilogue: warp w reads TMEM lanes 32*(w%4) .. +31 = rows of this CTA's half of the tile; the two
         // warps of a quarter take alternate pieces of 64 bytes
         const int q = warp & 3, c_first = warp >= 6 ? 32 : 0;
@@ -448,95 +525,109 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
             if (gave_up) continue;
             tc_fence_after();
             const uint32_t tm = tmem_base + buf * PR_TILE + ((uint32_t)(q * 32) << 16);
-            const float4 *w4 = reinterpret_cast<const float4 *>(sh.ws[buf]), *u4 = w4 + 32;
-            // 64 bytes of outputs at a time: a lane holds one token's; turned through shared memory so that a store covers whole
-            // 16-byte pieces of consecutive columns
-            if (SWIGLU || g.out == SPICE_OUT_BF16) {
-#pragma unroll 1
-                for (int c = c_first; c < (SWIGLU ? 128 : PR_TILE); c += 64) {
-                    if (col0 + c >= g.n) break;
-                    uint32_t v[32], u[SWIGLU ? 32 : 1];
-                    tc_ld32(tm + c, v);
-                    if constexpr (SWIGLU) tc_ld32(tm + 128 + c, u);
-                    tc_wait_ld();
-                    uint32_t pk[16];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float4 w = w4[c / 4 + j];
-                        float a[4] = {(float)(int32_t)v[4 * j] * xs * w.x, (float)(int32_t)v[4 * j + 1] * xs * w.y,
-                                      (float)(int32_t)v[4 * j + 2] * xs * w.z, (float)(int32_t)v[4 * j + 3] * xs * w.w};
-                        if constexpr (SWIGLU) {
-                            const float4 z = u4[c / 4 + j];
-                            a[0] = silu_times(a[0], (float)(int32_t)u[4 * j] * xs * z.x);
-                            a[1] = silu_times(a[1], (float)(int32_t)u[4 * j + 1] * xs * z.y);
-                            a[2] = silu_times(a[2], (float)(int32_t)u[4 * j + 2] * xs * z.z);
-                            a[3] = silu_times(a[3], (float)(int32_t)u[4 * j + 3] * xs * z.w);
-                        }
-                        pk[2 * j] = pack2(a[0], a[1]);
-                        pk[2 * j + 1] = pack2(a[2], a[3]);
-                    }
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        *reinterpret_cast<uint4 *>(stg + lane * PR_PITCH + k * 16) = make_uint4(pk[4 * k], pk[4 * k + 1], pk[4 * k + 2], pk[4 * k + 3]);
-                    __syncwarp();
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int rr = i * 8 + (lane >> 2), part = lane & 3, col = col0 + c + part * 8;
-                        const uint4 val = *reinterpret_cast<const uint4 *>(stg + rr * PR_PITCH + part * 16);
-                        if (row0 + rr < g.T && col < g.n)
-                            *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(g.y) + (size_t)(row0 + rr) * g.n + col) = val;
-                    }
-                    __syncwarp();
-                }
-            } else {
-#pragma unroll 1
-                for (int c = c_first / 2; c < PR_TILE; c += 32) {
-                    if (col0 + c >= g.n) break;
-                    uint32_t v[16];
-                    tc_ld16(tm + c, v);
-                    tc_wait_ld();
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float4 w = w4[c / 4 + j];
-                        *reinterpret_cast<float4 *>(stg + lane * PR_PITCH + j * 16) =
-                            make_float4((float)(int32_t)v[4 * j] * xs * w.x, (float)(int32_t)v[4 * j + 1] * xs * w.y,
-                                        (float)(int32_t)v[4 * j + 2] * xs * w.z, (float)(int32_t)v[4 * j + 3] * xs * w.w);
-                    }
-                    __syncwarp();
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int rr = i * 8 + (lane >> 2), part = lane & 3, col = col0 + c + part * 4;
-                        const float4 val = *reinterpret_cast<const float4 *>(stg + rr * PR_PITCH + part * 16);
-                        if (row0 + rr < g.T && col < g.n) store4(g, (size_t)(row0 + rr) * g.n + col, val);
-                    }
-                    __syncwarp();
-                }
-            }
+            pair_store<SWIGLU>(g, row0, xs, col0, c_first, SWIGLU ? 128 : PR_TILE, sh.ws[buf], stg, lane, [&](int c, auto &v) {
+                if constexpr (sizeof(v) == 128) tc_ld32(tm + c, v);
+                else tc_ld16(tm + c, v);
+            });
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&sh.tmem_empty[buf]), 0));
+        }
+    } else {
+        // ---------------- epilogue of a shared tile: scales, then this pair's sums as [column][128 rows] over the ring:
+        // a peer's warp then reads 128 consecutive bytes (rows of 16-byte pieces in the lanes cost it 4 to 8 us more)
+        const int q = warp & 3, wc = threadIdx.x - 64;
+        int mt, nt;
+        pair_tile(g, pair, mt, nt);
+        const int wcol = nt * (SWIGLU ? 128 : PR_TILE) + (SWIGLU ? wc & 127 : wc);
+        sh.ws[0][wc] = wcol < g.n ? g.ws[wcol + (SWIGLU && wc >= 128 ? g.n : 0)] : 0.0f;
+        if (lane == 0) mbar_wait(smem_u32(&sh.tmem_full[0]), 0, abort_flag);
+        __syncwarp();
+        tc_fence_after();
+        int32_t *sums = reinterpret_cast<int32_t *>(ring) + q * 32 + lane;
+        for (int c = warp >= 6 ? 32 : 0; c < PR_TILE; c += 64) {
+            uint32_t v[32];
+            tc_ld32(tmem_base + c + ((uint32_t)(q * 32) << 16), v);
+            tc_wait_ld();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) sums[(c + j) * 128] = (int32_t)v[j];
         }
     }
     tc_fence_before();
     __syncthreads();
     if (threadIdx.x == 0 && sh.abort_flag && g.status) atomicMax(g.status, (int)SPICE_ERR_TIMEOUT);
-    cluster_sync();   // the pair's MMAs, copies and signals are over in both CTAs
+    cluster_sync();   // the pair's MMAs, copies and signals are over in both CTAs; SPLIT: everybody's sums are there
+    if (SPLIT) {
+        if (warp >= 2) {
+            int mt, nt;
+            pair_tile(g, pair, mt, nt);
+            const int q = warp & 3, row0 = mt * PR_TILE + (int)rank * 128 + q * 32;
+            const float xs = row0 + lane < g.T ? g.xs[row0 + lane] : 0.0f;
+            constexpr int PIECES = SWIGLU ? 4 : 8;   // pieces of 32 columns, dealt out to the pairs
+            const int first = PIECES * (int)part / g.split * 32, last = PIECES * ((int)part + 1) / g.split * 32;
+            const uint32_t at = smem_u32(ring) + (uint32_t)(q * 32 + lane) * 4u;
+            pair_store<SWIGLU>(g, row0, xs, nt * (SWIGLU ? 128 : PR_TILE), first + (warp >= 6 ? 32 : 0), last, sh.ws[0],
+                               stage_base + (warp - 2) * PR_STG_WARP, lane, [&](int c, auto &v) {
+                constexpr int N = sizeof(v) / 4;
+#pragma unroll
+                for (int j = 0; j < N; ++j) v[j] = 0u;
+#pragma unroll 2
+                for (int r = 0; r < g.split; ++r) {
+                    const uint32_t peer = map_to_cta(at + (uint32_t)c * 512u, 2 * (uint32_t)r + rank);
+                    uint32_t p[N];
+#pragma unroll
+                    for (int j = 0; j < N; ++j) asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(p[j]) : "r"(peer + j * 512));
+#pragma unroll
+                    for (int j = 0; j < N; ++j) v[j] += p[j];
+                }
+            });
+        }
+        cluster_sync();   // nobody leaves while a peer reads its sums
+    }
     tc_fence_after();
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512));
 }
 
 // ------------------------------------------------------------------------------------------------ host side
-// dynamic shared memory limits are raised once per device
-bool prepare_device(int dev) {
-    static std::atomic<bool> done[64];
-    if (done[dev].load(std::memory_order_acquire)) return true;
-    bool ok = true;
-    ok &= cudaFuncSetAttribute(gemm_i8_skinny_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, SK_MAX_SMEM) == cudaSuccess;
-    ok &= cudaFuncSetAttribute(gemm_i8_skinny_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, SK_MAX_SMEM) == cudaSuccess;
-    ok &= cudaFuncSetAttribute(gemm_i8_pair_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PR_SMEM) == cudaSuccess;
-    ok &= cudaFuncSetAttribute(gemm_i8_pair_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PR_SMEM) == cudaSuccess;
-    if (ok) done[dev].store(true, std::memory_order_release);
-    return ok;
+constexpr int PR_MAX_SPLIT = 4;
+
+// What a device is asked once: dynamic shared memory limits are raised, and how many clusters of 2 s of the pair kernel run at
+// the same time (an SM holds one CTA, a cluster stays inside a group of SMs).
+struct DeviceFacts {
+    std::atomic<bool> ready;
+    int clusters[PR_MAX_SPLIT + 1];
+};
+const DeviceFacts *device_facts(int dev, int sms) {
+    static DeviceFacts facts[64];
+    static std::mutex mutex;
+    DeviceFacts &f = facts[dev];
+    if (f.ready.load(std::memory_order_acquire)) return &f;
+    std::lock_guard<std::mutex> lock(mutex);
+    if (f.ready.load(std::memory_order_relaxed)) return &f;
+    auto raise = [](const void *kernel, size_t bytes) {
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess;
+    };
+    if (!raise((const void *)gemm_i8_skinny_kernel<false>, SK_MAX_SMEM) || !raise((const void *)gemm_i8_skinny_kernel<true>, SK_MAX_SMEM) ||
+        !raise((const void *)gemm_i8_pair_kernel<false, false>, PR_SMEM) || !raise((const void *)gemm_i8_pair_kernel<true, false>, PR_SMEM) ||
+        !raise((const void *)gemm_i8_pair_kernel<false, true>, PR_SMEM) || !raise((const void *)gemm_i8_pair_kernel<true, true>, PR_SMEM))
+        return nullptr;
+    for (int s = 2; s <= PR_MAX_SPLIT; ++s) {
+        cudaLaunchConfig_t lc{};
+        lc.gridDim = dim3((unsigned)(2 * s * sms), 1, 1);
+        lc.blockDim = dim3(PR_THREADS, 1, 1);
+        lc.dynamicSmemBytes = PR_SMEM;
+        cudaLaunchAttribute at[1];
+        at[0].id = cudaLaunchAttributeClusterDimension;
+        at[0].val.clusterDim.x = (unsigned)(2 * s);
+        at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+        lc.attrs = at;
+        lc.numAttrs = 1;
+        int n = 0;
+        if (cudaOccupancyMaxActiveClusters(&n, gemm_i8_pair_kernel<false, true>, &lc) != cudaSuccess) return nullptr;
+        f.clusters[s] = n;
+    }
+    f.ready.store(true, std::memory_order_release);
+    return &f;
 }
 
 template <int NT, int NW, int UN, bool SWIGLU>
@@ -550,7 +641,9 @@ template <bool SWIGLU>
 spice_status launch_gemm_i8(GemmI8Args g, const int8_t *x, const int8_t *w, cudaStream_t st) {
     int dev = 0;
     const int sms = current_device_sms(&dev);
-    if (sms <= 0 || !prepare_device(dev)) return SPICE_ERR_CUDA;
+    if (sms <= 0) return SPICE_ERR_CUDA;
+    const DeviceFacts *facts = device_facts(dev, sms);
+    if (!facts) return SPICE_ERR_CUDA;
     const int w_rows = SWIGLU ? 2 * g.n : g.n;
     const int kblocks = (g.k + BK - 1) / BK;
     const int64_t weights = (int64_t)w_rows * g.k;
@@ -580,9 +673,19 @@ spice_status launch_gemm_i8(GemmI8Args g, const int8_t *x, const int8_t *w, cuda
     // every round of the pairs over their tiles.  Measured, few-token kernel / pairs, us: 128 tokens 2048 x 2816 12.3 / 13.6,
     // 5632 x 2048 (SwiGLU) 13.7 / 12.2, 3584 x 20480 22 / 54, 40960 x 3584 (SwiGLU) 35 / 39, 512 x 512 8.0 / 7.4;  256 tokens
     // 14.0 / 13.7, 13.7 / 12.3, 30 / 54, 58 / 40, 8.0 / 7.5.
-    const int64_t rounds = ((int64_t)g.m_tiles * g.n_tiles + sms / 2 - 1) / (sms / 2);
+    const int64_t tiles_pair = (int64_t)g.m_tiles * g.n_tiles;
+    const int64_t rounds = (tiles_pair + sms / 2 - 1) / (sms / 2);
+    int64_t pair_ns = 7000 + rounds * kblocks * 300 + (rounds - 1) * 2000;
+    // Fewer tiles than pairs: 2 to 4 pairs share a tile's reduction, as long as all the clusters run at once.
+    int share = 1;
+    for (int s = 2; s <= PR_MAX_SPLIT; ++s) {
+        const int64_t ns = 10500 + (s - 2) * 1500 + (int64_t)((kblocks + s - 1) / s) * 300;
+        if (tiles_pair <= facts->clusters[s] && kblocks >= 2 * s && ns < pair_ns) {
+            pair_ns = ns;
+            share = s;
+        }
+    }
     const int64_t few_ns = 5500 + 40 * g.cols + (int64_t)tiles * kblocks * (SK_W_BYTES + g.cols * BK) / 12000;
-    const int64_t pair_ns = 7000 + rounds * kblocks * 300 + (rounds - 1) * 2000;
     if (g.T <= 256 && few_ns <= pair_ns) {
         // split the reduction until two CTAs per SM are busy, three stages each at least
         g.split = max(1, std::min({SK_MAX_SPLIT, 2 * sms / tiles, kblocks / 3}));
@@ -607,8 +710,16 @@ spice_status launch_gemm_i8(GemmI8Args g, const int8_t *x, const int8_t *w, cuda
     if (!tc_encode_map2_bytes(&map_x, x, (uint64_t)g.T, (uint64_t)g.k, 128) ||
         !tc_encode_map2_bytes(&map_w, w, (uint64_t)w_rows, (uint64_t)g.k, 128))
         return SPICE_ERR_CUDA;
-    const int pairs = max(1, min(sms / 2, g.m_tiles * g.n_tiles));
-    return launch_early(gemm_i8_pair_kernel<SWIGLU>, dim3(2 * (unsigned)pairs), PR_THREADS, PR_SMEM, st, 2, map_x, map_w, g) ? SPICE_OK : SPICE_ERR_CUDA;
+    bool ok;
+    if (share > 1) {
+        g.split = share;
+        ok = launch_early(gemm_i8_pair_kernel<SWIGLU, true>, dim3((unsigned)(2 * share * tiles_pair)), PR_THREADS, PR_SMEM, st, 2 * share,
+                          map_x, map_w, g);
+    } else {
+        const int pairs = max(1, min(sms / 2, g.m_tiles * g.n_tiles));
+        ok = launch_early(gemm_i8_pair_kernel<SWIGLU, false>, dim3(2 * (unsigned)pairs), PR_THREADS, PR_SMEM, st, 2, map_x, map_w, g);
+    }
+    return ok ? SPICE_OK : SPICE_ERR_CUDA;
 }
 
 template <bool SWIGLU>

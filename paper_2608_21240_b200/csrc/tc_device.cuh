@@ -92,10 +92,11 @@ __device__ __forceinline__ void tc_mma_i8_pair(uint32_t d_tmem, uint64_t a_desc,
         ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(0)
         : "memory");
 }
-// arrives on the barrier at this shared-memory offset in both CTAs of the pair once the MMAs issued so far are over
-__device__ __forceinline__ void tc_commit_pair(uint32_t mbar) {
+// arrives on the barrier at this shared-memory offset in the CTAs of the cluster that `mask` names (the two of the pair) once
+// the MMAs issued so far are over
+__device__ __forceinline__ void tc_commit_pair(uint32_t mbar, uint32_t mask) {
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                 ::"r"(mbar), "h"((uint16_t)3) : "memory");
+                 ::"r"(mbar), "h"((uint16_t)mask) : "memory");
 }
 // the same on this CTA's barrier only
 __device__ __forceinline__ void tc_commit_pair_local(uint32_t mbar) {

@@ -51,7 +51,8 @@ def check(T, n, k, out, full=False):
 
 SHAPES = [(1, 8, 16), (1, 2048, 2816), (3, 72, 48), (16, 136, 144), (17, 128, 2048), (33, 1000, 528), (64, 3584, 1040),
           (77, 264, 20480), (128, 200, 256), (129, 512, 4096), (256, 72, 128), (257, 264, 80), (300, 2048, 400), (512, 256, 128),
-          (513, 520, 1408), (1000, 128, 16), (1025, 2816, 272)]
+          (513, 520, 1408), (1000, 128, 16), (1025, 2816, 272), (130, 3592, 8192), (256, 264, 20480), (300, 1000, 8208), (512, 3584, 6160),
+          (700, 520, 20480)]
 
 
 @pytest.mark.parametrize("T,n,k", SHAPES)
@@ -79,7 +80,7 @@ def test_results_do_not_depend_on_the_batch():
     xq, xs = codes(600, 1408, 1)
     wq, ws = codes(2048, 1408, 2)
     whole = run(xq, xs, wq, ws, "f32")
-    for a, b in ((0, 1), (3, 20), (100, 190), (0, 256), (300, 599)):
+    for a, b in ((0, 1), (3, 11), (40, 53), (7, 38), (3, 60), (100, 190), (0, 256), (300, 599)):
         assert torch.equal(run(xq[a:b].contiguous(), xs[a:b].contiguous(), wq, ws, "f32"), whole[a:b])
 
 
@@ -100,7 +101,8 @@ def check_swiglu(T, inter, k, scale=1.0):
 
 
 @pytest.mark.parametrize("T,inter,k", [(1, 8, 16), (1, 2816, 2048), (2, 72, 48), (16, 136, 2048), (31, 64, 3584), (100, 200, 528),
-                                       (256, 72, 144), (257, 264, 80), (513, 136, 400), (700, 1408, 256)])
+                                       (256, 72, 144), (257, 264, 80), (513, 136, 400), (700, 1408, 256),
+                                       (9, 264, 2048), (40, 1408, 8192), (256, 520, 8208), (300, 136, 20480), (513, 1000, 6160)])
 def test_swiglu_matches_its_definition(T, inter, k):
     check_swiglu(T, inter, k)
 

@@ -5,6 +5,10 @@ whose fp32 rows are the next norm's residual.  Against a 64-bit evaluation of th
 Tolerance: the outputs' own of the layer's parity tests, 1e-2 max |reference| + 1e-3.  What separates the two: bf16 h and
 activations (2^-8 each), 8-bit codes of activations whose bf16 value falls on the other side of a border (one step of
 m / 127 in few of them), all relative to sums of hundreds of terms."""
+import os
+import subprocess
+import sys
+
 import pytest
 import torch
 
@@ -128,3 +132,41 @@ def test_a_captured_step_replays():
         # (the routed experts' rows are added in the order of the batch: bitwise equal)
         assert torch.equal(got, ref)
     L.close()
+
+
+FIRST = """
+import torch
+from paper_2608_21240_b200 import binding as B
+dev, bf, i8 = "cuda", torch.bfloat16, torch.int8
+x, w = torch.randn(300, 512, device=dev).to(bf), torch.ones(512, device=dev, dtype=bf)
+q, s = torch.zeros(300, 512, device=dev, dtype=i8), torch.zeros(300, device=dev)
+wq, ws = torch.randint(-127, 128, (64, 512), device=dev).to(i8), torch.rand(64, device=dev)
+ys = [torch.zeros(T, 64, device=dev, dtype=bf) for T in (1, 40, 300)]
+act = torch.zeros(300, 32, device=dev, dtype=bf)
+lg, idx, gate = torch.randn(5, 64, device=dev), torch.zeros(5, 6, device=dev, dtype=torch.int32), torch.zeros(5, 6, device=dev)
+def step():
+    B.spice_residual_rmsnorm(x, w, 1e-6, q, s)
+    for y in ys:
+        T = y.shape[0]
+        B.spice_gemm_i8(q[:T], s[:T], wq, ws, y)
+    B.spice_swiglu_i8(q, s, wq, ws, act)
+    B.spice_route_scored(lg, idx, gate)
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    step()
+g.replay()
+torch.cuda.synchronize()
+got = [t.clone() for t in (q, s, *ys, act, idx, gate)]
+assert all(bool(t.float().abs().sum() > 0) for t in got)
+step()
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(got, (q, s, *ys, act, idx, gate)))
+print("captured")
+"""
+
+
+def test_the_first_calls_of_a_process_may_be_captured():
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "captured" in r.stdout, r.stderr[-2000:]
