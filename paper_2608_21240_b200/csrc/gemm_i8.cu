@@ -69,6 +69,19 @@ __device__ __forceinline__ void store4(const GemmI8Args &g, size_t at, float4 v)
 // does not matter.  The call is over before the tensor-memory kernel has its first tile (descriptors, barriers, TMEM and the
 // cluster's sums are a chain of some 6 us).  What limits it is the reads of the tokens, which every block repeats.
 constexpr int FEW_MAX_TOKENS = 32;
+
+// 16 bytes that are read once (weights), or again by other warps of the SM (tokens)
+__device__ __forceinline__ int4 load_once(const int4 *p) {
+    int4 v;
+    asm volatile("ld.global.cs.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ int4 load_shared_by_warps(const int4 *p) {
+    int4 v;
+    asm volatile("ld.global.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+
 template <int NT, int NW, int UN, bool DEAL, bool SWIGLU>
 __global__ void __launch_bounds__(NW * 32) gemm_i8_few_kernel(const int8_t *x, const int8_t *w,
                                                               const GemmI8Args g) {
@@ -97,14 +110,14 @@ __global__ void __launch_bounds__(NW * 32) gemm_i8_few_kernel(const int8_t *x, c
 #pragma unroll
         for (int u = 0; u < UN; ++u) {
             const int v = (p0 + u * (DEAL ? NW : 1)) * 4 + c;
-            a0[u] = v < nv ? __ldcs(w0 + v) : zero;
-            a1[u] = v < nv ? __ldcs(w1 + v) : zero;
+            a0[u] = v < nv ? load_once(w0 + v) : zero;
+            a1[u] = v < nv ? load_once(w1 + v) : zero;
         }
 #pragma unroll
         for (int u = 0; u < UN; ++u) {
             const int v = (p0 + u * (DEAL ? NW : 1)) * 4 + c;
 #pragma unroll
-            for (int i = 0; i < NT; ++i) b[u][i] = v < nv && i * 8 + gq < g.T ? x4[(size_t)(i * 8 + gq) * nv + v] : zero;
+            for (int i = 0; i < NT; ++i) b[u][i] = v < nv && i * 8 + gq < g.T ? load_shared_by_warps(x4 + (size_t)(i * 8 + gq) * nv + v) : zero;
         }
 #pragma unroll
         for (int u = 0; u < UN; ++u)
