@@ -290,13 +290,14 @@ def _rows_of(what: str, t: torch.Tensor):
 # The raw handle of a device's current stream without a Stream object around it (2 us less per call, as much as the launch
 # itself); the public way where this build of torch does not have it.
 _current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _call_on(dev: int, name: str, stream, *args) -> None:
     """The entry point on the tensors' device, whatever the current one is."""
     st = _current_raw_stream(dev) if stream is None else stream.cuda_stream
     f = getattr(_lib or lib(), name)
-    if dev == torch.cuda.current_device():
+    if dev == _current_device():
         code = f(*args, st)
     else:
         with torch.cuda.device(dev):
@@ -336,7 +337,7 @@ def spice_gemm_i8(x_q, x_scale, w_q, w_scale, y, accumulate=False, device_status
     added to.  device_status: zeroed int32 tensor of one element that receives an expired wait."""
     f = "spice_gemm_i8"
     T, k, dev = _rows_of(f, x_q)
-    n = _rows_of(f, w_q)[0]
+    n = min(w_q.shape[0], 0x7fffffff) if w_q.dim() else 0   # (its shape is checked with its address)
     i8, f32 = torch.int8, torch.float32
     out = (OUT_F32_ADD if accumulate else OUT_F32) if y.dtype == f32 else OUT_BF16
     if accumulate and out == OUT_BF16:
@@ -351,7 +352,7 @@ def spice_swiglu_i8(x_q, x_scale, w_gate_up_q, w_scale, act, device_status=None,
     act [T,inter] bf16."""
     f = "spice_swiglu_i8"
     T, k, dev = _rows_of(f, x_q)
-    n2 = _rows_of(f, w_gate_up_q)[0]
+    n2 = min(w_gate_up_q.shape[0], 0x7ffffffe) if w_gate_up_q.dim() else 0
     if n2 % 2:
         raise SpiceError(f"{f}: w_gate_up_q has an odd number of rows")
     i8, f32 = torch.int8, torch.float32
@@ -365,7 +366,7 @@ def spice_route_scored(logits, idx, gate, bias=None, score=SCORE_SOFTMAX, n_grou
     """logits [T,N] fp32 (and bias [N] fp32) -> idx [T,K] int32, gate [T,K] fp32."""
     f = "spice_route_scored"
     T, N, dev = _rows_of(f, logits)
-    K = _rows_of(f, idx)[1]
+    K = min(idx.shape[-1], 0x7fffffff) if idx.dim() else 0
     f32 = torch.float32
     _call_on(dev, f, stream, _addr(f, logits, f32, (T, N), dev), _addr(f, bias, f32, (N,), dev), T, N, K, score, n_groups,
              top_groups, group_score, int(norm_topk), scale, _addr(f, idx, torch.int32, (T, K), dev),
