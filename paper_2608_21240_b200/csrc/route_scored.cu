@@ -34,6 +34,8 @@ struct RouteArgs {
     int32_t *idx;          // [T, K]
     float *gate;           // [T, K]
     int32_t T, N, K, n_groups, top_groups, norm_topk, sigmoid, pair;
+    int32_t size;          // experts of a group
+    int32_t lanes_log2;    // 2^lanes_log2 lanes share a group when the groups are weighed
     uint32_t size_magic;   // ceil(2^32 / (N / n_groups)): e / size as a high product (exact for e < 1024); 0 for size 1
     float scale;
 };
@@ -75,8 +77,8 @@ __device__ __forceinline__ void warp_best64(unsigned long long &key, int &e) {
 template <typename F>
 __device__ __forceinline__ F group_value(const RouteArgs &a, const F *keys, int size, int lane) {
     // `width` lanes share a group: each looks at every width-th member, then they merge
-    const int G = a.n_groups, width = 32 >> (32 - __clz(G - 1));
-    const int g = lane / width;
+    const int G = a.n_groups, width = 1 << a.lanes_log2;
+    const int g = lane >> a.lanes_log2;
     F b0 = -(F)INFINITY, b1 = b0;   // the two largest
     if (g < G) {
         for (int j = lane & (width - 1); j < size; j += width) {
@@ -91,7 +93,7 @@ __device__ __forceinline__ F group_value(const RouteArgs &a, const F *keys, int 
         b0 = max(b0, o0);
     }
     const F value = a.pair && b1 > -(F)INFINITY ? b0 + b1 : b0;
-    return __shfl_sync(FULL, value, (lane * width) & 31);
+    return __shfl_sync(FULL, value, (lane << a.lanes_log2) & 31);
 }
 
 // Rank of lane's key among those of lanes 0..n-1 (equal keys: the smaller `tag` first).
@@ -215,7 +217,7 @@ __global__ void __launch_bounds__(WARPS * 32) route_scored_kernel(const RouteArg
 #pragma unroll
             for (int i = 0; i < V; ++i) s += v[i] == m ? (m > -INFINITY ? 1.0f : 0.0f) : fast_exp(v[i] - m);
             s = warp_add(s);
-            inv = s > 0.0f ? 1.0f / s : 0.0f;
+            inv = s > 0.0f ? __fdividef(1.0f, s) : 0.0f;
         }
     }
     // Two keys nearer than tol (plus the rounding of score + bias) are not told apart.  A sigmoid score is off by at most
@@ -237,7 +239,7 @@ __global__ void __launch_bounds__(WARPS * 32) route_scored_kernel(const RouteArg
     float sel[VS];
     uint32_t open = FULL;
     int count = N;
-    const int size = N / a.n_groups;
+    const int size = a.size;
     int32_t *list = reinterpret_cast<int32_t *>(sh_keys + (size_t)WARPS * N) + warp * 32;
     if (grouped) {
         __syncwarp();
@@ -397,8 +399,10 @@ extern "C" spice_status spice_route_scored(const float *logits, const float *bia
         return SPICE_ERR_INVALID_ARG;
     const uint32_t size = (uint32_t)(n_experts / n_groups);
     const int pair = n_groups > 1 && group_score == SPICE_GROUP_TOP2;
+    int lanes_log2 = 5;
+    while (lanes_log2 > 0 && (n_groups << lanes_log2) > 32) --lanes_log2;
     const RouteArgs a{logits, bias, idx, gate, T, n_experts, top_k, n_groups, top_groups, norm_topk, score == SPICE_SCORE_SIGMOID, pair,
-                      size > 1 ? (uint32_t)((0x100000000ull + size - 1) / size) : 0u, scale};
+                      (int32_t)size, lanes_log2, size > 1 ? (uint32_t)((0x100000000ull + size - 1) / size) : 0u, scale};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const unsigned grid = ((unsigned)T + WARPS - 1) / WARPS;
     const size_t smem = n_groups > 1 || bias ? (size_t)WARPS * (n_experts * sizeof(double) + 32 * sizeof(int32_t)) : 0;   // up to 33 KB

@@ -134,6 +134,47 @@ def test_a_captured_step_replays():
     L.close()
 
 
+def test_products_beside_the_fused_layer_on_another_stream():
+    """The fused decode layer on one stream and 8-bit products of several sizes on another, many times over: each gives what
+    it gives alone."""
+    T = 16
+    wl = W.make_layer("dsv2lite", T, variant=72)
+    s = wl.shape
+    L = B.SpiceLayer(cfg_of(s), T)
+    dev = "cuda"
+    rnd = lambda *shape: (torch.randn(*shape, device=dev) * 0.02).bfloat16()  # noqa: E731
+    w = B.LayerWeights(rnd(s.n_experts, s.d), rnd(s.n_slots, 2 * s.inter, s.d), rnd(s.n_slots, s.d, s.inter),
+                       torch.from_numpy(wl.slot_of_expert.copy()).to(dev), rnd(2 * s.inter_shared, s.d), rnd(s.d, s.inter_shared),
+                       rnd(s.n_experts, s.lore_rank, s.d), rnd(s.n_experts, s.d, s.lore_rank))
+    w8 = B.quantize_shared_i8(w)
+    h, conf = torch.randn(T, s.d, device=dev).bfloat16(), torch.from_numpy(wl.conf).cuda()
+    y_ref = L.moe_layer_fwd(w, h, conf).y.clone()
+    batches, refs = [], []
+    for n in (3, 40, 200, 700):
+        x, q, sc = torch.randn(n, s.d, device=dev).bfloat16(), torch.empty(n, s.d, dtype=torch.int8, device=dev), torch.empty(n, device=dev)
+        B.spice_quantize_i8_rows(x, q, sc)
+        act, y = torch.empty(n, s.inter_shared, dtype=torch.bfloat16, device=dev), torch.empty(n, s.d, device=dev)
+        B.spice_swiglu_i8(q, sc, w8.q_gate_up, w8.s_gate_up, act)
+        B.spice_gemm_i8(q, sc, w8.q_gate_up[:s.d].contiguous(), w8.s_gate_up[:s.d].contiguous(), y)
+        batches.append((q, sc, act, y))
+        refs.append((act.clone(), y.clone()))
+    wq, ws = w8.q_gate_up[:s.d].contiguous(), w8.s_gate_up[:s.d].contiguous()
+    torch.cuda.synchronize()
+    one, two = torch.cuda.Stream(), torch.cuda.Stream()
+    outs = []
+    for i in range(60):
+        outs.append(L.moe_layer_fwd(w, h, conf, stream=one).y)
+        for q, sc, act, y in batches:
+            B.spice_swiglu_i8(q, sc, w8.q_gate_up, w8.s_gate_up, act, stream=two)
+            B.spice_gemm_i8(q, sc, wq, ws, y, stream=two)
+    torch.cuda.synchronize()
+    assert L.device_status() == 0
+    assert all(torch.equal(y, y_ref) for y in outs)
+    for (_, _, act, y), (ra, ry) in zip(batches, refs):
+        assert torch.equal(act, ra) and torch.equal(y, ry)
+    L.close()
+
+
 FIRST = """
 import torch
 from paper_2608_21240_b200 import binding as B
