@@ -248,6 +248,7 @@ __global__ void __launch_bounds__(SK_THREADS) gemm_i8_skinny_kernel(const __grid
             tc_commit(smem_u32(&sh.empty[s]));
         }
         tc_commit(smem_u32(&sh.done));
+        mbar_drain(smem_u32(&sh.done), 0);   // (one thread polls, the others wait in hardware: pollers slow the two that work)
     }
     __syncwarp();
     if (threadIdx.x >= 128) {   // the scales arrive while the products run
@@ -255,10 +256,8 @@ __global__ void __launch_bounds__(SK_THREADS) gemm_i8_skinny_kernel(const __grid
         sh.ws[r] = row < g.n ? g.ws[row + (SWIGLU && r >= 64 ? g.n : 0)] : 0.0f;
         for (int c = r; c < cols; c += 128) sh.xs[c] = t0 + c < g.T ? g.xs[t0 + c] : 0.0f;
     }
-    if (lane == 0) mbar_drain(smem_u32(&sh.done), 0);
-    __syncwarp();
+    __syncthreads();   // the products are done, and the producer has seen its last copies land: the ring is free
     tc_fence_after();
-    __syncthreads();   // (the producer has seen its last copies land: the ring is free)
 
     // ---- sums into shared memory, [token column][128 rows]
     const int ncol = min(cols, g.T - t0);
@@ -334,7 +333,7 @@ constexpr int PR_GROUP_M = 16;                                 // token tiles th
 struct PairShared {
     alignas(8) unsigned long long full[PR_STAGES], empty[PR_STAGES], tmem_full[2], tmem_empty[2], mma_drain;
     uint32_t tmem_base;
-    int abort_flag;
+    int abort_flag, gave_up;
     alignas(16) float ws[2][PR_TILE];   // channel scales of the tile (SwiGLU: gate, then up), per accumulator buffer
 };
 
@@ -443,7 +442,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
             mbar_init(smem_u32(&sh.tmem_empty[b]), 2 * PR_EPI_WARPS);   // used in the even CTA: the epilogue warps of both
         }
         mbar_init(smem_u32(&sh.mma_drain), 1);
-        sh.abort_flag = 0;
+        sh.abort_flag = sh.gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {   // TMEM: all 512 columns (two 256-column accumulators), in both CTAs
@@ -530,11 +529,10 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
             const float xs = row0 + lane < g.T ? g.xs[row0 + lane] : 0.0f;
             const int wc = threadIdx.x - 64, wcol = col0 + (SWIGLU ? wc & 127 : wc);
             sh.ws[buf][wc] = wcol < g.n ? g.ws[wcol + (SWIGLU && wc >= 128 ? g.n : 0)] : 0.0f;
+            // (one thread polls, the others wait in hardware: pollers slow the two threads that feed the tensor cores)
+            if (threadIdx.x == 64 && !gave_up && !mbar_wait(smem_u32(&sh.tmem_full[buf]), (tcount >> 1) & 1, abort_flag)) sh.gave_up = 1;
             asm volatile("bar.sync 1, 256;" ::: "memory");
-            bool ok = true;
-            if (lane == 0 && !gave_up) ok = mbar_wait(smem_u32(&sh.tmem_full[buf]), (tcount >> 1) & 1, abort_flag);
-            ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
-            gave_up |= !ok;
+            gave_up = *(volatile int *)&sh.gave_up != 0;
             if (gave_up) continue;
             tc_fence_after();
             const uint32_t tm = tmem_base + buf * PR_TILE + ((uint32_t)(q * 32) << 16);
@@ -554,8 +552,8 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
         pair_tile(g, pair, mt, nt);
         const int wcol = nt * (SWIGLU ? 128 : PR_TILE) + (SWIGLU ? wc & 127 : wc);
         sh.ws[0][wc] = wcol < g.n ? g.ws[wcol + (SWIGLU && wc >= 128 ? g.n : 0)] : 0.0f;
-        if (lane == 0) mbar_wait(smem_u32(&sh.tmem_full[0]), 0, abort_flag);
-        __syncwarp();
+        if (threadIdx.x == 64) mbar_wait(smem_u32(&sh.tmem_full[0]), 0, abort_flag);
+        asm volatile("bar.sync 1, 256;" ::: "memory");
         tc_fence_after();
         int32_t *sums = reinterpret_cast<int32_t *>(ring) + q * 32 + lane;
         for (int c = warp >= 6 ? 32 : 0; c < PR_TILE; c += 64) {
