@@ -658,11 +658,11 @@ spice_status launch_gemm_i8(GemmI8Args g, const int8_t *x, const int8_t *w, cuda
     const int w_rows = SWIGLU ? 2 * g.n : g.n;
     const int kblocks = (g.k + BK - 1) / BK;
     const int64_t weights = (int64_t)w_rows * g.k;
-    // Up to a few MB of weights the short start wins, beyond that the reads of the tokens cost more than it saves.
-    // 2048 x 2816, 5632 x 2048, 11264 x 2048, 3584 x 20480, 40960 x 3584 weights, us with this kernel / the tensor-memory one:
-    // 8 tokens 3.4/7.4, 4.7/8.5, 6.5/10, 16/18, 26/27;  16 tokens 4.5/7.6, 4.9/8.7, 8.0/10, 20/18, 35/27;
-    // 32 tokens 6.7/8.2, 6.3/9.3, 10.5/11, 33/19, 46/28
-    if (g.T <= 8 || (g.T <= 16 && weights <= (48 << 20)) || (g.T <= FEW_MAX_TOKENS && weights <= (24 << 20))) {
+    // Up to some MB of weights the short start wins, beyond that the reads of the tokens cost more than it saves.
+    // 512 x 512, 2048 x 2816, 5632 x 2048, 11264 x 2048, 3584 x 20480, 40960 x 3584 weights, us with this kernel / the
+    // tensor-memory one:  8 tokens 1.5/3.6, 3.1/5.7, 4.3/6.8, 7.0/8.7, 17.5/15.9, 25.6/25.9;  16 tokens 1.9/3.7, 4.5/6.0,
+    // 4.6/7.1, 7.7/8.8, 20/16, 37/26;  32 tokens 2.2/4.1, 6.7/6.6, 6.0/7.8, 10.3/9.7, 35/17, 46/26
+    if ((g.T <= 16 && weights <= (48 << 20)) || (g.T <= FEW_MAX_TOKENS && weights <= (16 << 20))) {
         const int blocks = (g.n + (SWIGLU ? 7 : 15)) / (SWIGLU ? 8 : 16);
         const bool wide = blocks < 2 * sms;   // few blocks: sixteen warps in each, enough bytes in flight
         const bool ok = g.T <= 8 ? (wide ? launch_few<1, 16, 4, SWIGLU>(g, x, w, blocks, st) : launch_few<1, 8, 4, SWIGLU>(g, x, w, blocks, st))
@@ -679,27 +679,29 @@ spice_status launch_gemm_i8(GemmI8Args g, const int8_t *x, const int8_t *w, cuda
     g.cols = ((g.T <= 128 ? g.T : (g.T + 1) / 2) + 15) & ~15;
     const int token_tiles = (g.T + g.cols - 1) / g.cols;
     const int tiles = row_tiles * token_tiles;
-    // Up to 256 tokens either tensor-core kernel can be the faster one: in ns, a start, a term for the sums that pass through
-    // shared memory and the bytes that the CTAs bring in at 12 TB/s, against a start and 300 ns per 128 of the reduction for
-    // every round of the pairs over their tiles.  Measured, few-token kernel / pairs, us: 128 tokens 2048 x 2816 12.3 / 13.6,
-    // 5632 x 2048 (SwiGLU) 13.7 / 12.2, 3584 x 20480 22 / 54, 40960 x 3584 (SwiGLU) 35 / 39, 512 x 512 8.0 / 7.4;  256 tokens
-    // 14.0 / 13.7, 13.7 / 12.3, 30 / 54, 58 / 40, 8.0 / 7.5.
+    // the reduction is split until two CTAs per SM are busy, three stages each at least
+    g.split = max(1, std::min({SK_MAX_SPLIT, 2 * sms / tiles, kblocks / 3}));
+    // Up to 256 tokens either tensor-memory kernel can be the faster one.  Estimates in ns: a start, what a token column costs
+    // in sums, and the bytes that the CTAs bring in at 11.5 TB/s, against a start and 310 ns per 128 of the reduction for
+    // every round of the pairs over their tiles.  Measured, few-token kernel / pairs, us, in the order above:  64 tokens
+    // 5.0/5.3, 8.4/11.1, 9.5/10.2, 10.6/10.8, 18/25, 28/36;  128 tokens 6.6/6.1, 11.0/12.0, 12.2/10.7, 12.7/11.7, 21/25, 33/37;
+    // 192 tokens 5.8/6.2, 10.3/12.0, 10.6/10.7, 13.7/11.7, 27/25, 53/38;  256 tokens 6.7/6.2, 11.9/12.1, 12.0/10.8, 15.3/11.9,
+    // 29/26, 56/38.
+    const int64_t few_ns = 4000 + (g.split > 1 ? 46 : 16) * g.cols + (int64_t)tiles * kblocks * (SK_W_BYTES + g.cols * BK) / 11500;
     const int64_t tiles_pair = (int64_t)g.m_tiles * g.n_tiles;
     const int64_t rounds = (tiles_pair + sms / 2 - 1) / (sms / 2);
-    int64_t pair_ns = 7000 + rounds * kblocks * 300 + (rounds - 1) * 2000;
-    // Fewer tiles than pairs: 2 to 4 pairs share a tile's reduction, as long as all the clusters run at once.
+    int64_t pair_ns = 5200 + rounds * kblocks * 310 + (rounds - 1) * 2000;
+    // Fewer tiles than pairs: 2 to 4 pairs share a tile's reduction, as long as all the clusters run at once (512 x 3584 x
+    // 20480 with one / two pairs to a tile: 54.6 / 33.8 us, 256 x 3584 x 20480 with one / four: 54 / 25.5).
     int share = 1;
     for (int s = 2; s <= PR_MAX_SPLIT; ++s) {
-        const int64_t ns = 10500 + (s - 2) * 1500 + (int64_t)((kblocks + s - 1) / s) * 300;
+        const int64_t ns = 9000 + (s - 2) * 1850 + (int64_t)((kblocks + s - 1) / s) * 310;
         if (tiles_pair <= facts->clusters[s] && kblocks >= 2 * s && ns < pair_ns) {
             pair_ns = ns;
             share = s;
         }
     }
-    const int64_t few_ns = 5500 + 40 * g.cols + (int64_t)tiles * kblocks * (SK_W_BYTES + g.cols * BK) / 12000;
     if (g.T <= 256 && few_ns <= pair_ns) {
-        // split the reduction until two CTAs per SM are busy, three stages each at least
-        g.split = max(1, std::min({SK_MAX_SPLIT, 2 * sms / tiles, kblocks / 3}));
         int per_sm = (tiles * g.split + sms - 1) / sms;
         per_sm = std::max(g.split > 1 ? 2 : 1, std::min(per_sm, 3));   // (clusters pack badly with one CTA per SM)
         const int per_cta = (kblocks + g.split - 1) / g.split;
