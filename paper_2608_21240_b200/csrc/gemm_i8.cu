@@ -676,18 +676,28 @@ spice_status launch_gemm_i8(GemmI8Args g, const int8_t *x, const int8_t *w, cuda
     if ((int64_t)g.m_tiles * g.n_tiles > 0x3fffffff) return SPICE_ERR_UNSUPPORTED_SHAPE;
     const int tile_n = SWIGLU ? 64 : 128;
     const int row_tiles = (g.n + tile_n - 1) / tile_n;
-    g.cols = ((g.T <= 128 ? g.T : (g.T + 1) / 2) + 15) & ~15;
-    const int token_tiles = (g.T + g.cols - 1) / g.cols;
-    const int tiles = row_tiles * token_tiles;
-    // the reduction is split until two CTAs per SM are busy, three stages each at least
-    g.split = max(1, std::min({SK_MAX_SPLIT, 2 * sms / tiles, kblocks / 3}));
-    // Up to 256 tokens either tensor-memory kernel can be the faster one.  Estimates in ns: a start, what a token column costs
-    // in sums, and the bytes that the CTAs bring in at 11.5 TB/s, against a start and 310 ns per 128 of the reduction for
-    // every round of the pairs over their tiles.  Measured, few-token kernel / pairs, us, in the order above:  64 tokens
+    // Up to 512 tokens either tensor-memory kernel can be the faster one.  Estimates in ns: a start, what a token column of a
+    // tile costs in sums, and the bytes that the CTAs bring in at 11.5 TB/s (narrower token tiles: fewer columns, the weights
+    // more often), against a start and 310 ns per 128 of the reduction for every round of the pairs over their tiles.
+    // Measured, few-token kernel (tiles of up to 128 tokens) / pairs, us, in the order above:  64 tokens
     // 5.0/5.3, 8.4/11.1, 9.5/10.2, 10.6/10.8, 18/25, 28/36;  128 tokens 6.6/6.1, 11.0/12.0, 12.2/10.7, 12.7/11.7, 21/25, 33/37;
     // 192 tokens 5.8/6.2, 10.3/12.0, 10.6/10.7, 13.7/11.7, 27/25, 53/38;  256 tokens 6.7/6.2, 11.9/12.1, 12.0/10.8, 15.3/11.9,
     // 29/26, 56/38.
-    const int64_t few_ns = 4000 + (g.split > 1 ? 46 : 16) * g.cols + (int64_t)tiles * kblocks * (SK_W_BYTES + g.cols * BK) / 11500;
+    int64_t few_ns = INT64_MAX;
+    int token_tiles = 1;
+    for (int tt = (g.T + 127) / 128; g.T <= 512 && tt <= 16; ++tt) {
+        const int cols = ((g.T + tt - 1) / tt + 15) & ~15, tiles = row_tiles * tt;
+        // the reduction is split until two CTAs per SM are busy, three stages each at least
+        const int split = max(1, std::min({SK_MAX_SPLIT, 2 * sms / tiles, kblocks / 3}));
+        const int64_t ns = 4000 + (split > 1 ? 46 : 16) * cols + (int64_t)tiles * kblocks * (SK_W_BYTES + cols * BK) / 11500;
+        if (ns < few_ns) {
+            few_ns = ns;
+            token_tiles = tt;
+            g.cols = cols;
+            g.split = split;
+        }
+    }
+    const int tiles = row_tiles * token_tiles;
     const int64_t tiles_pair = (int64_t)g.m_tiles * g.n_tiles;
     const int64_t rounds = (tiles_pair + sms / 2 - 1) / (sms / 2);
     int64_t pair_ns = 5200 + rounds * kblocks * 310 + (rounds - 1) * 2000;
@@ -701,7 +711,7 @@ spice_status launch_gemm_i8(GemmI8Args g, const int8_t *x, const int8_t *w, cuda
             share = s;
         }
     }
-    if (g.T <= 256 && few_ns <= pair_ns) {
+    if (few_ns <= pair_ns) {
         int per_sm = (tiles * g.split + sms - 1) / sms;
         per_sm = std::max(g.split > 1 ? 2 : 1, std::min(per_sm, 3));   // (clusters pack badly with one CTA per SM)
         const int per_cta = (kblocks + g.split - 1) / g.split;
