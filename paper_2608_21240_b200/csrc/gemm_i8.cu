@@ -602,12 +602,13 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
 // ------------------------------------------------------------------------------------------------ host side
 constexpr int PR_MAX_SPLIT = 4;
 
-// What a device is asked once: dynamic shared memory limits are raised, and how many clusters of 2 s of the pair kernel run at
-// the same time (an SM holds one CTA, a cluster stays inside a group of SMs).
+// What a device is asked once: dynamic shared memory limits are raised, and how many clusters of c CTAs run at the same time
+// when an SM holds one CTA (a cluster stays inside a group of SMs; clusters beyond that wait for a whole round).
 struct DeviceFacts {
     std::atomic<bool> ready;
-    int clusters[PR_MAX_SPLIT + 1];
+    int clusters[SK_MAX_SPLIT + 1];
 };
+static_assert(2 * PR_MAX_SPLIT <= SK_MAX_SPLIT, "the sizes that are asked for");
 const DeviceFacts *device_facts(int dev, int sms) {
     static DeviceFacts facts[64];
     static std::mutex mutex;
@@ -622,20 +623,18 @@ const DeviceFacts *device_facts(int dev, int sms) {
         !raise((const void *)gemm_i8_pair_kernel<false, false>, PR_SMEM) || !raise((const void *)gemm_i8_pair_kernel<true, false>, PR_SMEM) ||
         !raise((const void *)gemm_i8_pair_kernel<false, true>, PR_SMEM) || !raise((const void *)gemm_i8_pair_kernel<true, true>, PR_SMEM))
         return nullptr;
-    for (int s = 2; s <= PR_MAX_SPLIT; ++s) {
+    for (int c = 2; c <= SK_MAX_SPLIT; ++c) {
         cudaLaunchConfig_t lc{};
-        lc.gridDim = dim3((unsigned)(2 * s * sms), 1, 1);
+        lc.gridDim = dim3((unsigned)(c * sms), 1, 1);
         lc.blockDim = dim3(PR_THREADS, 1, 1);
         lc.dynamicSmemBytes = PR_SMEM;
         cudaLaunchAttribute at[1];
         at[0].id = cudaLaunchAttributeClusterDimension;
-        at[0].val.clusterDim.x = (unsigned)(2 * s);
+        at[0].val.clusterDim.x = (unsigned)c;
         at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
         lc.attrs = at;
         lc.numAttrs = 1;
-        int n = 0;
-        if (cudaOccupancyMaxActiveClusters(&n, gemm_i8_pair_kernel<false, true>, &lc) != cudaSuccess) return nullptr;
-        f.clusters[s] = n;
+        if (cudaOccupancyMaxActiveClusters(&f.clusters[c], gemm_i8_pair_kernel<false, true>, &lc) != cudaSuccess) return nullptr;
     }
     f.ready.store(true, std::memory_order_release);
     return &f;
@@ -687,8 +686,10 @@ spice_status launch_gemm_i8(GemmI8Args g, const int8_t *x, const int8_t *w, cuda
     int token_tiles = 1;
     for (int tt = (g.T + 127) / 128; g.T <= 512 && tt <= 16; ++tt) {
         const int cols = ((g.T + tt - 1) / tt + 15) & ~15, tiles = row_tiles * tt;
-        // the reduction is split until two CTAs per SM are busy, three stages each at least
-        const int split = max(1, std::min({SK_MAX_SPLIT, 2 * sms / tiles, kblocks / 3}));
+        // the reduction is split as far as all clusters run at once, two CTAs to an SM, with three stages each at least (148 SMs:
+        // 148, 90, 66, 52, 44, 30, 30 clusters of 2 to 8)
+        int split = max(1, min(SK_MAX_SPLIT, kblocks / 3));
+        while (split > 1 && tiles > 2 * facts->clusters[split]) --split;
         const int64_t ns = 4000 + (split > 1 ? 46 : 16) * cols + (int64_t)tiles * kblocks * (SK_W_BYTES + cols * BK) / 11500;
         if (ns < few_ns) {
             few_ns = ns;
@@ -706,7 +707,7 @@ spice_status launch_gemm_i8(GemmI8Args g, const int8_t *x, const int8_t *w, cuda
     int share = 1;
     for (int s = 2; s <= PR_MAX_SPLIT; ++s) {
         const int64_t ns = 9000 + (s - 2) * 1850 + (int64_t)((kblocks + s - 1) / s) * 310;
-        if (tiles_pair <= facts->clusters[s] && kblocks >= 2 * s && ns < pair_ns) {
+        if (tiles_pair <= facts->clusters[2 * s] && kblocks >= 2 * s && ns < pair_ns) {
             pair_ns = ns;
             share = s;
         }
