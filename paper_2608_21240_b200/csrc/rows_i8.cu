@@ -6,8 +6,9 @@
 //
 // (the quantiser: p = w, r = 1, no h).  r cancels out of q, and p is a product of two bf16 values, exact in fp32, so the
 // codes are a function of exactly known numbers.  They are rounded exactly: where the fp32 quotient lies within its error
-// of a border k + 1/2, 254 |p_j| and (2k + 1) m are compared, both exact in fp32 once m is scaled into [1, 2)
-// (16 + 8 and 8 + 16 significant bits).  No implementation that keeps the definition can differ by a step.
+// of a border k + 1/2, 254 |p_j| and (2k + 1) m are compared, both exact in fp32 (16 + 7 and 8 + 16 significant bits; m is
+// scaled by a power of two where it lies at the ends of the range).  No implementation that keeps the definition can differ
+// by a step.
 //
 // Both are bound by the bytes that cross HBM (9 per element of a bf16 step with both outputs, 3 for the quantiser): every
 // row is read once, held in registers as the packed bf16 pairs it is stored as, and written once.
@@ -247,7 +248,7 @@ __global__ void __launch_bounds__(WIDE ? most_threads<V>() : 256) rows_i8_kernel
     if (MODE != NO_NORM) {
         const float mean = sum * a.inv_d + a.eps;
         r = rsqrtf(mean);
-        r = r * (1.5f - 0.5f * mean * r * r);   // (one Newton step: within an ulp)
+        if (mean > 0.0f && mean < INFINITY) r = r * (1.5f - 0.5f * mean * r * r);   // (one Newton step: within an ulp)
         if (finite && !(mean >= 0x1p-60f && mean < INFINITY)) {   // (the same for the whole row)
             // squares at the ends of fp32's range: once more, of scaled values
             const float S = mean < 1.0f ? 0x1p64f : 0x1p-100f;

@@ -122,6 +122,9 @@ def test_norm_of_special_rows():
     h, q, s = check_norm(x, None, torch.ones_like(w), 1e-6)
     assert float(s[0]) == 1.0 and (q[0] == 0).all() and (h[0] == 0).all() and (q[5] == -127).all()
     assert torch.isnan(s[[3, 4, 7]]).all() and (q[[3, 4, 7]] == 0).all() and torch.isnan(h[4]).all()
+    # 1 / sqrt(infinity) = 0: the finite values of such a row become 0, the infinite one NaN
+    for row, at in ((3, 4), (7, 3)):
+        assert torch.isnan(h[row, at]) and (h[row, torch.arange(384, device="cuda") != at] == 0).all()
     y, _, _ = draw(2, 2048, 6, None)                # the same over several warps
     y[0] *= 1e25
     check_norm(y, None, torch.ones(2048, dtype=bf, device="cuda"), 1e-6)

@@ -88,3 +88,45 @@ def test_binding_refuses_host_tensors_and_wrong_shapes():
         with pytest.raises(B.SpiceError, match="f: expected a contiguous"):
             B._addr("f", t, dtype, shape, 0)
     assert B._addr("f", None, bf, (2, 8), 0) is None
+
+
+def test_calls_go_to_the_tensors_device_and_its_stream(monkeypatch):
+    """With the tensors on device 1 while device 0 is current, the entry point runs inside a switch to device 1 and gets that
+    device's current stream (or the stream that was given); an error code becomes an exception."""
+    log = []
+
+    class Lib:
+        def spice_gemm_i8(self, *args):
+            log.append(("call", args))
+            return 0
+
+        def spice_swiglu_i8(self, *args):
+            return 1
+
+        def spice_status_string(self, code):
+            return b"invalid argument"
+
+    class On:
+        def __init__(self, dev):
+            self.dev = dev
+
+        def __enter__(self):
+            log.append(("enter", self.dev))
+
+        def __exit__(self, *exc):
+            log.append(("exit", self.dev))
+
+    class Stream:
+        cuda_stream = 4242
+
+    monkeypatch.setattr(B, "_lib", Lib())
+    monkeypatch.setattr(B, "_current_device", lambda: 0)
+    monkeypatch.setattr(B, "_current_raw_stream", lambda dev: 100 + dev)
+    monkeypatch.setattr(torch.cuda, "device", On)
+    B._call_on(1, "spice_gemm_i8", None, 7, 8)
+    assert log == [("enter", 1), ("call", (7, 8, 101)), ("exit", 1)]
+    log.clear()
+    B._call_on(0, "spice_gemm_i8", Stream(), 7)
+    assert log == [("call", (7, 4242))]
+    with pytest.raises(B.SpiceError, match="spice_swiglu_i8: invalid argument"):
+        B._call_on(0, "spice_swiglu_i8", None, 7)
