@@ -686,6 +686,7 @@ spice_status launch_gemm_i8(GemmI8Args g, const int8_t *x, const int8_t *w, cuda
     int token_tiles = 1;
     for (int tt = (g.T + 127) / 128; g.T <= 512 && tt <= 16; ++tt) {
         const int cols = ((g.T + tt - 1) / tt + 15) & ~15, tiles = row_tiles * tt;
+        if ((g.T + cols - 1) / cols < tt) continue;   // (fewer tiles of this width do)
         // the reduction is split as far as all clusters run at once, two CTAs to an SM, with three stages each at least (148 SMs:
         // 148, 90, 66, 52, 44, 30, 30 clusters of 2 to 8)
         int split = max(1, min(SK_MAX_SPLIT, kblocks / 3));
