@@ -681,6 +681,7 @@ spice_status launch_gemm_i8(GemmI8Args g, const int8_t *x, const int8_t *w, cuda
     // Measured, few-token kernel / pairs, us, in the order above:  64 tokens 3.8/5.3, 6.9/11.1, 8.7/10.2, 10.6/10.8, 18/25,
     // 28/36;  128 tokens 3.9/6.1, 8.0/12.0, 9.9/10.7, 12.7/11.7, 21/25, 33/37;  192 tokens 3.8/6.2, 8.7/12.0, 10.6/10.7,
     // 13.7/11.7, 27/25, 53/38;  256 tokens 4.0/6.2, 9.1/12.1, 12.0/10.8, 15.3/11.9, 29/26, 56/38;  384 tokens 4.4/6.3, 10.3/12.4.
+    // (Where the pairs are ahead, the other figure is that of tiles of up to 128 tokens, the widest there are.)
     int64_t few_ns = INT64_MAX;
     int token_tiles = 1;
     for (int tt = (g.T + 127) / 128; g.T <= 512 && tt <= 16; ++tt) {
