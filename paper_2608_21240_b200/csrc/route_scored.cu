@@ -73,9 +73,10 @@ __device__ __forceinline__ void warp_best64(unsigned long long &key, int &e) {
     }
 }
 
-// What the groups' values are made of, for the n_groups groups of `size` keys in shared memory: lane g gets group g's.
+// What the groups' values are made of, for the n_groups groups of `size` keys in shared memory: lane g gets group g's, and in
+// `terms` the magnitudes of the keys that it is made of (a sum of two may be far smaller than they are).
 template <typename F>
-__device__ __forceinline__ F group_value(const RouteArgs &a, const F *keys, int size, int lane) {
+__device__ __forceinline__ F group_value(const RouteArgs &a, const F *keys, int size, int lane, F &terms) {
     // `width` lanes share a group: each looks at every width-th member, then they merge
     const int G = a.n_groups, width = 1 << a.lanes_log2;
     const int g = lane >> a.lanes_log2;
@@ -92,7 +93,9 @@ __device__ __forceinline__ F group_value(const RouteArgs &a, const F *keys, int 
         b1 = max(max(b1, o1), min(b0, o0));
         b0 = max(b0, o0);
     }
-    const F value = a.pair && b1 > -(F)INFINITY ? b0 + b1 : b0;
+    const bool both = a.pair && b1 > -(F)INFINITY;
+    const F value = both ? b0 + b1 : b0;
+    terms = __shfl_sync(FULL, both ? fabs(b0) + fabs(b1) : fabs(b0), (lane << a.lanes_log2) & 31);
     return __shfl_sync(FULL, value, (lane << a.lanes_log2) & 31);
 }
 
@@ -137,7 +140,8 @@ __device__ __noinline__ uint32_t slow_groups(const RouteArgs &a, const float *l,
     __syncwarp();
     for (int e = lane; e < a.N; e += 32) keys[e] = sc.key(a, l, e);
     __syncwarp();
-    const double v = group_value<double>(a, keys, size, lane);
+    double terms;
+    const double v = group_value<double>(a, keys, size, lane, terms);
     const int rank = rank_of<double>(v, lane, a.n_groups);
     return __ballot_sync(FULL, lane < a.n_groups && rank < a.top_groups);
 }
@@ -244,17 +248,23 @@ __global__ void __launch_bounds__(WARPS * 32) route_scored_kernel(const RouteArg
     if (grouped) {
         __syncwarp();
         const int G = a.n_groups;
-        const float mine = group_value<float>(a, shf, size, lane);
-        float left = lane < G ? mine : none(), in = 0.0f;
+        float terms;
+        const float mine = group_value<float>(a, shf, size, lane, terms);
+        float left = lane < G ? mine : none();
         open = 0u;
         for (int i = 0; i < a.top_groups; ++i) {
-            in = warp_max(left);
-            const int best = __ffs(__ballot_sync(FULL, left == in)) - 1;
+            const float best_left = warp_max(left);
+            const int best = __ffs(__ballot_sync(FULL, left == best_left)) - 1;
             open |= 1u << best;
             if (lane == best) left = none();
         }
-        const float out = by_score ? warp_max(left) : none();   // the best that does not stay (none: NaN)
-        const bool call = out > -INFINITY && in - out <= 2.0f * tol + 2.4e-7f * (fabsf(in) + fabsf(out));   // warp-uniform
+        // A group's value is off by at most `off`: a score of each of its keys (tol / 2), the rounding of each key and that of
+        // their sum (2^-24 of the keys' magnitudes each).  The choice stands where no group that does not stay can be worth as
+        // much as one that does.
+        const float off = fminf(tol + 2.4e-7f * terms, 3e38f);
+        const float out = by_score ? warp_max(left + off) : none();                                             // (none: NaN)
+        const float in = -warp_max((open >> lane) & 1u ? off - mine : none());
+        const bool call = out > -INFINITY && !(in > out);   // warp-uniform
         if (call) open = slow_groups(a, l, shd, size, lane);
         if (call || (a.pair && !a.bias)) {
             // the winners' keys again: the doubles lay over them; or, without a bias, the logits in the place of the scores

@@ -211,3 +211,16 @@ def test_refusals_on_tensors():
                      ((lg, idx, gate), dict(n_groups=16, top_groups=1)), ((lg, idx, gate), dict(score=2))):
         with pytest.raises(B.SpiceError):
             B.spice_route_scored(*args, **kw)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("big", [4.0, 64.0, 256.0, 1e6])
+def test_groups_whose_two_best_keys_cancel(score, big):
+    """A group's value is the sum of two keys that may be far larger than it: +-big in every group, sums 1e-7 to 5e-6 apart.
+    The keys' own rounding decides how far fp32 can be trusted."""
+    r = np.random.default_rng(int(big))
+    for N, G, top, spread in ((64, 8, 4, 1e-5), (1024, 32, 8, 1e-3 if score == "softmax" else 1e-5)):
+        l = (0.3 + spread * r.standard_normal((200, N))).astype(np.float32)
+        bias = np.full(N, -4 * big, np.float32)
+        bias[::N // G], bias[1::N // G] = big, np.float32(-big + 0.125)
+        check(l, bias, 8, score, G=G, top=top, pair=True)
