@@ -18,6 +18,8 @@
 // One warp per token.  Keys live in registers; a round of the selection is one warp-wide maximum of the keys and one minimum of
 // the places that hold it (NaN marks a key that is out of the race: it is no maximum and equals nothing).  With groups, the keys pass through shared memory and only those of
 // the groups that stay are read back.  Bytes are few (4 N per token): the bound is the issue of instructions.
+#include <cfloat>
+
 #include "entry.cuh"
 #include "spice_internal.cuh"
 
@@ -94,7 +96,8 @@ __device__ __forceinline__ F group_value(const RouteArgs &a, const F *keys, int 
         b0 = max(b0, o0);
     }
     const bool both = a.pair && b1 > -(F)INFINITY;
-    const F value = both ? b0 + b1 : b0;
+    F value = both ? b0 + b1 : b0;
+    if (both && value == -(F)INFINITY) value = -(F)FLT_MAX;   // two keys at the low end of fp32: not a group without an expert
     terms = __shfl_sync(FULL, both ? fabs(b0) + fabs(b1) : fabs(b0), (lane << a.lanes_log2) & 31);
     return __shfl_sync(FULL, value, (lane << a.lanes_log2) & 31);
 }

@@ -224,3 +224,20 @@ def test_groups_whose_two_best_keys_cancel(score, big):
         bias = np.full(N, -4 * big, np.float32)
         bias[::N // G], bias[1::N // G] = big, np.float32(-big + 0.125)
         check(l, bias, 8, score, G=G, top=top, pair=True)
+
+
+def test_groups_whose_two_best_keys_sum_beyond_fp32():
+    """Biases of the type's lowest value: the sum of two is below fp32's range, but the experts are there, and come before a
+    group without an available one."""
+    low = np.finfo(np.float32).min
+    bias = np.full(24, -np.inf, np.float32)
+    bias[8:16] = low
+    l = draw(5, 24, 31, False)[0]
+    gi, gg = check(l, bias, 2, G=3, pair=True)
+    assert (gi >= 8).all() and (gi < 16).all() and (gg > 0).all()
+    bias[17] = low                                       # one such expert alone is worth more than two
+    gi, _ = check(l, bias, 1, G=3, pair=True)
+    assert (gi == 17).all()
+    bias[:8], bias[9], bias[10] = -0.8 * low, -low, -0.9 * low   # and the same above it
+    gi, _ = check(l, bias, 2, G=3, pair=True)
+    assert (gi == [9, 10]).all()
