@@ -155,6 +155,65 @@ __device__ __forceinline__ float warp_sum_xor(float v) {
     return v;
 }
 
+__device__ __forceinline__ double warp_sum_xor(double v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+__device__ __forceinline__ double warp_max_xor(double v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = fmax(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
+}
+
+// A row whose squares or products leave fp32's range, in fp64, where both are exact: the scale, the codes and h (the stream is
+// written already).  Such rows are rare, so the row is read again, by the threads that wrote it; nothing of it is kept in
+// registers.  The quotient 127 p / m is at least 2^-27 away from a border that it does not lie on (16 significant bits in p and
+// m, and p > m / 256 where a border is near), so its rounding to fp64 crosses none.
+template <bool WIDE>
+__device__ __noinline__ void row_in_fp64(const RowArgs a, size_t row, int i0, int step) {
+    __shared__ double sh_sum[32], sh_top[32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = blockDim.x >> 5;
+    const int nv = a.d >> 3;
+    const size_t base = row * (size_t)a.d;
+    auto word_x = [&](int i, int j) { return reinterpret_cast<const uint32_t *>(a.x + base)[i * 4 + j]; };
+    auto word_w = [&](int i, int j) { return reinterpret_cast<const uint32_t *>(a.weight)[i * 4 + j]; };
+    double sum = 0.0, top = 0.0;
+    for (int i = i0; i < nv; i += step) {
+#pragma unroll 1
+        for (int k = 0; k < 8; ++k) {
+            const uint32_t x = word_x(i, k >> 1), w = word_w(i, k >> 1);
+            const double s = k & 1 ? bf_hi(x) : bf_lo(x), p = s * (double)(k & 1 ? bf_hi(w) : bf_lo(w));
+            sum += s * s;
+            top = fmax(top, p == p ? fabs(p) : (double)INFINITY);
+        }
+    }
+    sum = warp_sum_xor(sum);
+    top = warp_max_xor(top);
+    if (WIDE) {
+        if (lane == 0) {
+            sh_sum[warp] = sum;
+            sh_top[warp] = top;
+        }
+        __syncthreads();
+        sum = warp_sum_xor(lane < nw ? sh_sum[lane] : 0.0);
+        top = warp_max_xor(lane < nw ? sh_top[lane] : 0.0);
+    }
+    const double r = 1.0 / sqrt(sum / a.d + (double)a.eps);
+    const bool codes = (float)top < INFINITY && ((float)r < INFINITY || top == 0.0);
+    if (a.q && i0 == 0) a.scale[row] = !codes ? __uint_as_float(0x7fffffffu) : top == 0.0 ? 1.0f : (float)(top * r / 127.0);
+    for (int i = i0; i < nv; i += step) {
+#pragma unroll 1
+        for (int k = 0; k < 8; ++k) {
+            const uint32_t x = word_x(i, k >> 1), w = word_w(i, k >> 1);
+            const double p = (double)(k & 1 ? bf_hi(x) : bf_lo(x)) * (double)(k & 1 ? bf_hi(w) : bf_lo(w));
+            const size_t at = base + (size_t)i * 8 + k;
+            if (a.h) a.h[at] = __float2bfloat16_rn((float)(p * r));
+            if (a.q) a.q[at] = codes && top > 0.0 ? (int8_t)(int)rint(127.0 * p / top) : (int8_t)0;
+        }
+    }
+}
+
 // threads of a block: what its registers leave room for
 template <int V>
 constexpr int most_threads() {
@@ -247,37 +306,17 @@ __global__ void __launch_bounds__(WIDE ? most_threads<V>() : 256) rows_i8_kernel
     float r = 1.0f;
     if (MODE != NO_NORM) {
         const float mean = sum * a.inv_d + a.eps;
-        r = rsqrtf(mean);
-        if (mean > 0.0f && mean < INFINITY) r = r * (1.5f - 0.5f * mean * r * r);   // (one Newton step: within an ulp)
-        if (finite && !(mean >= 0x1p-60f && mean < INFINITY)) {   // (the same for the whole row)
-            // squares at the ends of fp32's range: once more, of scaled values
-            const float S = mean < 1.0f ? 0x1p64f : 0x1p-100f;
-            float s2 = 0.0f;
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const uint32_t *x = reinterpret_cast<const uint32_t *>(&xs[v]);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float lo = bf_lo(x[j]) * S, hi = bf_hi(x[j]) * S;
-                    s2 = fmaf(lo, lo, s2);
-                    s2 = fmaf(hi, hi, s2);
-                }
-            }
-            s2 = warp_sum_xor(s2);
-            if (WIDE) {
-                __syncthreads();
-                if (lane == 0) sh_sum[warp] = s2;
-                __syncthreads();
-                s2 = warp_sum_xor(lane < nw ? sh_sum[lane] : 0.0f);
-            }
-            r = S / sqrtf(s2 * a.inv_d + a.eps * S * S);
+        if (!finite || !(mean >= 0x1p-60f && mean < INFINITY)) {   // (the same for the whole row)
+            row_in_fp64<WIDE>(a, row, i0, step);
+            return;
         }
+        r = rsqrtf(mean);
+        r = r * (1.5f - 0.5f * mean * r * r);   // (one Newton step: within an ulp)
     }
     const float m = __uint_as_float(big);
-    const bool codes = finite && (r < INFINITY || m == 0.0f);
     if (a.q && i0 == 0) {
         constexpr float C = 1.0f / 127.0f;
-        a.scale[row] = !codes ? __uint_as_float(0x7fffffffu) : m == 0.0f ? 1.0f : m > 1.0f ? (m * C) * r : m * (r * C);
+        a.scale[row] = !finite ? __uint_as_float(0x7fffffffu) : m == 0.0f ? 1.0f : m > 1.0f ? (m * C) * r : m * (r * C);
     }
     const CodeScale<MODE != NO_NORM> cs(finite ? m : 0.0f);
 #pragma unroll
@@ -295,7 +334,7 @@ __global__ void __launch_bounds__(WIDE ? most_threads<V>() : 256) rows_i8_kernel
         if (MODE != NO_NORM && a.h)
             *reinterpret_cast<uint4 *>(a.h + base + (size_t)i * 8) = make_uint4(pack_bf16(p[0] * r, p[1] * r), pack_bf16(p[2] * r, p[3] * r),
                                                                               pack_bf16(p[4] * r, p[5] * r), pack_bf16(p[6] * r, p[7] * r));
-        if (a.q) *reinterpret_cast<uint2 *>(a.q + base + (size_t)i * 8) = codes ? codes_of<MODE != NO_NORM>(p, cs) : make_uint2(0u, 0u);
+        if (a.q) *reinterpret_cast<uint2 *>(a.q + base + (size_t)i * 8) = finite ? codes_of<MODE != NO_NORM>(p, cs) : make_uint2(0u, 0u);
     }
 }
 

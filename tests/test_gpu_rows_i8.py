@@ -207,3 +207,21 @@ def test_refusals_on_tensors():
         B.spice_residual_rmsnorm(flat[4:4 + 256].view(4, 64), w, 1e-6, q, s)      # 8-byte aligned rows
     with pytest.raises(B.SpiceError):
         B.spice_quantize_i8_rows(x, q[:, :32], s)
+
+
+def test_norm_of_products_beyond_fp32():
+    """Squares beyond fp32 and one product that is, too (the codes are 0 and the scale NaN then): h is what the formula gives,
+    in every column."""
+    for d in (384, 2048, 20480):
+        x, _, w = draw(4, d, d, None)
+        x[:3] *= 1e25
+        x[:3, 7] = 2e25
+        w[7] = 1e15
+        h, q = torch.empty_like(x), torch.full((4, d), 77, dtype=torch.int8, device="cuda")
+        s = torch.zeros(4, device="cuda")
+        B.spice_residual_rmsnorm(x, w, 1e-6, q, s, h=h)
+        torch.cuda.synchronize()
+        assert torch.isnan(s[:3]).all() and (q[:3] == 0).all() and float(s[3]) > 0 and int(q[3].abs().max()) == 127
+        v = x.double()
+        e = v * w.double() / (v.square().mean(1, keepdim=True) + 1e-6).sqrt()
+        assert ((h.double() - e).abs() <= (2.0 ** -8 + R_RTOL) * e.abs()).all()
