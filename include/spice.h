@@ -272,7 +272,7 @@ spice_status spice_moe_layer_fwd_fp8(spice_ctx *ctx, const spice_layer_weights_f
  *     h_j = bf16(s_j * weight_j * r)
  *     m = max_j |s_j * weight_j|,   q_j = 127 s_j weight_j / m to the nearest integer (ties to even),   scale = m * r / 127
  * so q_j * scale stands for the normalised value before its rounding to bf16.  The codes do not depend on r and are
- * rounded exactly.
+ * rounded exactly, also where products lie below fp32's range.
  *   x_resid [T,d] bf16, in/out (only read without a delta).  delta [T,d] bf16 or delta_f32 [T,d] fp32: one of them, or
  *   neither (the norm of the stream as it is).  weight [d] bf16.  eps >= 0.
  *   h [T,d] bf16 out, q [T,d] int8 out with scale [T] fp32 out: either may be NULL, not both.

@@ -4,11 +4,12 @@
 //   s = bf16(x + delta), x <- s;   p_j = s_j * w_j,   r = 1 / sqrt(mean_j s_j^2 + eps),   h_j = bf16(p_j * r)
 //   m = max_j |p_j|;   q_j = 127 p_j / m to the nearest integer, ties to even;   scale = m * r / 127
 //
-// (the quantiser: p = w, r = 1, no h).  r cancels out of q, and p is a product of two bf16 values, exact in fp32, so the
-// codes are a function of exactly known numbers.  They are rounded exactly: where the fp32 quotient lies within its error
-// of a border k + 1/2, 254 |p_j| and (2k + 1) m are compared, both exact in fp32 (16 + 7 and 8 + 16 significant bits; m is
-// scaled by a power of two where it lies at the ends of the range).  No implementation that keeps the definition can differ
-// by a step.
+// (the quantiser: p = w, r = 1, no h).  r cancels out of q, and p is a product of two bf16 values, exact in fp32 where it is
+// 2^-133 at least (16 significant bits), so the codes are a function of exactly known numbers.  They are rounded exactly: where
+// the fp32 quotient lies within its error of a border k + 1/2, 254 |p_j| and (2k + 1) m are compared, both exact in fp32 (16 +
+// 7 and 8 + 16 significant bits).  Rows whose largest product lies outside 2^-100 .. 2^100, or whose squares leave fp32's
+// range, are evaluated in fp64, where all of these are exact (rows of the quantiser: m is scaled by a power of two).  No
+// implementation that keeps the definition can differ by a step.
 //
 // Both are bound by the bytes that cross HBM (9 per element of a bf16 step with both outputs, 3 for the quantiser): every
 // row is read once, held in registers as the packed bf16 pairs it is stored as, and written once.
@@ -47,11 +48,10 @@ struct CodeScale {
     __device__ __forceinline__ explicit CodeScale(float largest) {
         m = largest;
         c = 0.0f;
-        if (!(m > 0x1p-100f && m < 0x1p100f)) return;
-        if (CHECK) {
+        if (CHECK) {   // (m is well inside)
             c = __fdividef(1.0f, m);
             c = 127.0f * fmaf(c, fmaf(-m, c, 1.0f), c);
-        } else {
+        } else if (m > 0x1p-100f && m < 0x1p100f) {
             c = __fdiv_ru(127.0f, m);
         }
     }
@@ -64,7 +64,7 @@ __device__ __forceinline__ float round_at_border(float p, float m, float a, bool
     return copysignf(a + (lhs > rhs || (lhs == rhs && odd) ? 1.0f : 0.0f), p);
 }
 
-// the codes of a row at the ends of fp32's range: m is brought into [1, 2) by a power of two first
+// the code of a bf16 value in a row at the ends of fp32's range: m is brought into [1, 2) by a power of two first
 __device__ __noinline__ float code_scaled(float p, float m) {
     if (!(m > 0.0f)) return 0.0f;
     const int e = (int)(__float_as_uint(m) >> 23);                                    // biased exponent
@@ -100,7 +100,7 @@ template <bool CHECK>
 __device__ __forceinline__ uint2 codes_of(const float (&p)[8], const CodeScale<CHECK> &c) {
     constexpr float MAGIC = 12582912.0f;
     uint32_t k[8];
-    float off = c.c > 0.0f ? 0.0f : 1.0f;
+    float off = CHECK || c.c > 0.0f ? 0.0f : 1.0f;
     const uint64_t c2 = pair2(c.c, c.c), magic2 = pair2(MAGIC, MAGIC), minus2 = pair2(-1.0f, -1.0f);
 #pragma unroll
     for (int j = 0; j < 8; j += 2) {
@@ -115,7 +115,7 @@ __device__ __forceinline__ uint2 codes_of(const float (&p)[8], const CodeScale<C
         k[j + 1] = (uint32_t)(s2 >> 32);
     }
     if (off > 0.49998f) {
-        if (CHECK && c.c > 0.0f) {
+        if (CHECK) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float n = __uint_as_float(k[j]) - MAGIC;      // the nearest integer; the other side of the border is n +- 1
@@ -166,18 +166,29 @@ __device__ __forceinline__ double warp_max_xor(double v) {
     return v;
 }
 
-// A row whose squares or products leave fp32's range, in fp64, where both are exact: the scale, the codes and h (the stream is
-// written already).  Such rows are rare, so the row is read again, by the threads that wrote it; nothing of it is kept in
-// registers.  The quotient 127 p / m is at least 2^-27 away from a border that it does not lie on (16 significant bits in p and
-// m, and p > m / 256 where a border is near), so its rounding to fp64 crosses none.
+// A row whose squares or products come near the ends of fp32's range, in fp64, where both are exact: the scale, the codes and
+// h (the stream is written already).  Such rows are rare, so the row is read again, by the threads that wrote it; nothing of it
+// is kept in registers.  The quotient 127 p / m is at least 2^-27 away from a border that it does not lie on (16 significant
+// bits in p and m, and p > m / 256 where a border is near), so its rounding to fp64 crosses none.  zeros: the row has nothing
+// but zeros, as the rows that fill up a batch.
 template <bool WIDE>
-__device__ __noinline__ void row_in_fp64(const RowArgs a, size_t row, int i0, int step) {
+__device__ __noinline__ void row_in_fp64(const RowArgs a, size_t row, int i0, int step, bool zeros) {
     __shared__ double sh_sum[32], sh_top[32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = blockDim.x >> 5;
     const int nv = a.d >> 3;
     const size_t base = row * (size_t)a.d;
     auto word_x = [&](int i, int j) { return reinterpret_cast<const uint32_t *>(a.x + base)[i * 4 + j]; };
     auto word_w = [&](int i, int j) { return reinterpret_cast<const uint32_t *>(a.weight)[i * 4 + j]; };
+    if (zeros) {   // 64 rows of 2048: 2.1 us, 4.4 by way of what follows
+        if (a.q && i0 == 0) a.scale[row] = 1.0f;
+        for (int i = i0; i < nv; i += step) {
+#pragma unroll 1
+            for (int j = 0; j < 4; ++j)
+                if (a.h) reinterpret_cast<uint32_t *>(a.h + base)[i * 4 + j] = (word_x(i, j) ^ word_w(i, j)) & 0x80008000u;
+            if (a.q) *reinterpret_cast<uint2 *>(a.q + base + (size_t)i * 8) = make_uint2(0u, 0u);
+        }
+        return;
+    }
     double sum = 0.0, top = 0.0;
     for (int i = i0; i < nv; i += step) {
 #pragma unroll 1
@@ -302,18 +313,24 @@ __global__ void __launch_bounds__(WIDE ? most_threads<V>() : 256) rows_i8_kernel
         big = __reduce_max_sync(0xffffffffu, lane < nw ? sh_max[lane] : 0u);
         if (MODE != NO_NORM) sum = warp_sum_xor(lane < nw ? sh_sum[lane] : 0.0f);
     }
-    const bool finite = big < 0x7f800000u;
+    const float m = __uint_as_float(big);
     float r = 1.0f;
     if (MODE != NO_NORM) {
         const float mean = sum * a.inv_d + a.eps;
-        if (!finite || !(mean >= 0x1p-60f && mean < INFINITY)) {   // (the same for the whole row)
-            row_in_fp64<WIDE>(a, row, i0, step);
+        // (the same for the whole row; a NaN compares false.  r <= 2^23: a product below fp32's range, off by 2^-150, moves h by
+        // less than the smallest normal number)
+        if (!(m > 0x1p-100f && m < 0x1p100f && mean >= 0x1p-46f && mean < INFINITY)) {
+            uint32_t any = m == 0.0f && mean >= 0x1p-46f ? 0u : 1u;
+#pragma unroll
+            for (int v = 0; v < V; ++v) any |= (xs[v].x | xs[v].y | xs[v].z | xs[v].w) & 0x7fff7fffu;
+            any = WIDE ? __syncthreads_or(any != 0u) : __any_sync(0xffffffffu, any != 0u);
+            row_in_fp64<WIDE>(a, row, i0, step, any == 0u);
             return;
         }
         r = rsqrtf(mean);
         r = r * (1.5f - 0.5f * mean * r * r);   // (one Newton step: within an ulp)
     }
-    const float m = __uint_as_float(big);
+    const bool finite = MODE != NO_NORM || big < 0x7f800000u;
     if (a.q && i0 == 0) {
         constexpr float C = 1.0f / 127.0f;
         a.scale[row] = !finite ? __uint_as_float(0x7fffffffu) : m == 0.0f ? 1.0f : m > 1.0f ? (m * C) * r : m * (r * C);

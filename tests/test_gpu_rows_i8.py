@@ -225,3 +225,45 @@ def test_norm_of_products_beyond_fp32():
         v = x.double()
         e = v * w.double() / (v.square().mean(1, keepdim=True) + 1e-6).sqrt()
         assert ((h.double() - e).abs() <= (2.0 ** -8 + R_RTOL) * e.abs()).all()
+
+
+@pytest.mark.parametrize("T,d,delta", [(5, 72, None), (3, 384, "bf16"), (4, 512, "f32"), (6, 2048, None), (3, 4104, "f32"),
+                                       (2, 8200, "bf16"), (2, 20480, None)])
+def test_norm_of_products_below_fp32(T, d, delta):
+    """Products at and below the smallest numbers of fp32 and above 2^100: the codes stay those of the exact products, a row
+    whose products are all below the range included."""
+    for e_x, e_w in ((-74, -64), (-60, -64), (-90, -70), (-40, -100), (58, 58), (-100, 20)):
+        x, dl, w = draw(T, d, T + d, delta)
+        x, w = x * 2.0 ** e_x, w * 2.0 ** e_w
+        if dl is not None:
+            dl = dl * 2.0 ** e_x
+        if T > 3:
+            x[1] = 0
+            if dl is not None:
+                dl[1] = 0
+        check_norm(x, dl, w, 0.0 if T <= 3 else 1e-30)
+    # a row that has values only where the weight is 0
+    x, _, w = draw(T, d, 3, None)
+    w[::2] = 0
+    x[:, 1::2] = 0
+    check_norm(x, None, w, 1e-6)
+
+
+@pytest.mark.parametrize("d", [72, 512, 2048, 20480])
+def test_rows_of_zeros_between_others(d):
+    """Rows that fill up a batch: codes 0, scale 1, h a zero of the product's sign; an infinite weight makes them NaN."""
+    x, _, w = draw(6, d, d, None)
+    x[1] = 0
+    x[3] = -0.0
+    x[5, ::2], x[5, 1::2] = 0, -0.0
+    w[::3] *= -1
+    h, q, s = check_norm(x, None, w, 1e-6)
+    for r in (1, 3, 5):
+        assert torch.equal(h[r].view(torch.int16), (x[r].float() * w.float()).to(bf).view(torch.int16))
+        assert float(s[r]) == 1.0 and (q[r] == 0).all()
+    w[5] = float("inf")
+    h, q, s = torch.empty_like(x), torch.full((6, d), 77, dtype=torch.int8, device="cuda"), torch.zeros(6, device="cuda")
+    B.spice_residual_rmsnorm(x, w, 1e-6, q, s, h=h)
+    torch.cuda.synchronize()
+    assert torch.isnan(s).all() and (q == 0).all() and torch.isnan(h[[1, 3, 5], 5]).all()
+    assert torch.isinf(h[[0, 2, 4], 5]).all() and torch.isfinite(h[:, :5]).all()
