@@ -376,13 +376,17 @@ spice_status launch_rows(const RowArgs &a, size_t rows, cudaStream_t st) {
     // (reductions, the row's scale) is spread over more of it, as long as enough warps stay resident.
     // 16 rows of 2048: norm 1.7 / 1.8 / 2.3 us with 1 / 2 / 4; 4096 rows of 2048: norm 14.5 / 13.5 / 14.8 us; 40960 rows of
     // 3584: quantiser 111 / 90 / 67 us; 333 rows of 2816: 2.46 / 2.46 / 2.55.
-    const int want = rows < 1024 ? 1 : MODE == NO_NORM ? 4 : 2;
+    const bool many = rows >= 1024;
     if (nv <= 32) narrow(integral_constant<int, 1>{});
     else if (nv <= 64) narrow(integral_constant<int, 2>{});
-    else if (want <= 1 && nv <= 1024) wide(integral_constant<int, 1>{});
-    else if (want <= 2 && nv <= 2048) wide(integral_constant<int, 2>{});
-    else if (nv <= 2048) wide(integral_constant<int, 4>{});
-    else wide(integral_constant<int, 8>{});
+    else if (!many && nv <= 1024) wide(integral_constant<int, 1>{});
+    else if (nv > 2048) wide(integral_constant<int, 8>{});
+    else if constexpr (MODE == NO_NORM) {
+        if (many) wide(integral_constant<int, 4>{});
+        else wide(integral_constant<int, 2>{});
+    } else {
+        wide(integral_constant<int, 2>{});
+    }
     return ok ? SPICE_OK : SPICE_ERR_CUDA;
 }
 

@@ -267,3 +267,9 @@ def test_rows_of_zeros_between_others(d):
     torch.cuda.synchronize()
     assert torch.isnan(s).all() and (q == 0).all() and torch.isnan(h[[1, 3, 5], 5]).all()
     assert torch.isinf(h[[0, 2, 4], 5]).all() and torch.isfinite(h[:, :5]).all()
+
+
+@pytest.mark.parametrize("rows,cols", [(1100, 520), (1030, 2816), (1024, 8200), (1024, 16384), (3, 12296), (1050, 18000)])
+def test_quantise_many_rows_and_wide_ones(rows, cols):
+    """As above at 1024 rows and more, where a thread holds four vectors of a block's row, and at two vectors of one."""
+    test_quantise_rows(rows, cols)
