@@ -173,3 +173,31 @@ def test_empty_batches_and_refusals_on_tensors():
         B.spice_swiglu_i8(xq, xs, wq[:15], ws[:15], y[:, :7])
     with pytest.raises(B.SpiceError):
         B.spice_swiglu_i8(xq, xs, wq, ws, y)
+
+
+# Shapes that the choice of kernel (148 SMs) sends where the ones above do not go: more tiles than CTA pairs (second
+# accumulator, ring and barriers carried from tile to tile; 17 and more token tiles: several groups, the last one partial),
+# three and four pairs to a tile, token tiles of 128 columns, whole lines of a long reduction per warp.
+MORE_SHAPES = [(2600, 2056, 1040), (4100, 2824, 272), (5000, 3592, 144), (257, 3584, 8208), (513, 264, 8208), (1100, 520, 6160),
+               (130, 3584, 20480), (128, 3584, 20480), (1, 4096, 11008), (12, 264, 11008), (16, 4096, 11008)]
+
+
+@pytest.mark.parametrize("T,n,k", MORE_SHAPES)
+@pytest.mark.parametrize("out", ["bf16", "f32", "add"])
+def test_product_of_more_tiles_and_longer_sums(T, n, k, out):
+    check(T, n, k, out)
+
+
+@pytest.mark.parametrize("T,inter,k", [(2600, 1032, 1040), (4500, 2824, 144), (513, 264, 8208), (513, 520, 12304), (128, 1792, 20480),
+                                       (1, 4096, 5504), (5, 1032, 11008), (12, 72, 11008)])
+def test_swiglu_of_more_tiles_and_longer_sums(T, inter, k):
+    check_swiglu(T, inter, k)
+
+
+def test_results_of_a_prompt_do_not_depend_on_the_batch():
+    """Rows of 4200 tokens through the persistent kernel are the bits of smaller calls."""
+    xq, xs = codes(4200, 528, 31)
+    wq, ws = codes(2056, 528, 32)
+    whole = run(xq, xs, wq, ws, "f32")
+    for a, b in ((0, 1), (700, 1300), (2500, 2530), (4090, 4200)):
+        assert torch.equal(run(xq[a:b].contiguous(), xs[a:b].contiguous(), wq, ws, "f32"), whole[a:b])
