@@ -379,8 +379,10 @@ spice_status spice_launch_count(const spice_ctx *ctx, int64_t *launches /* host 
  * run on (default 2^22 polls).  A wait that gives up ends its thread block early: the call's outputs are then
  * undefined, SPICE_ERR_TIMEOUT is recorded in the status word, nothing stays in flight, and the next call on the
  * ctx starts clean (dependency counters are reset by the kernel that gave up; the status word stays set until
- * spice_get_device_status reads it). */
-enum { SPICE_OPT_PATH = 0, SPICE_OPT_SPIN_LIMIT = 1, SPICE_OPT_TC_WAIT_LIMIT = 2 };
+ * spice_get_device_status reads it).  SPICE_OPT_I8_WAIT_LIMIT: the same for the pipeline waits of spice_gemm_i8 and
+ * spice_swiglu_i8, which have no ctx: ctx is NULL, the limit holds for the calls that the process makes from then on (0:
+ * every wait gives up at once), and SPICE_ERR_TIMEOUT goes to the call's own device_status. */
+enum { SPICE_OPT_PATH = 0, SPICE_OPT_SPIN_LIMIT = 1, SPICE_OPT_TC_WAIT_LIMIT = 2, SPICE_OPT_I8_WAIT_LIMIT = 3 };
 spice_status spice_set_option(spice_ctx *ctx, int32_t option, int64_t value);
 
 /* Text for a status code (static storage, never NULL). */

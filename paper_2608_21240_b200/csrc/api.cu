@@ -313,6 +313,11 @@ spice_status spice_get_device_status(spice_ctx *ctx, int32_t *code) {
 }
 
 spice_status spice_set_option(spice_ctx *ctx, int32_t option, int64_t value) {
+    if (option == SPICE_OPT_I8_WAIT_LIMIT) {   // (of calls that have no context)
+        if (ctx || value < 0 || value > (1ll << 30)) return SPICE_ERR_INVALID_ARG;
+        set_gemm_i8_wait_limit((uint32_t)value);
+        return SPICE_OK;
+    }
     if (!ctx) return SPICE_ERR_INVALID_ARG;
     switch (option) {
         case SPICE_OPT_PATH:

@@ -34,6 +34,7 @@ struct GemmI8Args {
     int32_t T, n, k;        // n: columns of y
     int32_t out;            // SPICE_OUT_*
     int32_t *status;        // optional
+    uint32_t wait_limit;    // polls after which a wait inside a kernel gives up
     // few tokens
     int32_t split, stages, cols;   // CTAs (pairs) along the reduction; ring stages, token columns of a tile (multiple of 16)
     // many tokens
@@ -230,16 +231,17 @@ __global__ void __launch_bounds__(SK_THREADS) gemm_i8_skinny_kernel(const __grid
     if (warp == 0 && lane == 0) {
         int it = min(stages, n_it);
         for (; it < n_it; ++it) {
-            if (!mbar_wait(smem_u32(&sh.empty[it % stages]), ((it / stages) & 1) ^ 1, abort_flag)) break;
+            if (!mbar_wait(smem_u32(&sh.empty[it % stages]), ((it / stages) & 1) ^ 1, abort_flag, g.wait_limit)) break;
             load_stage(it);
         }
         // every stage that was armed has landed before the ring is reused or the CTA ends
-        for (int j = it > stages ? it - stages : 0; j < it; ++j) mbar_drain(smem_u32(&sh.full[j % stages]), (j / stages) & 1);
+        for (int j = it > stages ? it - stages : 0; j < it; ++j)
+            if (!mbar_drain(smem_u32(&sh.full[j % stages]), (j / stages) & 1)) *abort_flag = 1;
     } else if (warp == 1 && lane == 0) {
         const uint32_t idesc = make_idesc_i8(128, cols);
         for (int it = 0; it < n_it; ++it) {
             const int s = it % stages;
-            if (!mbar_wait(smem_u32(&sh.full[s]), (it / stages) & 1, abort_flag)) break;
+            if (!mbar_wait(smem_u32(&sh.full[s]), (it / stages) & 1, abort_flag, g.wait_limit)) break;
             tc_fence_after();
             const uint32_t w0 = smem_u32(ring + s * stage_bytes);
             const uint64_t dw = make_desc(w0), dx = make_desc(w0 + SK_W_BYTES);
@@ -248,7 +250,8 @@ __global__ void __launch_bounds__(SK_THREADS) gemm_i8_skinny_kernel(const __grid
             tc_commit(smem_u32(&sh.empty[s]));
         }
         tc_commit(smem_u32(&sh.done));
-        mbar_drain(smem_u32(&sh.done), 0);   // (one thread polls, the others wait in hardware: pollers slow the two that work)
+        // (one thread polls, the others wait in hardware: pollers slow the two that work)
+        if (!mbar_drain(smem_u32(&sh.done), 0)) *abort_flag = 1;
     }
     __syncwarp();
     if (threadIdx.x >= 128) {   // the scales arrive while the products run
@@ -473,7 +476,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
                 const int w_row = SWIGLU ? (rank ? g.n : 0) + nt * 128 : nt * PR_TILE + (int)rank * 128;
                 for (int kb = 0; kb < kblocks; ++kb, ++it) {
                     const int s = it % PR_STAGES;
-                    if (!mbar_wait(smem_u32(&sh.empty[s]), ((it / PR_STAGES) & 1) ^ 1, abort_flag)) { ok = false; break; }
+                    if (!mbar_wait(smem_u32(&sh.empty[s]), ((it / PR_STAGES) & 1) ^ 1, abort_flag, g.wait_limit)) { ok = false; break; }
                     const uint32_t full = map_to_cta(smem_u32(&sh.full[s]), leader);
                     const uint32_t dst = smem_u32(ring + s * PR_STAGE_BYTES);
                     if (rank == 0) mbar_expect_tx(smem_u32(&sh.full[s]), 2 * PR_STAGE_BYTES);
@@ -482,9 +485,12 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
                 }
             }
             // a CTA ends when the stages it filled have been read by the MMAs: nothing of it is in flight then, neither a
-            // copy nor a release of a stage (also after an abort, within the limit)
+            // copy nor a release of a stage (also after an abort, within the limit: copies have long landed by then)
             for (uint32_t j = (it > PR_STAGES ? it - PR_STAGES : 0); j < it; ++j)
-                mbar_drain(smem_u32(&sh.empty[j % PR_STAGES]), (j / PR_STAGES) & 1);
+                if (!mbar_drain(smem_u32(&sh.empty[j % PR_STAGES]), (j / PR_STAGES) & 1)) {
+                    *abort_flag = 1;
+                    break;
+                }
         }
     } else if (warp == 1) {
         if (rank == 0 && lane == 0) {
@@ -493,12 +499,12 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
             bool ok = true;
             for (int tile = pair; tile < n_tiles && ok; tile += pairs, ++tcount) {
                 const int buf = tcount & 1;
-                if (!mbar_wait(smem_u32(&sh.tmem_empty[buf]), ((tcount >> 1) & 1) ^ 1, abort_flag)) break;
+                if (!mbar_wait(smem_u32(&sh.tmem_empty[buf]), ((tcount >> 1) & 1) ^ 1, abort_flag, g.wait_limit)) break;
                 tc_fence_after();
                 const uint32_t d_tmem = tmem_base + buf * PR_TILE;
                 for (int kb = 0; kb < kblocks; ++kb, ++it) {
                     const int s = it % PR_STAGES;
-                    if (!mbar_wait(smem_u32(&sh.full[s]), (it / PR_STAGES) & 1, abort_flag)) { ok = false; break; }
+                    if (!mbar_wait(smem_u32(&sh.full[s]), (it / PR_STAGES) & 1, abort_flag, g.wait_limit)) { ok = false; break; }
                     tc_fence_after();
                     const uint32_t a0 = smem_u32(ring + s * PR_STAGE_BYTES);
                     const uint64_t da = make_desc(a0), db = make_desc(a0 + PR_HALF_BYTES);
@@ -509,7 +515,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
                 if (ok) tc_commit_pair(smem_u32(&sh.tmem_full[buf]), pair_mask);
             }
             tc_commit_pair_local(smem_u32(&sh.mma_drain));
-            mbar_drain(smem_u32(&sh.mma_drain), 0);
+            if (!mbar_drain(smem_u32(&sh.mma_drain), 0)) *abort_flag = 1;
         }
     } else if (!SPLIT) {
         // ---------------- epilogue: warp w reads TMEM lanes 32*(w%4) .. +31 = rows of this CTA's half of the tile; the two
@@ -530,7 +536,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
             const int wc = threadIdx.x - 64, wcol = col0 + (SWIGLU ? wc & 127 : wc);
             sh.ws[buf][wc] = wcol < g.n ? g.ws[wcol + (SWIGLU && wc >= 128 ? g.n : 0)] : 0.0f;
             // (one thread polls, the others wait in hardware: pollers slow the two threads that feed the tensor cores)
-            if (threadIdx.x == 64 && !gave_up && !mbar_wait(smem_u32(&sh.tmem_full[buf]), (tcount >> 1) & 1, abort_flag)) sh.gave_up = 1;
+            if (threadIdx.x == 64 && !gave_up && !mbar_wait(smem_u32(&sh.tmem_full[buf]), (tcount >> 1) & 1, abort_flag, g.wait_limit)) sh.gave_up = 1;
             asm volatile("bar.sync 1, 256;" ::: "memory");
             gave_up = *(volatile int *)&sh.gave_up != 0;
             if (gave_up) continue;
@@ -552,7 +558,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
         pair_tile(g, pair, mt, nt);
         const int wcol = nt * (SWIGLU ? 128 : PR_TILE) + (SWIGLU ? wc & 127 : wc);
         sh.ws[0][wc] = wcol < g.n ? g.ws[wcol + (SWIGLU && wc >= 128 ? g.n : 0)] : 0.0f;
-        if (threadIdx.x == 64) mbar_wait(smem_u32(&sh.tmem_full[0]), 0, abort_flag);
+        if (threadIdx.x == 64) mbar_wait(smem_u32(&sh.tmem_full[0]), 0, abort_flag, g.wait_limit);
         asm volatile("bar.sync 1, 256;" ::: "memory");
         tc_fence_after();
         int32_t *sums = reinterpret_cast<int32_t *>(ring) + q * 32 + lane;
@@ -601,6 +607,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
 
 // ------------------------------------------------------------------------------------------------ host side
 constexpr int PR_MAX_SPLIT = 4;
+std::atomic<uint32_t> wait_limit{WAIT_LIMIT};   // (SPICE_OPT_I8_WAIT_LIMIT)
 
 // What a device is asked once: dynamic shared memory limits are raised, and how many clusters of c CTAs run at the same time
 // when an SM holds one CTA (a cluster stays inside a group of SMs; clusters beyond that wait for a whole round).
@@ -767,10 +774,13 @@ spice_status call_gemm_i8(const int8_t *x_q, const float *x_scale, const int8_t 
     g.k = k;
     g.out = out;
     g.status = device_status;
+    g.wait_limit = wait_limit.load(std::memory_order_relaxed);
     return launch_gemm_i8<SWIGLU>(g, x_q, w_q, static_cast<cudaStream_t>(stream));
 }
 
 }  // namespace
+
+void set_gemm_i8_wait_limit(uint32_t polls) { wait_limit.store(polls, std::memory_order_relaxed); }
 
 }  // namespace spice
 

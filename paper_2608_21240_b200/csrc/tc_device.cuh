@@ -46,10 +46,12 @@ __device__ __forceinline__ bool mbar_wait(uint32_t a, uint32_t parity, volatile 
     *abort_flag = 1;
     return false;
 }
-// wait for work already in flight (copies, MMAs) that must be over before the CTA ends: ignores the abort flag
-__device__ __forceinline__ void mbar_drain(uint32_t a, uint32_t parity) {
+// wait for work already in flight (copies, MMAs) that must be over before the CTA ends: ignores the abort flag; false when the
+// limit expired
+__device__ __forceinline__ bool mbar_drain(uint32_t a, uint32_t parity) {
     for (uint32_t i = 0; i < WAIT_LIMIT; ++i)
-        if (mbar_try(a, parity)) return;
+        if (mbar_try(a, parity)) return true;
+    return false;
 }
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t mbar) {
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"

@@ -201,3 +201,26 @@ def test_results_of_a_prompt_do_not_depend_on_the_batch():
     whole = run(xq, xs, wq, ws, "f32")
     for a, b in ((0, 1), (700, 1300), (2500, 2530), (4090, 4200)):
         assert torch.equal(run(xq[a:b].contiguous(), xs[a:b].contiguous(), wq, ws, "f32"), whole[a:b])
+
+
+@pytest.mark.parametrize("T,n,k", [(40, 272, 2048), (300, 272, 2048), (700, 2064, 528), (2600, 2064, 528), (513, 272, 8208)])
+def test_expired_waits_are_reported(T, n, k):
+    """With waits that give up at once, a call ends by itself, reports it, and writes nothing behind its rows; the next call is
+    as always.  (Few tokens with a split reduction, pairs, pairs that share tiles.)"""
+    xq, xs = codes(T, k, 1)
+    wq, ws = codes(n, k, 2)
+    st = torch.zeros(2, dtype=torch.int32, device="cuda")
+    y = torch.full((T + 2, n), 3.0, dtype=f32, device="cuda")
+    act = torch.full((T + 2, n // 2), 3.0, dtype=bf, device="cuda")
+    torch.cuda.synchronize()
+    B.spice_set_option(None, B.OPT_I8_WAIT_LIMIT, 0)
+    try:
+        B.spice_gemm_i8(xq, xs, wq, ws, y[:T], device_status=st[:1])
+        B.spice_swiglu_i8(xq, xs, wq, ws, act[:T], device_status=st[1:])
+        torch.cuda.synchronize()
+    finally:
+        B.spice_set_option(None, B.OPT_I8_WAIT_LIMIT, 1 << 22)
+    assert st.tolist() == [6, 6]                     # SPICE_ERR_TIMEOUT
+    assert (y[T:] == 3).all() and (act[T:] == 3).all()
+    e = exact(xq, xs, wq, ws)
+    assert ((run(xq, xs, wq, ws, "f32").to(f64) - e).abs() <= 3 * HALF * e.abs() * (1 + 1e-6)).all()

@@ -1,5 +1,7 @@
 """Host-side checks of the steps next to the layer (residual norm, 8-bit integer rows and products, routing by scores): every
 refusal answers without a device and launches nothing; a call without rows is fine."""
+import ctypes as C
+
 import pytest
 import torch
 
@@ -130,3 +132,12 @@ def test_calls_go_to_the_tensors_device_and_its_stream(monkeypatch):
     assert log == [("call", (7, 4242))]
     with pytest.raises(B.SpiceError, match="spice_swiglu_i8: invalid argument"):
         B._call_on(0, "spice_swiglu_i8", None, 7)
+
+
+def test_wait_limit_of_the_products_is_set_without_a_context():
+    assert B.lib().spice_set_option(None, B.OPT_I8_WAIT_LIMIT, C.c_int64(1 << 22)) == OK
+    for value in (-1, (1 << 30) + 1):
+        assert B.lib().spice_set_option(None, B.OPT_I8_WAIT_LIMIT, C.c_int64(value)) == INVALID
+    assert B.lib().spice_set_option(None, B.OPT_TC_WAIT_LIMIT, C.c_int64(5)) == INVALID
+    with pytest.raises(B.SpiceError):
+        B.spice_set_option(None, B.OPT_PATH, 0)
