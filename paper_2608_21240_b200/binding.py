@@ -266,11 +266,12 @@ GROUP_MAX, GROUP_TOP2 = 0, 1
 OUT_BF16, OUT_F32, OUT_F32_ADD = 0, 1, 2
 
 
-def _addr(what: str, t: Optional[torch.Tensor], dtype, shape, dev: int) -> Optional[int]:
-    """Address of a tensor of this type and shape on CUDA device `dev` (or in pinned host memory); None for None."""
+def _addr(what: str, t: Optional[torch.Tensor], dtype, shape, dev: int, pinned: bool = True) -> Optional[int]:
+    """Address of a tensor of this type and shape on CUDA device `dev` (or, with `pinned`, in pinned host memory); None for
+    None."""
     if t is None:
         return None
-    if t.dtype is dtype and t.shape == shape and t.is_contiguous() and (t.get_device() == dev or t.is_pinned()):
+    if t.dtype is dtype and t.shape == shape and t.is_contiguous() and (t.get_device() == dev or (pinned and t.is_pinned())):
         return t.data_ptr()
     raise SpiceError(f"{what}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on cuda:{dev}, got {t.dtype} "
                      f"{tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ', not contiguous'}")
@@ -334,7 +335,8 @@ def spice_quantize_i8_rows(w, q, scale, stream=None) -> None:
 
 def spice_gemm_i8(x_q, x_scale, w_q, w_scale, y, accumulate=False, device_status=None, stream=None) -> None:
     """x_q [T,k] int8, x_scale [T] fp32, w_q [n,k] int8, w_scale [n] fp32 -> y [T,n] bf16 or fp32; accumulate: y fp32 is
-    added to.  device_status: zeroed int32 tensor of one element that receives an expired wait."""
+    added to.  x_q and w_q live on the device (the kernels' bulk copies read them).  device_status: zeroed int32 tensor of one
+    element that receives an expired wait."""
     f = "spice_gemm_i8"
     T, k, dev = _rows_of(f, x_q)
     n = min(w_q.shape[0], 0x7fffffff) if w_q.dim() else 0   # (its shape is checked with its address)
@@ -342,14 +344,14 @@ def spice_gemm_i8(x_q, x_scale, w_q, w_scale, y, accumulate=False, device_status
     out = (OUT_F32_ADD if accumulate else OUT_F32) if y.dtype == f32 else OUT_BF16
     if accumulate and out == OUT_BF16:
         raise SpiceError(f"{f}: only an fp32 y is added to")
-    _call_on(dev, f, stream, _addr(f, x_q, i8, (T, k), dev), _addr(f, x_scale, f32, (T,), dev), _addr(f, w_q, i8, (n, k), dev),
-             _addr(f, w_scale, f32, (n,), dev), T, n, k, out, _addr(f, y, torch.bfloat16 if out == OUT_BF16 else f32, (T, n), dev),
-             _addr(f, device_status, torch.int32, (1,), dev))
+    _call_on(dev, f, stream, _addr(f, x_q, i8, (T, k), dev), _addr(f, x_scale, f32, (T,), dev),
+             _addr(f, w_q, i8, (n, k), dev, False), _addr(f, w_scale, f32, (n,), dev), T, n, k, out,
+             _addr(f, y, torch.bfloat16 if out == OUT_BF16 else f32, (T, n), dev), _addr(f, device_status, torch.int32, (1,), dev))
 
 
 def spice_swiglu_i8(x_q, x_scale, w_gate_up_q, w_scale, act, device_status=None, stream=None) -> None:
     """x_q [T,k] int8, x_scale [T] fp32, w_gate_up_q [2 inter,k] int8 (gate rows, then up rows), w_scale [2 inter] fp32 ->
-    act [T,inter] bf16."""
+    act [T,inter] bf16.  x_q and w_gate_up_q live on the device."""
     f = "spice_swiglu_i8"
     T, k, dev = _rows_of(f, x_q)
     n2 = min(w_gate_up_q.shape[0], 0x7ffffffe) if w_gate_up_q.dim() else 0
@@ -357,7 +359,7 @@ def spice_swiglu_i8(x_q, x_scale, w_gate_up_q, w_scale, act, device_status=None,
         raise SpiceError(f"{f}: w_gate_up_q has an odd number of rows")
     i8, f32 = torch.int8, torch.float32
     _call_on(dev, f, stream, _addr(f, x_q, i8, (T, k), dev), _addr(f, x_scale, f32, (T,), dev),
-             _addr(f, w_gate_up_q, i8, (n2, k), dev), _addr(f, w_scale, f32, (n2,), dev), T, n2 // 2, k,
+             _addr(f, w_gate_up_q, i8, (n2, k), dev, False), _addr(f, w_scale, f32, (n2,), dev), T, n2 // 2, k,
              _addr(f, act, torch.bfloat16, (T, n2 // 2), dev), _addr(f, device_status, torch.int32, (1,), dev))
 
 

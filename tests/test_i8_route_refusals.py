@@ -141,3 +141,45 @@ def test_wait_limit_of_the_products_is_set_without_a_context():
     assert B.lib().spice_set_option(None, B.OPT_TC_WAIT_LIMIT, C.c_int64(5)) == INVALID
     with pytest.raises(B.SpiceError):
         B.spice_set_option(None, B.OPT_PATH, 0)
+
+
+class Stand:
+    """What the binding asks of a tensor."""
+
+    def __init__(self, dtype, shape, dev):
+        self.dtype, self.shape, self.dev = dtype, torch.Size(shape), dev
+        self.is_cuda, self.device = dev >= 0, f"cuda:{dev}" if dev >= 0 else "cpu"
+
+    def get_device(self):
+        return self.dev
+
+    def is_pinned(self):
+        return self.dev < 0
+
+    def dim(self):
+        return len(self.shape)
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return P
+
+
+def test_operands_of_the_bulk_copies_are_not_taken_from_host_memory(monkeypatch):
+    """Pinned host memory may take a product's results and hold its scales; the codes are read by bulk copies and have to be
+    on the device."""
+    calls = []
+    monkeypatch.setattr(B, "_call_on", lambda dev, name, stream, *args: calls.append(name))
+    i8, f32, bf = torch.int8, torch.float32, torch.bfloat16
+    xq, wq = Stand(i8, (4, 64), 0), Stand(i8, (16, 64), 0)
+    xs, ws = Stand(f32, (4,), -1), Stand(f32, (16,), -1)
+    B.spice_gemm_i8(xq, xs, wq, ws, Stand(bf, (4, 16), -1))
+    B.spice_swiglu_i8(xq, xs, wq, ws, Stand(bf, (4, 8), -1))
+    assert calls == ["spice_gemm_i8", "spice_swiglu_i8"]
+    for x, w in ((Stand(i8, (4, 64), -1), wq), (xq, Stand(i8, (16, 64), -1))):
+        with pytest.raises(B.SpiceError):
+            B.spice_gemm_i8(x, xs, w, ws, Stand(bf, (4, 16), 0))
+        with pytest.raises(B.SpiceError):
+            B.spice_swiglu_i8(x, xs, w, ws, Stand(bf, (4, 8), 0))
+    assert len(calls) == 2
