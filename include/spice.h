@@ -264,6 +264,11 @@ spice_status spice_moe_layer_fwd_fp8(spice_ctx *ctx, const spice_layer_weights_f
  * Used together: spice_residual_rmsnorm -> h, (q, scale);  spice_route_topk(h) -> logits;  spice_route_scored -> idx, gate
  * for spice_classify_misses and spice_grouped_expert_ffn;  spice_swiglu_i8(q) -> act;  spice_quantize_i8_rows(act);
  * spice_gemm_i8 -> y fp32 (SPICE_OUT_F32_ADD: into the sum of the routed experts), the next norm's delta_f32.
+ * The 8-bit shared expert adds S(h) once, which is the whole layer only where no entry is LOWCONF: a dense FFN, every expert
+ * resident, or tau = 0 (all misses recovered exactly).  A layer with low-confidence misses needs S(h) once more for each of
+ * them: spice_lore_surrogate, which evaluates S(h) from the bf16 weights, then takes the place of the three 8-bit calls (both
+ * together would count S(h) twice).  spice_moe_layer_fwd and spice_moe_layer_fwd_fp8 route by themselves and take no idx and
+ * gate: a layer that is routed by spice_route_scored runs through the separate calls.
  * A call's kernel may be set up while the kernel before it in the stream drains; it touches no memory before that one is
  * complete, so the caller sees ordinary stream order.  Outputs may not overlap inputs unless a call says so. */
 

@@ -455,7 +455,9 @@ def quantize_shared_i8(w: "LayerWeights") -> SharedExpertI8:
 
 def shared_expert_i8(w: SharedExpertI8, x_q, x_scale, y, accumulate=False, device_status=None, stream=None) -> torch.Tensor:
     """y (bf16 or fp32, or added to fp32) = the SwiGLU FFN of the 8-bit rows that spice_residual_rmsnorm wrote: three calls
-    (gate/up products with the activation, the activations' 8-bit rows, the down product) and the buffers between them."""
+    (gate/up products with the activation, the activations' 8-bit rows, the down product) and the buffers between them.
+    S(h) once: a layer in which entries are LOWCONF needs it once more for each of them and takes spice_lore_surrogate (bf16
+    weights) instead."""
     T, dev = x_q.shape[0], x_q.device
     with torch.cuda.stream(stream):
         act = torch.empty(T, w.q_down.shape[1], dtype=torch.bfloat16, device=dev)

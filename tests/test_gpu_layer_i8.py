@@ -211,3 +211,55 @@ def test_the_first_calls_of_a_process_may_be_captured():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", FIRST], cwd=root, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and "captured" in r.stdout, r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("T", [1, 7, 300])
+@pytest.mark.parametrize("tau", [0.0, 0.5])
+def test_layers_with_and_without_low_confidence_misses(tau, T):
+    """The layer's formula, routed by scores: y = (1 + sum of the LOWCONF gates) S(h) + sum over HIT of g E(h) + sum over LOWCONF
+    of g B A h.  Without such misses S(h) is the shared expert in 8-bit integers, with them the call for the surrogate."""
+    wl = W.make_layer("tiny", T, variant=73)
+    s = wl.shape
+    L = B.SpiceLayer(cfg_of(s, tau=tau), T)
+    w = upload(wl)
+    g = torch.Generator(device="cuda").manual_seed(T)
+    rnd = lambda *shape: torch.randn(*shape, device="cuda", generator=g)  # noqa: E731
+    x, weight, bias = rnd(T, s.d).bfloat16(), (1 + 0.1 * rnd(s.d)).bfloat16(), 0.05 * rnd(s.n_experts)
+    conf = torch.from_numpy(wl.conf).cuda()
+    e = lambda *shape, t=torch.float32: torch.empty(*shape, dtype=t, device="cuda")  # noqa: E731
+    h, q, sc = e(T, s.d, t=torch.bfloat16), e(T, s.d, t=torch.int8), e(T)
+    B.spice_residual_rmsnorm(x, weight, 1e-6, q, sc, h=h)
+    _, _, logits = L.route_topk(h, w.w_router, want_logits=True)
+    idx, gate = e(T, s.top_k, t=torch.int32), e(T, s.top_k)
+    B.spice_route_scored(logits, idx, gate, bias=bias, score=B.SCORE_SIGMOID, n_groups=4, top_groups=2, scale=2.5)
+    cls, slot, counts, _ = L.classify_misses(idx, gate, w.slot_of_expert, conf)
+    y = torch.zeros(T, s.d, device="cuda")
+    L.grouped_expert_ffn(w, h, idx, gate, cls, slot, y)
+    if tau == 0:
+        B.shared_expert_i8(B.quantize_shared_i8(w), q, sc, y, accumulate=True)
+    else:
+        L.lore_surrogate(w, h, idx, gate, cls, y)
+    torch.cuda.synchronize()
+    low = cls == B.LOWCONF
+    assert int(counts[2]) == int(low.sum()) and (int(low.sum()) > 0 if tau > 0 and T > 1 else tau > 0 or not low.any())
+    h64, g64 = h.to(f64), gate.to(f64)
+    if tau == 0:
+        p = x.to(f64) * weight.to(f64)
+        r = 1 / (x.to(f64).square().mean(1, keepdim=True) + 1e-6).sqrt()
+        a = silu_acts(codes64(p) * r, codes64(w.shared_w_gate_up.to(f64)))
+        shared = codes64(a.bfloat16().to(f64)) @ codes64(w.shared_w_down.to(f64)).T
+    else:
+        shared = silu_ffn(h64, w.shared_w_gate_up.to(f64), w.shared_w_down.to(f64))
+    ref = shared * (1 + (g64 * low).sum(1, keepdim=True))
+    for t in range(T):
+        for k in range(s.top_k):
+            ex = int(idx[t, k])
+            if low[t, k]:
+                ref[t] += g64[t, k] * (w.lore_B[ex].to(f64) @ (w.lore_A[ex].to(f64) @ h64[t]))
+            elif cls[t, k] == B.HIT:
+                sl = int(slot[t, k])
+                ref[t] += g64[t, k] * silu_ffn(h64[t:t + 1], w.slot_w_gate_up[sl].to(f64), w.slot_w_down[sl].to(f64))[0]
+    err, bound = y_close(y.cpu().numpy(), ref.cpu().numpy())
+    assert err <= bound, (err, bound)
+    assert L.device_status() == 0
+    L.close()
