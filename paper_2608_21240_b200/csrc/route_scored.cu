@@ -16,8 +16,9 @@
 // that of the logits nothing is rounded and the first answer stands.
 //
 // One warp per token.  Keys live in registers; a round of the selection is one warp-wide maximum of the keys and one minimum of
-// the places that hold it (NaN marks a key that is out of the race: it is no maximum and equals nothing).  With groups, the keys pass through shared memory and only those of
-// the groups that stay are read back.  Bytes are few (4 N per token): the bound is the issue of instructions.
+// the places that hold it (NaN marks a key that is out of the race: it is no maximum and equals nothing).  With groups, the keys
+// pass through shared memory and only those of the groups that stay are read back.  Bytes are few (4 N per token, 1.4 us for
+// 8192 x 256, which takes 12.9 us with a bias and groups): the time goes into the issue of some 1000 instructions per warp.
 #include <cfloat>
 
 #include "entry.cuh"
@@ -75,8 +76,11 @@ __device__ __forceinline__ void warp_best64(unsigned long long &key, int &e) {
     }
 }
 
-// What the groups' values are made of, for the n_groups groups of `size` keys in shared memory: lane g gets group g's, and in
-// `terms` the magnitudes of the keys that it is made of (a sum of two may be far smaller than they are).
+// the first of the lanes that share group g when the groups are weighed
+__device__ __forceinline__ int first_lane(const RouteArgs &a, int g) { return (g << a.lanes_log2) & 31; }
+
+// What the groups' values are made of, for the n_groups groups of `size` keys in shared memory: lane g gets group g's value,
+// lane first_lane(g), in `terms`, the magnitudes of the keys that it is made of (a sum of two may be far smaller than they are).
 template <typename F>
 __device__ __forceinline__ F group_value(const RouteArgs &a, const F *keys, int size, int lane, F &terms) {
     // `width` lanes share a group: each looks at every width-th member, then they merge
@@ -98,8 +102,8 @@ __device__ __forceinline__ F group_value(const RouteArgs &a, const F *keys, int 
     const bool both = a.pair && b1 > -(F)INFINITY;
     F value = both ? b0 + b1 : b0;
     if (both && value == -(F)INFINITY) value = -(F)FLT_MAX;   // two keys at the low end of fp32: not a group without an expert
-    terms = __shfl_sync(FULL, both ? fabs(b0) + fabs(b1) : fabs(b0), (lane << a.lanes_log2) & 31);
-    return __shfl_sync(FULL, value, (lane << a.lanes_log2) & 31);
+    terms = both ? fabs(b0) + fabs(b1) : fabs(b0);
+    return __shfl_sync(FULL, value, first_lane(a, lane));
 }
 
 // Rank of lane's key among those of lanes 0..n-1 (equal keys: the smaller `tag` first).
@@ -264,10 +268,12 @@ __global__ void __launch_bounds__(WARPS * 32) route_scored_kernel(const RouteArg
         // A group's value is off by at most `off`: a score of each of its keys (tol / 2), the rounding of each key and that of
         // their sum (2^-24 of the keys' magnitudes each).  The choice stands where no group that does not stay can be worth as
         // much as one that does.
-        const float off = fminf(tol + 2.4e-7f * terms, 3e38f);
-        const float out = by_score ? warp_max(left + off) : none();                                             // (none: NaN)
-        const float in = -warp_max((open >> lane) & 1u ? off - mine : none());
-        const bool call = out > -INFINITY && !(in > out);   // warp-uniform
+        bool call = false;   // warp-uniform
+        if (by_score && a.top_groups < G) {
+            const float off = fminf(tol + 2.4e-7f * __shfl_sync(FULL, terms, first_lane(a, lane)), 3e38f);
+            const float out = warp_max(left + off), in = -warp_max((open >> lane) & 1u ? off - mine : none());
+            call = out > -INFINITY && !(in > out);
+        }
         if (call) open = slow_groups(a, l, shd, size, lane);
         if (call || (a.pair && !a.bias)) {
             // the winners' keys again: the doubles lay over them; or, without a bias, the logits in the place of the scores
