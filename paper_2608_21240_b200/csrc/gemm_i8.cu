@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(NW * 32) gemm_i8_few_kernel(const int8_t *x, c
     const int nv = g.k >> 4, pieces = (nv + 3) >> 2;
     // DEAL: pieces are dealt out one at a time, so that every warp has the same share of a short reduction; of a long one a
     // warp takes UN pieces side by side, whole lines of DRAM (dealt out / side by side, us: 8 tokens 2048 x 2816 3.0 / 4.0, 4096
-    // x 11008 12.1 / 11.7, one token 4096 x 11008 11.9 / 11.2; 16 tokens 4096 x 11008 12.2 / 13.3, the one case where it loses).
+    // x 11008 12.1 / 11.7, one token 4096 x 11008 11.9 / 11.2; 16 tokens 4096 x 11008 12.2 / 13.3: there it loses).
     int32_t acc[NT][4];
 #pragma unroll
     for (int i = 0; i < NT; ++i)
