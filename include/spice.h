@@ -335,6 +335,83 @@ spice_status spice_route_scored(const float *logits, const float *bias, int32_t 
                                 int32_t score, int32_t n_groups, int32_t top_groups, int32_t group_score, int32_t norm_topk,
                                 float scale, int32_t *idx, float *gate, void *stream);
 
+/* ---- Experts of one's own: tokens sorted by expert and back, products in E4M3 with a scale for each block of 128 ----
+ * The calls above group the (token, expert) entries inside a context.  These hand the grouping to the caller: its experts
+ * (any computation on rows that lie together) run between spice_sort_tokens and spice_combine_tokens, both have their gradients, and
+ * the library's own products on such rows take 8-bit floating-point weights at any batch size.  As above: no ctx, no
+ * workspace, the GPU is the calling thread's current device, every call can be captured into a graph, stream order.
+ * Used together: spice_quantize_e4m3_blocks(h) -> q, scale;  spice_sort_tokens(idx, q, scale) -> offset, pos, rows;
+ * spice_swiglu_e4m3_blocks(rows, offset) -> activations;  spice_gemm_e4m3_blocks -> rows of outputs;  spice_combine_tokens(pos,
+ * gate) -> y.  idx is the routing's idx over all experts, or the slot array of spice_classify_misses over the slot pool: what is
+ * not resident there (-1) is dropped, and comes from elsewhere as before. */
+
+/* Stable sort of the entries i = t * top_k + k by expert.  An entry with idx outside 0 .. n_experts-1 is dropped.
+ *   idx [T, top_k] int32
+ *   -> offset [n_experts + 1] int32: the kept entries of expert e take the places offset[e] .. offset[e+1]-1, in the order of i
+ *      pos [T, top_k] int32: place of the entry, -1 when dropped;  entry [T * top_k] int32: i of each place, -1 behind the kept ones
+ *   x [T, row_bytes], optional: rows of any type (row_bytes a multiple of 16) -> rows [T * top_k, row_bytes]: rows[p] = x[entry[p] / top_k];
+ *   x_scale [T, scale_cols] fp32, optional with x -> rows_scale [T * top_k, scale_cols], likewise.
+ *   Rows behind the kept ones are left as they are.  The gradient of x is spice_combine_tokens of the rows' gradients without gates.
+ *   The same expert may stand twice in a token's row: both entries are kept.  (T = 0 writes nothing, offset neither.)
+ *   n_experts up to 1024, top_k up to 32, T * top_k up to 2^28 (SPICE_ERR_UNSUPPORTED_SHAPE); x and rows 16-byte aligned. */
+spice_status spice_sort_tokens(const int32_t *idx, int32_t T, int32_t top_k, int32_t n_experts, int32_t *offset, int32_t *pos,
+                               int32_t *entry, const void *x, int32_t row_bytes, void *rows, const float *x_scale,
+                               int32_t scale_cols, float *rows_scale, void *stream);
+
+/* Rows back to their tokens:  y[t,:] = sum_k gate[t,k] * rows[pos[t,k],:], in fp32 and in the order of k; dropped entries (and
+ * places outside 0 .. n_rows-1) do not count, and the rows nobody points to are not read.
+ *   rows [n_rows, d] of rows_type (SPICE_OUT_BF16 or SPICE_OUT_F32), pos [T, top_k], gate [T, top_k] fp32 or NULL (weights of 1);
+ *   out: the type of y [T, d]: SPICE_OUT_BF16, SPICE_OUT_F32 or SPICE_OUT_F32_ADD.
+ *   d a multiple of 8 up to 2^24, top_k up to 32, T * top_k up to 2^28; rows and y 16-byte aligned. */
+spice_status spice_combine_tokens(const void *rows, int32_t rows_type, int32_t n_rows, const int32_t *pos, const float *gate,
+                                  int32_t T, int32_t top_k, int32_t d, int32_t out, void *y, void *stream);
+
+/* Its gradient, from dy [T, d] of dy_type:
+ *   d_rows[pos[t,k],:] = gate[t,k] * dy[t,:]  (of rows_type; rows that nobody points to are left as they are),
+ *   d_gate[t,k] = sum_j dy[t,j] * rows[pos[t,k],j] fp32 (0 for a dropped entry).
+ *   d_rows or d_gate may be NULL (not wanted); rows may be NULL without d_gate.  pos as spice_sort_tokens writes it: two entries
+ *   with the same place would race.  Limits as above. */
+spice_status spice_combine_tokens_grad(const void *dy, int32_t dy_type, const void *rows, int32_t rows_type, int32_t n_rows,
+                                       const int32_t *pos, const float *gate, int32_t T, int32_t top_k, int32_t d, void *d_rows,
+                                       float *d_gate, void *stream);
+
+/* E4M3 codes (the format above) of bf16 matrices with a scale for each block of block_rows x 128 values, block_rows = 1 (rows of
+ * activations) or 128 (weights); blocks at the ends are smaller.  With m = the block's largest magnitude:
+ *     q = the E4M3 value nearest to 448 w / m (ties to the even code, rounded exactly),   scale = m / 448
+ *   A block of zeros has codes 0 and scale 1; one with a value that is not finite has codes 0 and scale NaN.
+ *   w, q [count, rows, cols];  scale [count, ceil(rows / block_rows), ceil(cols / 128)] fp32.  cols a multiple of 8 up to 2^24, rows
+ *   and count below 2^31, at most 2^31 blocks of 128 x 128 and 2^35 of 1 x 128; w 16-byte, q 8-byte aligned. */
+spice_status spice_quantize_e4m3_blocks(const spice_bf16 *w, int64_t count, int64_t rows, int32_t cols, int32_t block_rows,
+                                        uint8_t *q, float *scale, void *stream);
+
+/* Product of such rows with such weights, dense or by groups of rows:
+ *     y[t,j] = sum_b x_scale[t,b] w_scale[g][j/128,b] * ( sum over i in block b of x_q[t,i] w_q[g][j,i] ),   g the group of row t
+ * Blocks are summed on the tensor cores, scaled and added up in fp32.
+ *   x_q [T, k] uint8 with x_scale [T, ceil(k/128)] fp32;  w_q [n_groups, n, k] with w_scale [n_groups, ceil(n/128), ceil(k/128)].
+ *   Any scales are taken, not only those of the quantiser.
+ *   offset [n_groups + 1] int32, device: group g has the rows offset[g] .. offset[g+1]-1; rows of y outside of all groups are
+ *   left as they are.  NULL with n_groups = 1: all T rows.  A group whose offsets are not in order, or outside 0 .. T, counts as
+ *   empty, and SPICE_ERR_BAD_TABLE is reported.
+ *   out, y [T, n]: as in spice_gemm_i8.  device_status: optional device int32 which the caller has set to 0: raised to
+ *   SPICE_ERR_BAD_TABLE or SPICE_ERR_TIMEOUT (a bounded wait inside the kernel expired: the outputs are undefined then).
+ *   k a multiple of 16, n a multiple of 8; T, n, k up to 2^24, n_groups up to 1024, n_groups * n below 2^31
+ *   (SPICE_ERR_UNSUPPORTED_SHAPE).  x_q, w_q and y 16-byte aligned.  For a given T and n_groups a row's bits do not depend on
+ *   how the rows are spread over the groups. */
+spice_status spice_gemm_e4m3_blocks(const uint8_t *x_q, const float *x_scale, const uint8_t *w_q, const float *w_scale,
+                                    const int32_t *offset, int32_t n_groups, int32_t T, int32_t n, int32_t k, int32_t out, void *y,
+                                    int32_t *device_status, void *stream);
+
+/* The gate and up products of a SwiGLU FFN in the same arithmetic, with activations that are rows of blocks again:
+ *     g, u = rows j and inter + j of the product above,   a = g / (1 + exp(-g)) * u  (fp32, not rounded to bf16),
+ *     act_q, act_scale = codes and scales of a in blocks of 1 x 128 along j (scale = m / 448 within an ulp, codes of the fp32
+ *     quotient; a block below 2^-100 is taken for zeros)
+ *   w_gate_up_q [n_groups, 2 inter, k]: inter gate rows, then inter up rows;  w_scale [n_groups, 2 inter / 128, ceil(k/128)];
+ *   act_q [T, inter] uint8, act_scale [T, inter / 128] fp32 out.  inter a multiple of 128 (SPICE_ERR_UNSUPPORTED_SHAPE), so that
+ *   no block of weights has gate and up rows.  Everything else as above with n = inter. */
+spice_status spice_swiglu_e4m3_blocks(const uint8_t *x_q, const float *x_scale, const uint8_t *w_gate_up_q, const float *w_scale,
+                                      const int32_t *offset, int32_t n_groups, int32_t T, int32_t inter, int32_t k, uint8_t *act_q,
+                                      float *act_scale, int32_t *device_status, void *stream);
+
 /* The resident-expert FFN for callers that cannot allocate (the paper has no counterpart: this is
  * a packaging variant of spice_grouped_expert_ffn, not a step of the method).
  *
@@ -386,8 +463,10 @@ spice_status spice_launch_count(const spice_ctx *ctx, int64_t *launches /* host 
  * ctx starts clean (dependency counters are reset by the kernel that gave up; the status word stays set until
  * spice_get_device_status reads it).  SPICE_OPT_I8_WAIT_LIMIT: the same for the pipeline waits of spice_gemm_i8 and
  * spice_swiglu_i8, which have no ctx: ctx is NULL, the limit holds for the calls that the process makes from then on (0:
- * every wait gives up at once), and SPICE_ERR_TIMEOUT goes to the call's own device_status. */
-enum { SPICE_OPT_PATH = 0, SPICE_OPT_SPIN_LIMIT = 1, SPICE_OPT_TC_WAIT_LIMIT = 2, SPICE_OPT_I8_WAIT_LIMIT = 3 };
+ * every wait gives up at once), and SPICE_ERR_TIMEOUT goes to the call's own device_status.  SPICE_OPT_E4M3_WAIT_LIMIT: the
+ * same for spice_gemm_e4m3_blocks and spice_swiglu_e4m3_blocks. */
+enum { SPICE_OPT_PATH = 0, SPICE_OPT_SPIN_LIMIT = 1, SPICE_OPT_TC_WAIT_LIMIT = 2, SPICE_OPT_I8_WAIT_LIMIT = 3,
+       SPICE_OPT_E4M3_WAIT_LIMIT = 4 };
 spice_status spice_set_option(spice_ctx *ctx, int32_t option, int64_t value);
 
 /* Text for a status code (static storage, never NULL). */

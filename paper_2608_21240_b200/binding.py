@@ -71,6 +71,12 @@ def lib() -> C.CDLL:
                            ("spice_quantize_i8_rows", [ptr, i64, i32, ptr, ptr, ptr]),
                            ("spice_gemm_i8", [ptr, ptr, ptr, ptr, i32, i32, i32, i32, ptr, ptr, ptr]),
                            ("spice_swiglu_i8", [ptr, ptr, ptr, ptr, i32, i32, i32, ptr, ptr, ptr]),
+                           ("spice_sort_tokens", [ptr, i32, i32, i32, ptr, ptr, ptr, ptr, i32, ptr, ptr, i32, ptr, ptr]),
+                           ("spice_combine_tokens", [ptr, i32, i32, ptr, ptr, i32, i32, i32, i32, ptr, ptr]),
+                           ("spice_combine_tokens_grad", [ptr, i32, ptr, i32, i32, ptr, ptr, i32, i32, i32, ptr, ptr, ptr]),
+                           ("spice_quantize_e4m3_blocks", [ptr, i64, i64, i32, i32, ptr, ptr, ptr]),
+                           ("spice_gemm_e4m3_blocks", [ptr, ptr, ptr, ptr, ptr, i32, i32, i32, i32, i32, ptr, ptr, ptr]),
+                           ("spice_swiglu_e4m3_blocks", [ptr, ptr, ptr, ptr, ptr, i32, i32, i32, i32, ptr, ptr, ptr, ptr]),
                            ("spice_route_scored", [ptr, ptr, i32, i32, i32, i32, i32, i32, i32, i32, f32, ptr, ptr, ptr])):
             getattr(L, name).argtypes, getattr(L, name).restype = args, C.c_int
         L.spice_static_scratch_bytes.restype = C.c_size_t
@@ -126,7 +132,7 @@ def spice_launch_count(ctx) -> int:
     return n.value
 
 
-OPT_PATH, OPT_SPIN_LIMIT, OPT_TC_WAIT_LIMIT, OPT_I8_WAIT_LIMIT = 0, 1, 2, 3
+OPT_PATH, OPT_SPIN_LIMIT, OPT_TC_WAIT_LIMIT, OPT_I8_WAIT_LIMIT, OPT_E4M3_WAIT_LIMIT = 0, 1, 2, 3, 4
 
 
 def spice_set_option(ctx, option: int, value: int) -> None:
@@ -375,6 +381,120 @@ def spice_route_scored(logits, idx, gate, bias=None, score=SCORE_SOFTMAX, n_grou
              _addr(f, gate, f32, (T, K), dev))
 
 
+# ---- experts of one's own: tokens sorted by expert and back, products in E4M3 with a scale for each block of 128
+def spice_sort_tokens(idx, offset, pos, entry, x=None, rows=None, x_scale=None, rows_scale=None, stream=None) -> None:
+    """idx [T,K] int32 -> offset [n_experts + 1], pos [T,K], entry [T*K] int32; with x [T,d] (any type, rows of a multiple of 16
+    bytes) rows [T*K,d] of the same type, with x_scale [T,c] fp32 rows_scale [T*K,c]."""
+    f = "spice_sort_tokens"
+    T, K, dev = _rows_of(f, idx)
+    i32, f32 = torch.int32, torch.float32
+    if offset.dim() != 1 or offset.shape[0] < 2:
+        raise SpiceError(f"{f}: offset has an element for each expert and one more")
+    if (x is None) != (rows is None) or (x_scale is None) != (rows_scale is None) or (x is None and x_scale is not None):
+        raise SpiceError(f"{f}: x and rows, x_scale and rows_scale are given together, scales with rows")
+    d = row_bytes = cols = 0
+    if x is not None:
+        d = _rows_of(f, x)[1]
+        row_bytes = min(d * x.element_size(), 0x7fffffff)
+    if x_scale is not None:
+        cols = _rows_of(f, x_scale)[1]
+    _call_on(dev, f, stream, _addr(f, idx, i32, (T, K), dev), T, K, offset.shape[0] - 1, _addr(f, offset, i32, offset.shape, dev),
+             _addr(f, pos, i32, (T, K), dev), _addr(f, entry, i32, (T * K,), dev),
+             None if x is None else _addr(f, x, x.dtype, (T, d), dev), row_bytes,
+             None if x is None else _addr(f, rows, x.dtype, (T * K, d), dev), _addr(f, x_scale, f32, (T, cols), dev), cols,
+             _addr(f, rows_scale, f32, (T * K, cols), dev))
+
+
+def _row_type(what: str, t: torch.Tensor) -> int:
+    if t.dtype == torch.float32:
+        return OUT_F32
+    if t.dtype == torch.bfloat16:
+        return OUT_BF16
+    raise SpiceError(f"{what}: expected rows of bfloat16 or float32, got {t.dtype}")
+
+
+def spice_combine_tokens(rows, pos, y, gate=None, accumulate=False, stream=None) -> None:
+    """rows [R,d] bf16 or fp32, pos [T,K] int32, gate [T,K] fp32 or None -> y [T,d] bf16 or fp32; accumulate: y fp32 is added to."""
+    f = "spice_combine_tokens"
+    R, d, dev = _rows_of(f, rows)
+    T, K, _ = _rows_of(f, pos)
+    f32 = torch.float32
+    out = _row_type(f, y)
+    if accumulate and out == OUT_BF16:
+        raise SpiceError(f"{f}: only an fp32 y is added to")
+    _call_on(dev, f, stream, _addr(f, rows, rows.dtype, (R, d), dev), _row_type(f, rows), R, _addr(f, pos, torch.int32, (T, K), dev),
+             _addr(f, gate, f32, (T, K), dev), T, K, d, OUT_F32_ADD if accumulate else out, _addr(f, y, y.dtype, (T, d), dev))
+
+
+def spice_combine_tokens_grad(dy, rows, pos, gate=None, d_rows=None, d_gate=None, stream=None) -> None:
+    """dy [T,d] bf16 or fp32, rows [R,d] bf16 or fp32 (None without d_gate), pos [T,K] int32, gate [T,K] fp32 or None -> d_rows
+    [R,d] bf16 or fp32 (the type of rows) and / or d_gate [T,K] fp32."""
+    f = "spice_combine_tokens_grad"
+    T, d, dev = _rows_of(f, dy)
+    K = _rows_of(f, pos)[1]
+    like = rows if rows is not None else d_rows
+    if like is None or (d_rows is None and d_gate is None) or (d_gate is not None and rows is None):
+        raise SpiceError(f"{f}: nothing is asked for, or d_gate without rows")
+    R = _rows_of(f, like)[0]
+    f32 = torch.float32
+    _call_on(dev, f, stream, _addr(f, dy, dy.dtype, (T, d), dev), _row_type(f, dy), _addr(f, rows, like.dtype, (R, d), dev),
+             _row_type(f, like), R, _addr(f, pos, torch.int32, (T, K), dev), _addr(f, gate, f32, (T, K), dev), T, K, d,
+             _addr(f, d_rows, like.dtype, (R, d), dev), _addr(f, d_gate, f32, (T, K), dev))
+
+
+def spice_quantize_e4m3_blocks(w, q, scale, block_rows=1, stream=None) -> None:
+    """w [..., rows, cols] bf16 -> q (uint8 E4M3 codes, same shape) and scale [..., ceil(rows / block_rows), ceil(cols / 128)] fp32;
+    block_rows 1 (activations) or 128 (weights)."""
+    f = "spice_quantize_e4m3_blocks"
+    if w.dim() < 2 or not w.is_cuda:
+        raise SpiceError(f"{f}: expected a CUDA tensor of matrices, got shape {tuple(w.shape)} on {w.device}")
+    if block_rows not in (1, 128):
+        raise SpiceError(f"{f}: blocks have 1 or 128 rows")
+    (rows, cols), dev = w.shape[-2:], w.get_device()
+    if cols < 1 or cols > 0x7fffffff:
+        raise SpiceError(f"{f}: unsupported row length {cols}")
+    lead = w.shape[:-2]
+    _call_on(dev, f, stream, _addr(f, w, torch.bfloat16, w.shape, dev), lead.numel(), rows, cols, block_rows,
+             _addr(f, q, torch.uint8, w.shape, dev),
+             _addr(f, scale, torch.float32, (*lead, -(-rows // block_rows), -(-cols // 128)), dev))
+
+
+def _block_operands(f, x_q, x_scale, w_q, w_scale, offset):
+    """What the two products check alike: (addresses of the operands and offsets, groups, T, rows of a weight matrix, k, device)."""
+    T, k, dev = _rows_of(f, x_q)
+    u8, f32, kb = torch.uint8, torch.float32, -(-k // 128)
+    lead = () if offset is None else (min(w_q.shape[0] if w_q.dim() else 0, 0x7fffffff),)
+    n = min(w_q.shape[len(lead)], 0x7ffffffe) if w_q.dim() > len(lead) else 0   # (its shape is checked with its address)
+    G = lead[0] if lead else 1
+    return ((_addr(f, x_q, u8, (T, k), dev, False), _addr(f, x_scale, f32, (T, kb), dev), _addr(f, w_q, u8, (*lead, n, k), dev, False),
+             _addr(f, w_scale, f32, (*lead, -(-n // 128), kb), dev), _addr(f, offset, torch.int32, (G + 1,), dev)), G, T, n, k, dev)
+
+
+def spice_gemm_e4m3_blocks(x_q, x_scale, w_q, w_scale, y, offset=None, accumulate=False, device_status=None, stream=None) -> None:
+    """x_q [T,k] uint8, x_scale [T,ceil(k/128)] fp32, w_q [n,k] uint8 with w_scale [ceil(n/128),ceil(k/128)], or with offset [G+1]
+    int32 w_q [G,n,k] and w_scale [G,...] -> y [T,n] bf16 or fp32; accumulate: y fp32 is added to.  x_q and w_q live on the device.
+    device_status: zeroed int32 tensor of one element that receives bad offsets and an expired wait."""
+    f = "spice_gemm_e4m3_blocks"
+    ptrs, G, T, n, k, dev = _block_operands(f, x_q, x_scale, w_q, w_scale, offset)
+    out = _row_type(f, y)
+    if accumulate and out == OUT_BF16:
+        raise SpiceError(f"{f}: only an fp32 y is added to")
+    _call_on(dev, f, stream, *ptrs, G, T, n, k, OUT_F32_ADD if accumulate else out, _addr(f, y, y.dtype, (T, n), dev),
+             _addr(f, device_status, torch.int32, (1,), dev))
+
+
+def spice_swiglu_e4m3_blocks(x_q, x_scale, w_gate_up_q, w_scale, act_q, act_scale, offset=None, device_status=None, stream=None) -> None:
+    """As spice_gemm_e4m3_blocks with w_gate_up_q [(G,) 2 inter, k] (gate rows, then up rows) -> act_q [T,inter] uint8 E4M3 codes with
+    act_scale [T, inter / 128] fp32."""
+    f = "spice_swiglu_e4m3_blocks"
+    ptrs, G, T, n2, k, dev = _block_operands(f, x_q, x_scale, w_gate_up_q, w_scale, offset)
+    if n2 % 256:
+        raise SpiceError(f"{f}: w_gate_up_q has {n2} rows, not two times a multiple of 128")
+    inter = n2 // 2
+    _call_on(dev, f, stream, *ptrs, G, T, inter, k, _addr(f, act_q, torch.uint8, (T, inter), dev),
+             _addr(f, act_scale, torch.float32, (T, inter // 128), dev), _addr(f, device_status, torch.int32, (1,), dev))
+
+
 # ------------------------------------------------------------------ convenience wrappers
 @dataclass
 class LayerWeights:
@@ -465,6 +585,46 @@ def shared_expert_i8(w: SharedExpertI8, x_q, x_scale, y, accumulate=False, devic
     spice_swiglu_i8(x_q, x_scale, w.q_gate_up, w.s_gate_up, act, device_status, stream)
     spice_quantize_i8_rows(act, q, s, stream)
     spice_gemm_i8(q, s, w.q_down, w.s_down, y, accumulate, device_status, stream)
+    return y
+
+
+@dataclass
+class ExpertsE4M3:
+    """Device tensors of SwiGLU experts in E4M3 with a scale for each block of 128 x 128."""
+    q_gate_up: torch.Tensor    # [G,2I,d] uint8
+    s_gate_up: torch.Tensor    # [G,2I/128,ceil(d/128)] fp32
+    q_down: torch.Tensor       # [G,d,I] uint8
+    s_down: torch.Tensor       # [G,ceil(d/128),I/128] fp32
+
+
+def quantize_experts_e4m3(w_gate_up: torch.Tensor, w_down: torch.Tensor) -> ExpertsE4M3:
+    """Experts [G,2I,d] and [G,d,I] bf16 (the slot pool of a LayerWeights) in E4M3: two calls of spice_quantize_e4m3_blocks."""
+    def qz(t):
+        q = torch.empty(t.shape, dtype=torch.uint8, device=t.device)
+        s = torch.empty(*t.shape[:-2], -(-t.shape[-2] // 128), -(-t.shape[-1] // 128), dtype=torch.float32, device=t.device)
+        spice_quantize_e4m3_blocks(t, q, s, block_rows=128)
+        return q, s
+    return ExpertsE4M3(*qz(w_gate_up), *qz(w_down))
+
+
+def routed_experts_e4m3(w: ExpertsE4M3, h, idx, gate, y, accumulate=False, device_status=None, stream=None) -> torch.Tensor:
+    """y (bf16 or fp32, or added to fp32) = sum_k gate[t,k] E_{idx[t,k]}(h[t]) over the entries with 0 <= idx < G, for any batch: five calls
+    (8-bit rows of h, sort, gate/up products with the activation, down products, weighted sum) and the buffers between them.
+    idx: the routing's idx, or the slot array of spice_classify_misses for the experts of a slot pool."""
+    (T, K), (G, d, inter), dev = idx.shape, w.q_down.shape, h.device
+    f32, i32, u8 = torch.float32, torch.int32, torch.uint8
+    with torch.cuda.stream(stream):
+        new = lambda *shape, dtype: torch.empty(*shape, dtype=dtype, device=dev)  # noqa: E731
+        q, s = new(T, d, dtype=u8), new(T, -(-d // 128), dtype=f32)
+        offset, pos, entry = new(G + 1, dtype=i32), new(T, K, dtype=i32), new(T * K, dtype=i32)
+        rows, rows_s = new(T * K, d, dtype=u8), new(T * K, -(-d // 128), dtype=f32)
+        act, act_s = new(T * K, inter, dtype=u8), new(T * K, inter // 128, dtype=f32)
+        down = new(T * K, d, dtype=torch.bfloat16)
+    spice_quantize_e4m3_blocks(h, q, s, 1, stream)
+    spice_sort_tokens(idx, offset, pos, entry, q, rows, s, rows_s, stream)
+    spice_swiglu_e4m3_blocks(rows, rows_s, w.q_gate_up, w.s_gate_up, act, act_s, offset, device_status, stream)
+    spice_gemm_e4m3_blocks(act, act_s, w.q_down, w.s_down, down, offset, False, device_status, stream)
+    spice_combine_tokens(down, pos, y, gate, accumulate, stream)
     return y
 
 

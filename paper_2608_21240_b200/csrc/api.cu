@@ -313,9 +313,10 @@ spice_status spice_get_device_status(spice_ctx *ctx, int32_t *code) {
 }
 
 spice_status spice_set_option(spice_ctx *ctx, int32_t option, int64_t value) {
-    if (option == SPICE_OPT_I8_WAIT_LIMIT) {   // (of calls that have no context)
+    if (option == SPICE_OPT_I8_WAIT_LIMIT || option == SPICE_OPT_E4M3_WAIT_LIMIT) {   // (of calls that have no context)
         if (ctx || value < 0 || value > (1ll << 30)) return SPICE_ERR_INVALID_ARG;
-        set_gemm_i8_wait_limit((uint32_t)value);
+        if (option == SPICE_OPT_I8_WAIT_LIMIT) set_gemm_i8_wait_limit((uint32_t)value);
+        else set_gemm_e4m3_wait_limit((uint32_t)value);
         return SPICE_OK;
     }
     if (!ctx) return SPICE_ERR_INVALID_ARG;

@@ -185,6 +185,7 @@ int launch_quantize_e4m3_rows(const __nv_bfloat16 *w, size_t rows, int cols, uin
 
 // polls after which a wait inside the products of 8-bit integers gives up (gemm_i8.cu)
 void set_gemm_i8_wait_limit(uint32_t polls);
+void set_gemm_e4m3_wait_limit(uint32_t polls);
 
 // ---- tensor-core path for large batches (tc_gemm.cu)
 // One m-tile of the grouped problem: rows [row0, row0+rows) of the gathered activation buffer, all of
