@@ -9,12 +9,10 @@
 //
 // Two kernels.  Few rows a group: every weight byte is used for few products and the call is bound by streaming the weights:
 // they go from global memory straight into the registers of warp-wide products.  Otherwise pairs of CTAs (cta_group::2) work on
-// tiles of 256 weight rows x up to 256 tokens, persistent.  The weights are the M operand, so that the tokens' side of a tile is as
-// wide as the group's rows need (a multiple of 32): groups are ragged, and a tile of 256 tokens would be padding for a third.
+// tiles of 256 tokens x 256 weight rows, persistent.
 #include <cuda_fp8.h>
 
 #include <algorithm>
-#include <mutex>
 
 #include "entry.cuh"
 #include "spice_internal.cuh"
@@ -40,6 +38,7 @@ struct GemmE4m3Args {
     int32_t *status;         // optional
     uint32_t wait_limit;     // polls after which a wait inside a kernel gives up
     int32_t n_tiles;         // tiles along n
+    int32_t sectors;         // rows of y begin on 32-byte boundaries
 };
 
 // (fast exponential and quotient: a few 2^-23 for |g| of some units)
@@ -65,20 +64,8 @@ __device__ __forceinline__ uint64_t pair2(float lo, float hi) {
     asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
     return r;
 }
-__device__ __forceinline__ uint64_t pair2(uint32_t lo, uint32_t hi) {
-    uint64_t r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
-    return r;
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
+__device__ __forceinline__ void add_scaled2(uint64_t &sum, uint32_t lo, uint32_t hi, uint64_t scale) {
+    asm("{\n\t.reg .b64 v;\n\tmov.b64 v, {%1, %2};\n\tfma.rn.f32x2 %0, v, %3, %0;\n\t}" : "+l"(sum) : "r"(lo), "r"(hi), "l"(scale));
 }
 __device__ __forceinline__ float low(uint64_t v) { return __uint_as_float((uint32_t)v); }
 __device__ __forceinline__ float high(uint64_t v) { return __uint_as_float((uint32_t)(v >> 32)); }
@@ -103,6 +90,16 @@ __device__ __forceinline__ float max_magnitude(float m, float a) {
     return r;
 }
 
+// 32 bytes; whole: they begin on a boundary of 32 bytes
+__device__ __forceinline__ void store_sector(void *to, const uint32_t (&v)[8], int32_t whole) {
+    if (whole) {
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                     ::"l"(to), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+    } else {
+        reinterpret_cast<uint4 *>(to)[0] = make_uint4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<uint4 *>(to)[1] = make_uint4(v[4], v[5], v[6], v[7]);
+    }
+}
 __device__ __forceinline__ void store1(const GemmE4m3Args &g, size_t at, float v) {
     if (g.out == SPICE_OUT_BF16) static_cast<__nv_bfloat16 *>(g.y)[at] = __float2bfloat16_rn(v);
     else if (g.out == SPICE_OUT_F32) static_cast<float *>(g.y)[at] = v;
@@ -303,76 +300,66 @@ __global__ void __launch_bounds__(FEW_WARPS * 32) gemm_e4m3_few_kernel(const uin
 }
 
 // ------------------------------------------------------------------------------------------------ more rows
-constexpr int PR_THREADS = 384, PR_STAGES = 6, PR_EPI_WARPS = 8;
-constexpr int PR_TILE = 256;                      // weight rows of a pair's tile (128 per CTA), and its most tokens
-constexpr int PR_W_BYTES = 128 * BK, PR_X_BYTES = 128 * BK, PR_STAGE_BYTES = PR_W_BYTES + PR_X_BYTES;
-constexpr int PR_BATCH = 4;                       // blocks of the reduction whose scales are staged at a time
+constexpr int PR_THREADS = 384, PR_EPI_WARPS = 8;
+constexpr uint32_t PR_STAGES = 6;
+constexpr int PR_TILE = 256;                      // tokens of a pair's tile (128 per CTA), and its accumulator columns
+constexpr int PR_HALF_BYTES = 128 * BK;           // a CTA's half of one operand
+constexpr int PR_STAGE_BYTES = 2 * PR_HALF_BYTES;
 constexpr int PR_GROUP_M = 16;                    // token tiles that share a sweep over the weight tiles
-constexpr int PR_PITCH = 80;                      // 64 B of a token's outputs + 16: 16-byte accesses do not collide
-constexpr int PR_F32_PITCH = 144;                 // the same for 128 B
-constexpr int PR_STG_WARP = 2048;                 // a warp's transposition buffers: 8 tokens x 32 columns, bf16 twice
-static_assert(2 * 8 * PR_PITCH <= PR_STG_WARP && 8 * PR_F32_PITCH <= PR_STG_WARP, "they fit");
 // The sums of a tile take 128 registers of each epilogue thread: the four warps that copy and multiply give theirs up.
-constexpr int PR_REGS_HELPERS = 40, PR_REGS_EPILOGUE = 232;
+constexpr int PR_REGS_HELPERS = 72, PR_REGS_EPILOGUE = 216;
 static_assert(PR_REGS_HELPERS + 2 * PR_REGS_EPILOGUE <= 3 * (65536 / PR_THREADS / 8 * 8), "what the block is launched with");
 
 struct PairShared {
-    alignas(16) float xs[2][PR_BATCH][PR_TILE];   // token scales (product: times the weights' scale); the buffer that is not in
-                                                  // use also takes the largest magnitudes of a token's columns (SwiGLU)
-    alignas(16) unsigned char stg[PR_EPI_WARPS * PR_STG_WARP];   // transposition buffers; SwiGLU: [256 tokens][64 codes]
-    float other[2][PR_TILE];                      // SwiGLU: the largest magnitudes of the other CTA's columns, which it writes here
+    float peak[2][128];                           // SwiGLU: largest magnitude of a token's columns, per half of them
     int32_t first[MAX_GROUPS + 1];                // tiles before each group
-    alignas(8) unsigned long long full[PR_STAGES], empty[PR_STAGES], tmem_full[2], tmem_empty[2], mma_drain, peer[2];
+    alignas(8) unsigned long long full[PR_STAGES], empty[PR_STAGES], tmem_full[2], tmem_empty[2], mma_drain[2];
     uint32_t tmem_base;
     int abort_flag;
 };
 constexpr size_t PR_SMEM_BYTES = sizeof(PairShared) + (size_t)PR_STAGES * PR_STAGE_BYTES + 1024;
 static_assert(PR_SMEM_BYTES <= 232448, "what a block can have");
-static_assert(PR_TILE * 64 <= PR_EPI_WARPS * PR_STG_WARP && 4 <= PR_BATCH, "codes and largest magnitudes fit");
 
 struct Tile {
-    int group, t0, cols, nt;   // first token, tokens, weight tile
+    int group, t0, rows, nt;   // first token, tokens, weight tile
 };
 
-// tokens of a tile as the products of a pair take them
-__device__ __forceinline__ int padded(int tokens) { return (tokens + 31) & ~31; }
-
 // Tiles are numbered group by group; within a group sweeps of up to PR_GROUP_M token tiles, the token tile fastest, so that
-// pairs working at the same time share both operands in L2.  A group's rows are spread evenly over as few token tiles as there
-// can be.  The group only moves forward.
+// pairs working at the same time share both operands in L2.  The group only moves forward.
 __device__ __forceinline__ Tile find_tile(const PairShared &sh, const GemmE4m3Args &g, int tile, int &group) {
     while (tile >= sh.first[group + 1]) ++group;
     const int begin = g.offset ? load_s32(g.offset + group) : 0, m = (g.offset ? load_s32(g.offset + group + 1) : g.T) - begin;
     const int in = tile - sh.first[group];
-    const int tt = (m + PR_TILE - 1) / PR_TILE, width = padded((m + tt - 1) / tt);
-    const int per_sweep = PR_GROUP_M * g.n_tiles;
-    const int sweep = in / per_sweep, mt0 = sweep * PR_GROUP_M, left = min(PR_GROUP_M, tt - mt0), r = in - sweep * per_sweep;
+    const int per_sweep = PR_GROUP_M * g.n_tiles, sweep = in / per_sweep, r = in - sweep * per_sweep;
+    const int mt0 = sweep * PR_GROUP_M, left = min(PR_GROUP_M, (m + PR_TILE - 1) / PR_TILE - mt0);
     const int mt = mt0 + r % left;
-    return Tile{group, begin + mt * width, min(width, m - mt * width), r / left};
+    return Tile{group, begin + mt * PR_TILE, min(PR_TILE, m - mt * PR_TILE), r / left};
 }
+// Rows of a CTA's half of the tile as they are copied.  Some always are: a copying thread that the products do not wait for
+// could fall two uses of a stage behind, and the parity of a barrier would no longer tell it which use is meant.
+__device__ __forceinline__ int copied(int rows, int rank) { return (min(max(rows - rank * 128, 1), 128) + 15) & ~15; }
 
 template <bool SWIGLU>
 __global__ void __launch_bounds__(PR_THREADS, 1)
-    gemm_e4m3_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x64,
-                          const __grid_constant__ CUtensorMap map_x32, const __grid_constant__ CUtensorMap map_x16, const GemmE4m3Args g) {
+    gemm_e4m3_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x128,
+                          const __grid_constant__ CUtensorMap map_x16, const GemmE4m3Args g) {
     extern __shared__ __align__(16) unsigned char smem_raw[];   // (aligned to 1024 by hand: the swizzled tiles)
     unsigned char *ring = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     PairShared &sh = *reinterpret_cast<PairShared *>(ring + PR_STAGES * PR_STAGE_BYTES);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = cluster_rank();
+    const int rank = (int)cluster_rank();
     volatile int *abort_flag = &sh.abort_flag;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < PR_STAGES; ++s) {
+        for (uint32_t s = 0; s < PR_STAGES; ++s) {
             mbar_init(smem_u32(&sh.full[s]), 1);    // used in the even CTA: both CTAs' copies report there
             mbar_init(smem_u32(&sh.empty[s]), 1);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(smem_u32(&sh.tmem_full[b]), 1);
             mbar_init(smem_u32(&sh.tmem_empty[b]), 2 * PR_EPI_WARPS);   // used in the even CTA: the epilogue warps of both
-            mbar_init(smem_u32(&sh.peer[b]), PR_EPI_WARPS);             // the other CTA's epilogue warps
+            mbar_init(smem_u32(&sh.mma_drain[b]), 1);
         }
-        mbar_init(smem_u32(&sh.mma_drain), 1);
         sh.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -415,254 +402,198 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
     const uint32_t tmem_base = sh.tmem_base;
     const int n_tiles = sh.first[g.G];
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-    const int row_blocks = ((SWIGLU ? 2 * g.n : g.n) + 127) / 128;
 
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PR_REGS_HELPERS));
-        if (warp == 0 && lane == 0) {
-            uint32_t it = 0;
-            bool ok = true;
+        if ((warp == 0 || warp == 3) && lane == 0) {
+            // one of the two brings the weights, the other the tokens: what a thread does for a block takes it some hundred cycles
+            const uint32_t empty0 = smem_u32(&sh.empty[0]), full0 = smem_u32(&sh.full[0]);
+            uint32_t s = 0, phase = 1, filled = 0, limit = g.wait_limit;
             int group = 0;
-            for (int tile = pair; tile < n_tiles && ok; tile += pairs) {
+            for (int tile = pair; tile < n_tiles && limit != 0; tile += pairs) {
                 const Tile t = find_tile(sh, g, tile, group);
-                const int half = padded(t.cols) / 2, x_row = t.t0 + (int)rank * half;
-                for (int kb = 0; kb < g.kb; ++kb, ++it) {
-                    const int s = it % PR_STAGES;
-                    if (!mbar_wait(smem_u32(&sh.empty[s]), ((it / PR_STAGES) & 1) ^ 1, abort_flag, g.wait_limit)) { ok = false; break; }
-                    const uint32_t full = map_to_cta(smem_u32(&sh.full[s]), 0);
-                    const uint32_t dst = smem_u32(ring + s * PR_STAGE_BYTES);
-                    if (rank == 0) mbar_expect_tx(smem_u32(&sh.full[s]), 2 * (PR_W_BYTES + half * BK));
-                    if (SWIGLU) tma_load_5d_pair(dst, &map_w, kb * BK, 0, 0, 2 * t.group, t.nt * 8 + (int)rank * 4, full);
-                    else tma_load_2d_pair(dst, &map_w, kb * BK, t.group * g.n + t.nt * PR_TILE + (int)rank * 128, full);
-                    uint32_t to = dst + PR_W_BYTES;
-                    int row = x_row;
-                    auto rows = [&](const CUtensorMap *map, int n) {
-                        tma_load_2d_pair(to, map, kb * BK, row, full);
-                        to += n * BK;
-                        row += n;
-                    };
-                    if (half & 128) rows(&map_x64, 64);
-                    if (half & (128 | 64)) rows(&map_x64, 64);
-                    if (half & 32) rows(&map_x32, 32);
-                    if (half & 16) rows(&map_x16, 16);
+                // (SwiGLU: the even CTA brings the gate rows, the odd one the up rows)
+                const int row = warp != 0 ? t.t0 + rank * 128 : SWIGLU ? (2 * t.group + rank) * g.n + t.nt * 128 : t.group * g.n + t.nt * PR_TILE + rank * 128;
+                const int x_rows = copied(t.rows, rank);
+                const uint32_t bytes = 2 * PR_HALF_BYTES + (x_rows + copied(t.rows, rank ^ 1)) * BK;
+                for (int k0 = 0; k0 < g.k; k0 += BK) {
+                    mbar_wait_quick(empty0 + s * 8, phase, abort_flag, limit);
+                    if (limit == 0) break;
+                    const uint32_t full = map_to_cta(full0 + s * 8, 0), dst = smem_u32(ring) + s * PR_STAGE_BYTES;
+                    if (warp == 0) {
+                        if (rank == 0) mbar_expect_tx(full0 + s * 8, bytes);
+                        tma_load_2d_pair(dst + PR_HALF_BYTES, &map_w, k0, row, full);
+                    } else if (x_rows == 128) {
+                        tma_load_2d_pair(dst, &map_x128, k0, row, full);
+                    } else {
+                        for (int done = 0; done < x_rows; done += 16) tma_load_2d_pair(dst + done * BK, &map_x16, k0, row + done, full);
+                    }
+                    filled = min(filled + 1, PR_STAGES);
+                    if (++s == PR_STAGES) {
+                        s = 0;
+                        phase ^= 1;
+                    }
                 }
             }
             // a CTA ends when the stages it filled have been read by the MMAs: nothing of it is in flight then, neither a
             // copy nor a release of a stage (also after an abort, within the limit: copies have long landed by then)
-            for (uint32_t j = (it > PR_STAGES ? it - PR_STAGES : 0); j < it; ++j)
-                if (!mbar_drain(smem_u32(&sh.empty[j % PR_STAGES]), (j / PR_STAGES) & 1)) {
+            for (uint32_t left = filled; left > 0; --left) {
+                const uint32_t back = s >= left ? 0u : 1u;   // the stage filled `left` blocks ago: in this round of the ring, or the one before
+                if (!mbar_drain(empty0 + (s + back * PR_STAGES - left) * 8, phase ^ 1 ^ back)) {
                     *abort_flag = 1;
                     break;
                 }
-        } else if (warp == 1 && rank == 0 && lane == 0) {
-            uint32_t it = 0;
-            bool ok = true;
-            int group = 0;
-            for (int tile = pair; tile < n_tiles && ok; tile += pairs) {
-                const Tile t = find_tile(sh, g, tile, group);
-                const uint32_t idesc = make_idesc_e4m3(256, padded(t.cols));
-                for (int kb = 0; kb < g.kb; ++kb, ++it) {
-                    const int s = it % PR_STAGES, buf = it & 1;
-                    if (!mbar_wait(smem_u32(&sh.tmem_empty[buf]), ((it >> 1) & 1) ^ 1, abort_flag, g.wait_limit)) { ok = false; break; }
-                    if (!mbar_wait(smem_u32(&sh.full[s]), (it / PR_STAGES) & 1, abort_flag, g.wait_limit)) { ok = false; break; }
-                    tc_fence_after();
-                    const uint32_t a0 = smem_u32(ring + s * PR_STAGE_BYTES);
-                    const uint64_t da = make_desc(a0), db = make_desc(a0 + PR_W_BYTES);
+            }
+        } else if ((warp == 1 || warp == 2) && rank == 0 && lane == 0) {
+            // Every other block of the reduction is issued by the other of these warps, into its own accumulator: issuing a block
+            // takes longer than its products do.
+            static_assert(PR_STAGES % 2 == 0, "a stage always belongs to the same warp");
+            constexpr uint32_t idesc = make_idesc_e4m3(256, PR_TILE);
+            const uint32_t buf = warp - 1, d_tmem = tmem_base + buf * PR_TILE;
+            const uint32_t tmem_empty = smem_u32(&sh.tmem_empty[buf]), tmem_full = smem_u32(&sh.tmem_full[buf]);
+            const uint32_t full0 = smem_u32(&sh.full[0]), empty0 = smem_u32(&sh.empty[0]);
+            const uint64_t desc0 = make_desc(smem_u32(ring));
+            uint32_t s = buf, phase = 0, tmem_phase = 1, limit = g.wait_limit;
+            // blocks of all this pair's tiles that are this warp's
+            const uint32_t total = (uint32_t)(n_tiles > pair ? (n_tiles - pair + pairs - 1) / pairs : 0) * (uint32_t)g.kb;
+            for (uint32_t left = (total + 1 - buf) / 2; left > 0; --left) {
+                mbar_wait_quick(tmem_empty, tmem_phase, abort_flag, limit);
+                mbar_wait_quick(full0 + s * 8, phase, abort_flag, limit);
+                if (limit == 0) break;
+                tc_fence_after();
+                const uint64_t da = desc0 + s * (PR_STAGE_BYTES >> 4), db = da + (PR_HALF_BYTES >> 4);
 #pragma unroll
-                    for (int k = 0; k < BK / 32; ++k) tc_mma_f8_pair(tmem_base + buf * PR_TILE, da + 2 * k, db + 2 * k, idesc, k ? 1u : 0u);
-                    tc_commit_pair(smem_u32(&sh.empty[s]), 3u);
-                    tc_commit_pair(smem_u32(&sh.tmem_full[buf]), 3u);
+                for (int k = 0; k < BK / 32; ++k) tc_mma_f8_pair(d_tmem, da + 2 * k, db + 2 * k, idesc, k ? 1u : 0u);
+                tc_commit_pair(empty0 + s * 8, 3u);
+                tc_commit_pair(tmem_full, 3u);
+                tmem_phase ^= 1;
+                s += 2;
+                if (s >= PR_STAGES) {
+                    s -= PR_STAGES;
+                    phase ^= 1;
                 }
             }
-            tc_commit_pair_local(smem_u32(&sh.mma_drain));
-            if (!mbar_drain(smem_u32(&sh.mma_drain), 0)) *abort_flag = 1;
+            tc_commit_pair_local(smem_u32(&sh.mma_drain[buf]));
+            if (!mbar_drain(smem_u32(&sh.mma_drain[buf]), 0)) *abort_flag = 1;
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(PR_REGS_EPILOGUE));
-        // ---------------- epilogue: warp w reads TMEM lanes 32*(w%4) .. +31 = weight rows of this CTA's half of the tile; the two
-        // warps of a quarter take half of the tokens each.  Sums are held in registers in the layout of warp-wide products: a
-        // thread has two neighbouring tokens of every eight, so that it needs a quarter of the tokens' scales.
-        const int q = warp & 3, h = warp >= 8 ? 1 : 0, e = threadIdx.x - 128;
-        const int r4 = lane >> 2, c2 = 2 * (lane & 3);
-        uint32_t it = 0, batch = 0, count = 0;   // blocks, batches of scales and tiles so far
+        // ---------------- epilogue: warp w reads TMEM lanes 32*(w%4) .. +31 = tokens of this CTA's half of the tile, a token per
+        // thread; the two warps of a quarter take 128 columns each (SwiGLU: 64 gate columns and their up columns), which are one
+        // block of weight rows: a thread's sums of a block all have the same scale.
+        const int q = warp & 3, h = warp >= 8 ? 1 : 0;
+        const int row_blocks = ((SWIGLU ? 2 * g.n : g.n) + 127) / 128;
+        const uint32_t full0 = smem_u32(&sh.tmem_full[0]), empty0 = map_to_cta(smem_u32(&sh.tmem_empty[0]), 0);
+        const uint32_t tm0 = tmem_base + ((uint32_t)(q * 32) << 16) + h * (SWIGLU ? 64 : 128);
+        uint32_t it = 0;
+        uint32_t limit = g.wait_limit;   // 0 after an expired wait: a warp only keeps the others' barriers
         int group = 0;
-        bool ok = true;   // after an expired wait a warp only keeps the others' barriers
-        for (int tile = pair; tile < n_tiles; tile += pairs, ++count) {
+        for (int tile = pair; tile < n_tiles; tile += pairs) {
             const Tile t = find_tile(sh, g, tile, group);
-            const int cols = padded(t.cols), mine = cols / 2, col0 = h * mine;
-            const int nb = SWIGLU ? t.nt : t.nt * 2 + (int)rank;    // block of weight rows
-            const float *ws = g.ws + ((size_t)t.group * row_blocks + min(nb, row_blocks - 1)) * g.kb;
-            const float *ws_up = SWIGLU ? ws + (size_t)(g.n / 128) * g.kb : ws;
-            const float *xs = g.xs + (size_t)(t.t0 + min(e, t.cols - 1)) * g.kb;
-            uint64_t acc[16][2][2];   // [eight tokens][16 rows][rows r4, r4 + 8]: two tokens
+            const int rows = t.rows - rank * 128 - q * 32;              // of this warp
+            const int row = t.t0 + rank * 128 + q * 32 + lane;          // of this thread
+            const int nb = SWIGLU ? t.nt : min(t.nt * 2 + h, row_blocks - 1);
+            const float *ws = g.ws + ((size_t)t.group * row_blocks + nb) * g.kb, *wu = ws + (size_t)(g.n / 128) * g.kb;
+            const float *xs = g.xs + (size_t)(lane < rows ? row : t.t0) * g.kb;
+            uint64_t acc[64];   // two columns each
 #pragma unroll
-            for (int i = 0; i < 16; ++i) acc[i][0][0] = acc[i][0][1] = acc[i][1][0] = acc[i][1][1] = 0;
-            float next[PR_BATCH], next_w[PR_BATCH];
-            auto fetch = [&](int kb0) {
+            for (int i = 0; i < 64; ++i) acc[i] = 0;
+            float x = load_f32(xs), w = load_f32(ws), u = SWIGLU ? load_f32(wu) : 0.0f;   // a block ahead
+#pragma unroll 1
+            for (int kb = 0; kb < g.kb; ++kb, ++it) {
+                const uint32_t buf = it & 1, tm = tm0 + buf * PR_TILE;
+                const float sw = x * w, su = SWIGLU ? x * u : sw;
+                const int ahead = min(kb + 1, g.kb - 1);
+                x = load_f32(xs + ahead);
+                w = load_f32(ws + ahead);
+                if (SWIGLU) u = load_f32(wu + ahead);
+                mbar_wait_quick(full0 + buf * 8, (it >> 1) & 1, abort_flag, limit);
+                tc_fence_after();
+                if (rows > 0) {
 #pragma unroll
-                for (int j = 0; j < PR_BATCH; ++j) {
-                    next[j] = kb0 + j < g.kb ? load_f32(xs + kb0 + j) : 0.0f;
-                    if (!SWIGLU) next_w[j] = kb0 + j < g.kb ? load_f32(ws + kb0 + j) : 0.0f;
-                }
-            };
-            fetch(0);
-            for (int kb0 = 0; kb0 < g.kb; kb0 += PR_BATCH, ++batch) {
-                float (*stage)[PR_TILE] = sh.xs[batch & 1];
-#pragma unroll
-                for (int j = 0; j < PR_BATCH; ++j) stage[j][e] = SWIGLU ? next[j] : next[j] * next_w[j];
-                fetch(kb0 + PR_BATCH);
-                // (a warp that writes a buffer again has seen this barrier after the batch before: everyone has read it)
-                asm volatile("bar.sync 1, 256;" ::: "memory");
-                const int last = min(PR_BATCH, g.kb - kb0);
-                for (int j = 0; j < last; ++j, ++it) {
-                    const int buf = it & 1;
-                    uint64_t wg = 0, wu = 0;
-                    if (SWIGLU) {
-                        const float a = load_f32(ws + kb0 + j), b = load_f32(ws_up + kb0 + j);
-                        wg = pair2(a, a);
-                        wu = pair2(b, b);
-                    }
-                    if (ok && lane == 0) ok = mbar_wait(smem_u32(&sh.tmem_full[buf]), (it >> 1) & 1, abort_flag, g.wait_limit);
-                    ok = __shfl_sync(0xffffffffu, ok, 0);
-                    if (!ok) continue;
-                    tc_fence_after();
-                    const uint32_t tm = tmem_base + buf * PR_TILE + col0 + ((uint32_t)(q * 32) << 16);
-#pragma unroll
-                    for (int ch = 0; ch < 4; ++ch) {
-                        if (ch * 32 >= mine) break;
-                        uint32_t v0[16], v1[16];
-                        tc_ld_fragments(tm + ch * 32, v0);
-                        tc_ld_fragments(tm + ch * 32 + (16u << 16), v1);
-                        uint64_t s[4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) s[i] = *reinterpret_cast<const uint64_t *>(&stage[j][(col0 + ch * 32 + i * 8 + c2) & (PR_TILE - 1)]);
+                    for (int ch = 0; ch < 8; ++ch) {
+                        uint32_t v[16];
+                        const int off = (SWIGLU && ch >= 4 ? 64 : 0) + ch * 16;
+                        tc_ld16(tm + off, v);
                         tc_wait_ld();
-                        if (ch * 32 + 32 >= mine) {   // the last columns are in registers: the buffer is free
+                        asm volatile("" : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]));
+                        if (ch == 7) {   // the last columns are in registers: the buffer is free
                             tc_fence_before();
-                            __syncwarp();
-                            if (lane == 0) mbar_arrive_cluster(map_to_cta(smem_u32(&sh.tmem_empty[buf]), 0));
+                            mbar_arrive_cluster_tmem(empty0 + buf * 8, lane);
                         }
+                        const float f = SWIGLU && ch >= 4 ? su : sw;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const uint64_t sg = SWIGLU ? mul2(s[i], wg) : s[i], su = SWIGLU ? mul2(s[i], wu) : s[i];
-                            uint64_t (&a)[2][2] = acc[ch * 4 + i];
-                            a[0][0] = fma2(pair2(v0[4 * i], v0[4 * i + 1]), sg, a[0][0]);
-                            a[0][1] = fma2(pair2(v0[4 * i + 2], v0[4 * i + 3]), sg, a[0][1]);
-                            a[1][0] = fma2(pair2(v1[4 * i], v1[4 * i + 1]), su, a[1][0]);
-                            a[1][1] = fma2(pair2(v1[4 * i + 2], v1[4 * i + 3]), su, a[1][1]);
-                        }
+                        for (int i = 0; i < 8; ++i) add_scaled2(acc[ch * 8 + i], v[2 * i], v[2 * i + 1], pair2(f, f));
                     }
+                } else {
+                    mbar_arrive_cluster_tmem(empty0 + buf * 8, lane);
                 }
             }
+            // a thread writes its token's columns, whole sectors at a time
+            const bool in = limit != 0 && lane < rows;
             if constexpr (SWIGLU) {
-                // rows 2 r4, 2 r4 + 1 of this quarter's 16 (the copy laid the weight rows out that way): activations into acc[.][0]
-                const int b2 = count & 1;
-                float (*peak)[PR_TILE] = sh.xs[batch & 1];   // (the last batch may still be read; everyone is past the one before)
+                // activations into the gate columns' sums; a block is the columns of both warps of the quarter
+                float big = 0.0f;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    if (i * 8 >= mine) break;
-                    float big0 = 0.0f, big1 = 0.0f;
-#pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        const float a0 = silu_times(low(acc[i][0][r]), low(acc[i][1][r])), a1 = silu_times(high(acc[i][0][r]), high(acc[i][1][r]));
-                        acc[i][0][r] = pair2(a0, a1);
-                        big0 = max_magnitude(big0, a0);
-                        big1 = max_magnitude(big1, a1);
-                    }
-#pragma unroll
-                    for (int o = 4; o < 32; o *= 2) {
-                        big0 = max_magnitude(big0, __shfl_xor_sync(0xffffffffu, big0, o));
-                        big1 = max_magnitude(big1, __shfl_xor_sync(0xffffffffu, big1, o));
-                    }
-                    if (lane < 4) *reinterpret_cast<float2 *>(&peak[q][col0 + i * 8 + c2]) = make_float2(big0, big1);
+                for (int i = 0; i < 32; ++i) {
+                    const float a = silu_times(low(acc[i]), low(acc[32 + i])), b = silu_times(high(acc[i]), high(acc[32 + i]));
+                    acc[i] = pair2(a, b);
+                    big = max_magnitude(max_magnitude(big, a), b);
                 }
-                asm volatile("bar.sync 1, 256;" ::: "memory");
-                // this CTA's largest values, and the other's (two buffers: neither CTA can be more than a tile ahead)
-                float own = 0.0f;
-                if (e < cols) {
+                sh.peak[h][q * 32 + lane] = big;
+                asm volatile("bar.sync %0, 64;" ::"r"(1 + q) : "memory");
+                const OutScale s(max_magnitude(big, sh.peak[h ^ 1][q * 32 + lane]));
+                asm volatile("bar.sync %0, 64;" ::"r"(1 + q) : "memory");   // (both have read before either writes again)
+                if (in) {
+                    if (h == 0) g.ys[(size_t)row * (g.n / 128) + t.nt] = s.scale;
+                    uint8_t *to = static_cast<uint8_t *>(g.y) + (size_t)row * g.n + t.nt * 128 + h * 64;
 #pragma unroll
-                    for (int p = 0; p < 4; ++p) own = max_magnitude(own, peak[p][e]);
-                    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(map_to_cta(smem_u32(&sh.other[b2][e]), rank ^ 1u)), "f"(own) : "memory");
-                }
-                __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive_cluster(map_to_cta(smem_u32(&sh.peer[b2]), rank ^ 1u));
-                    if (ok) ok = mbar_wait_cluster(smem_u32(&sh.peer[b2]), (count >> 1) & 1, abort_flag, g.wait_limit);
-                }
-                ok = __shfl_sync(0xffffffffu, ok, 0);
-                __syncwarp();
-                if (e < cols) {
-                    const OutScale s(max_magnitude(own, *(volatile float *)&sh.other[b2][e]));
-                    peak[0][e] = s.r;   // (only this thread looked at its token's column)
-                    if (ok && rank == 0 && e < t.cols) g.ys[(size_t)(t.t0 + e) * (g.n / 128) + t.nt] = s.scale;
-                }
-                asm volatile("bar.sync 1, 256;" ::: "memory");
-                // codes as [token][64 columns]
-                uint16_t *codes = reinterpret_cast<uint16_t *>(sh.stg);
+                    for (int k = 0; k < 2; ++k) {
+                        uint32_t c[8];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    if (i * 8 >= mine) break;
-                    const int c = col0 + i * 8 + c2;
-                    const float2 r = *reinterpret_cast<const float2 *>(&peak[0][c]);
-                    const int slot = q * 8 + r4;
-                    codes[c * 32 + (slot ^ ((c >> 1 & 3) * 8))] = (uint16_t)code2(low(acc[i][0][0]), low(acc[i][0][1]), r.x);
-                    codes[(c + 1) * 32 + (slot ^ ((c >> 1 & 3) * 8))] = (uint16_t)code2(high(acc[i][0][0]), high(acc[i][0][1]), r.y);
-                }
-                asm volatile("bar.sync 1, 256;" ::: "memory");
-                for (int i = e; i < t.cols * 4; i += 256) {
-                    const int c = i >> 2, part = i & 3;
-                    const uint4 v = *reinterpret_cast<const uint4 *>(&codes[c * 32 + ((part * 8) ^ ((c >> 1 & 3) * 8))]);
-                    if (ok) *reinterpret_cast<uint4 *>(static_cast<uint8_t *>(g.y) + (size_t)(t.t0 + c) * g.n + t.nt * 128 + rank * 64 + part * 16) = v;
-                }
-                // (the next tile writes codes behind several of its barriers)
-            } else {
-                // eight tokens at a time are turned through shared memory, so that a store covers whole pieces of consecutive columns
-                const int n_col = t.nt * PR_TILE + (int)rank * 128 + q * 32;
-                unsigned char *stg = sh.stg + (warp - 4) * PR_STG_WARP;
-                if (ok && n_col < g.n) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int c0 = col0 + i * 8;
-                        if (i * 8 >= mine || c0 >= t.cols) break;
-                        if (g.out == SPICE_OUT_BF16) {
-                            unsigned char *to = stg + (i & 1) * (8 * PR_PITCH);
-                            asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};"
-                                         ::"r"(smem_u32(to + (lane & 7) * PR_PITCH + (lane >> 3) * 16)),
-                                           "r"(pack2(low(acc[i][0][0]), high(acc[i][0][0]))), "r"(pack2(low(acc[i][0][1]), high(acc[i][0][1]))),
-                                           "r"(pack2(low(acc[i][1][0]), high(acc[i][1][0]))), "r"(pack2(low(acc[i][1][1]), high(acc[i][1][1]))) : "memory");
-                            __syncwarp();
-                            const int part = lane & 3, col = n_col + part * 8;
-                            const uint4 v = *reinterpret_cast<const uint4 *>(to + r4 * PR_PITCH + part * 16);
-                            if (c0 + r4 < t.cols && col < g.n)
-                                *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(g.y) + (size_t)(t.t0 + c0 + r4) * g.n + col) = v;
-                        } else {
-                            float *to = reinterpret_cast<float *>(stg);
-                            constexpr int P = PR_F32_PITCH / 4;
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) {
-                                const uint64_t v = acc[i][r >> 1][r & 1];
-                                to[c2 * P + r * 8 + r4] = low(v);
-                                to[(c2 + 1) * P + r * 8 + r4] = high(v);
-                            }
-                            __syncwarp();
-#pragma unroll
-                            for (int p = 0; p < 2; ++p) {
-                                const int tok = p * 4 + (lane >> 3), part = lane & 7, col = n_col + part * 4;
-                                float4 v = *reinterpret_cast<const float4 *>(to + tok * P + part * 4);
-                                if (c0 + tok < t.cols && col < g.n) {
-                                    float4 *dst = reinterpret_cast<float4 *>(static_cast<float *>(g.y) + (size_t)(t.t0 + c0 + tok) * g.n + col);
-                                    if (g.out == SPICE_OUT_F32_ADD) {
-                                        const float4 o = *dst;
-                                        v = make_float4(o.x + v.x, o.y + v.y, o.z + v.z, o.w + v.w);
-                                    }
-                                    *dst = v;
-                                }
-                            }
-                            __syncwarp();
+                        for (int i = 0; i < 8; ++i) {
+                            const uint64_t a = acc[k * 16 + 2 * i], b = acc[k * 16 + 2 * i + 1];
+                            c[i] = code2(low(a), high(a), s.r) | code2(low(b), high(b), s.r) << 16;
                         }
+                        store_sector(to + k * 32, c, g.sectors);
                     }
                 }
-                __syncwarp();   // (the buffers are free again)
+            } else if (in) {
+                const int col0 = t.nt * PR_TILE + h * 128;
+                if (g.out == SPICE_OUT_BF16) {
+                    __nv_bfloat16 *to = static_cast<__nv_bfloat16 *>(g.y) + (size_t)row * g.n + col0;
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        if (col0 + c * 16 >= g.n) break;
+                        uint32_t v[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) v[i] = pack2(low(acc[c * 8 + i]), high(acc[c * 8 + i]));
+                        if (col0 + c * 16 + 16 <= g.n) store_sector(to + c * 16, v, g.sectors);
+                        else *reinterpret_cast<uint4 *>(to + c * 16) = make_uint4(v[0], v[1], v[2], v[3]);   // (n is a multiple of 8)
+                    }
+                } else {
+                    float *to = static_cast<float *>(g.y) + (size_t)row * g.n + col0;
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) {
+                        if (col0 + c * 8 >= g.n) break;
+                        float f[8];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            f[2 * i] = low(acc[c * 4 + i]);
+                            f[2 * i + 1] = high(acc[c * 4 + i]);
+                        }
+                        if (g.out == SPICE_OUT_F32_ADD) {
+                            const float4 a = *reinterpret_cast<const float4 *>(to + c * 8), b = *reinterpret_cast<const float4 *>(to + c * 8 + 4);
+                            const float o[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) f[i] += o[i];
+                        }
+                        uint32_t v[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) v[i] = __float_as_uint(f[i]);
+                        store_sector(to + c * 8, v, g.sectors);
+                    }
+                }
             }
         }
     }
@@ -704,24 +635,18 @@ spice_status launch_gemm_e4m3(GemmE4m3Args g, const uint8_t *x, const uint8_t *w
         return launch_early(kernel, grid, FEW_WARPS * 32, 0, st, SWIGLU ? FEW_CLUSTER : 1, x, w, g) ? SPICE_OK : SPICE_ERR_CUDA;
     }
     g.n_tiles = SWIGLU ? g.n / 128 : (g.n + PR_TILE - 1) / PR_TILE;
+    const int row_bytes = SWIGLU ? 1 : g.out == SPICE_OUT_BF16 ? 2 : 4;
+    g.sectors = ((reinterpret_cast<uintptr_t>(g.y) | (uintptr_t)g.n * row_bytes) & 31u) == 0;
     const int64_t most = ((int64_t)g.T / PR_TILE + g.G) * g.n_tiles;   // tiles there can be
     if (most > 0x3fffffff) return SPICE_ERR_UNSUPPORTED_SHAPE;
-    CUtensorMap map_w, map_x[3];
-    if (SWIGLU) {
-        // rows of a tile in shared memory: 16 gate rows, their 16 up rows, the next 16 gate rows, ...; within 16 the even rows, then
-        // the odd ones: a thread's two sums of a token are neighbours
-        const uint64_t k = (uint64_t)g.k, in = (uint64_t)g.n;
-        const uint64_t dims[5] = {k, 8, 2, 2 * (uint64_t)g.G, in / 16}, strides[4] = {2 * k, k, in * k, 16 * k};
-        const uint32_t box[5] = {BK, 8, 2, 2, 4};
-        if (!tc_encode_map5(&map_w, w, dims, strides, box, 1)) return SPICE_ERR_CUDA;
-    } else if (!tc_encode_map2_bytes(&map_w, w, (uint64_t)g.G * w_rows, (uint64_t)g.k, 128)) {
+    CUtensorMap map_w, map_x128, map_x16;
+    if (!tc_encode_map2_bytes(&map_w, w, (uint64_t)g.G * w_rows, (uint64_t)g.k, 128) ||
+        !tc_encode_map2_bytes(&map_x128, x, (uint64_t)g.T, (uint64_t)g.k, 128) ||
+        !tc_encode_map2_bytes(&map_x16, x, (uint64_t)g.T, (uint64_t)g.k, 16))
         return SPICE_ERR_CUDA;
-    }
-    for (int i = 0; i < 3; ++i)
-        if (!tc_encode_map2_bytes(&map_x[i], x, (uint64_t)g.T, (uint64_t)g.k, 64u >> i)) return SPICE_ERR_CUDA;
     const int pairs = (int)std::min<int64_t>(sms / 2, most);
-    return launch_early(gemm_e4m3_pair_kernel<SWIGLU>, dim3(2 * (unsigned)pairs), PR_THREADS, PR_SMEM_BYTES, st, 2, map_w, map_x[0], map_x[1],
-                        map_x[2], g) ? SPICE_OK : SPICE_ERR_CUDA;
+    return launch_early(gemm_e4m3_pair_kernel<SWIGLU>, dim3(2 * (unsigned)pairs), PR_THREADS, PR_SMEM_BYTES, st, 2, map_w, map_x128, map_x16,
+                        g) ? SPICE_OK : SPICE_ERR_CUDA;
 }
 
 bool misaligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }

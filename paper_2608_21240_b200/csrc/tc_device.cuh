@@ -46,19 +46,23 @@ __device__ __forceinline__ bool mbar_wait(uint32_t a, uint32_t parity, volatile 
     *abort_flag = 1;
     return false;
 }
-// the same for a barrier on which another CTA of the cluster arrives after writing into this one's shared memory
-__device__ __forceinline__ bool mbar_wait_cluster(uint32_t a, uint32_t parity, volatile int *abort_flag, uint32_t limit) {
-    for (uint32_t i = 0; i < limit; ++i) {
-        uint32_t ok;
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                     : "=r"(ok)
-                     : "r"(a), "r"(parity)
-                     : "memory");
-        if (ok) return true;
-        if ((i & 1023u) == 1023u && *abort_flag) return false;
+// The same for inner loops: no answer to branch on.  limit: tries this wait has; a wait that runs out raises the flag, leaves 0 (the
+// caller's later waits look once) and the caller carries on with what is there.
+__device__ __forceinline__ void mbar_wait_quick(uint32_t a, uint32_t parity, volatile int *abort_flag, uint32_t &limit) {
+    uint32_t left;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\tmov.u32 n, %3;\n\t"
+        "TRY:\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t@p bra DONE;\n\t"
+        "setp.eq.u32 q, n, 0;\n\t@q bra OUT;\n\tsub.u32 n, n, 1;\n\tbra TRY;\n\t"
+        "OUT:\n\tmov.u32 %0, 0;\n\tbra END;\n\t"
+        "DONE:\n\tmov.u32 %0, 1;\n\tEND:\n\t}"
+        : "=r"(left)
+        : "r"(a), "r"(parity), "r"(limit)
+        : "memory");
+    if (left == 0) {
+        *abort_flag = 1;
+        limit = 0;
     }
-    *abort_flag = 1;
-    return false;
 }
 // wait for work already in flight (copies, MMAs) that must be over before the CTA ends: ignores the abort flag; false when the
 // limit expired
@@ -135,6 +139,11 @@ __device__ __forceinline__ uint32_t map_to_cta(uint32_t saddr, uint32_t rank) {
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
+// the same where nothing but tensor memory is handed over (its reads are over, tcgen05.fence orders them): no fence over the
+// cluster's shared and global memory, which would wait for this thread's outstanding stores
+__device__ __forceinline__ void mbar_arrive_cluster_tmem(uint32_t cluster_addr, int lane) {   // (lane 0 of the warp does)
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.eq.s32 p, %1, 0;\n\t@p mbarrier.arrive.shared::cluster.b64 _, [%0];\n\t}" ::"r"(cluster_addr), "r"(lane) : "memory");
+}
 // a tile into this CTA's shared memory whose bytes are reported to a barrier of either CTA of the pair
 __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t mbar_cluster) {
     asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
@@ -160,14 +169,11 @@ __device__ __forceinline__ void tc_ld32(uint32_t taddr, uint32_t (&v)[32]) {
           "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
         : "r"(taddr));
 }
-// 16 lanes x 32 columns in the fragment layout of the warp-wide products: v[4 j + i] holds lane (l / 4) + 8 (i / 2), column
-// 8 j + 2 (l % 4) + i % 2
-__device__ __forceinline__ void tc_ld_fragments(uint32_t taddr, uint32_t (&v)[16]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
-          "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
-        : "r"(taddr));
+// values that a wait has made valid: nothing that uses them is computed before this point
+__device__ __forceinline__ void tc_pin(uint32_t (&v)[32]) {
+#pragma unroll
+    for (int i = 0; i < 32; i += 8)
+        asm volatile("" : "+r"(v[i]), "+r"(v[i + 1]), "+r"(v[i + 2]), "+r"(v[i + 3]), "+r"(v[i + 4]), "+r"(v[i + 5]), "+r"(v[i + 6]), "+r"(v[i + 7]));
 }
 __device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
@@ -195,14 +201,6 @@ __device__ __forceinline__ void tma_load_5d_hint(uint32_t dst, const CUtensorMap
     asm volatile(
         "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%2, %3, %4, %5, %6}], [%7], %8;"
         ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4), "r"(mbar), "l"(policy)
-        : "memory");
-}
-// ... reported to a barrier of either CTA of the pair
-__device__ __forceinline__ void tma_load_5d_pair(uint32_t dst, const CUtensorMap *map, int c0, int c1, int c2, int c3, int c4,
-                                                 uint32_t mbar_cluster) {
-    asm volatile(
-        "cp.async.bulk.tensor.5d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
-        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4), "r"(mbar_cluster)
         : "memory");
 }
 // L2 policy "evict first": data that is read exactly once (streamed weights) should not push out what is reused
