@@ -13,6 +13,8 @@
 #include <cuda_fp8.h>
 
 #include <algorithm>
+#include <mutex>
+#include <type_traits>
 
 #include "entry.cuh"
 #include "spice_internal.cuh"
@@ -38,6 +40,7 @@ struct GemmE4m3Args {
     int32_t *status;         // optional
     uint32_t wait_limit;     // polls after which a wait inside a kernel gives up
     int32_t n_tiles;         // tiles along n
+    int32_t split;           // some rows a group: CTAs of a cluster that share a reduction
     int32_t sectors;         // rows of y begin on 32-byte boundaries
 };
 
@@ -100,6 +103,19 @@ __device__ __forceinline__ void store_sector(void *to, const uint32_t (&v)[8], i
         reinterpret_cast<uint4 *>(to)[1] = make_uint4(v[4], v[5], v[6], v[7]);
     }
 }
+// four neighbouring columns
+__device__ __forceinline__ void store4(const GemmE4m3Args &g, size_t at, float4 v) {
+    if (g.out == SPICE_OUT_BF16) {
+        *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(g.y) + at) = make_uint2(pack2(v.x, v.y), pack2(v.z, v.w));
+        return;
+    }
+    float4 *dst = reinterpret_cast<float4 *>(static_cast<float *>(g.y) + at);
+    if (g.out == SPICE_OUT_F32_ADD) {
+        const float4 o = *dst;
+        v = make_float4(o.x + v.x, o.y + v.y, o.z + v.z, o.w + v.w);
+    }
+    *dst = v;
+}
 __device__ __forceinline__ void store1(const GemmE4m3Args &g, size_t at, float v) {
     if (g.out == SPICE_OUT_BF16) static_cast<__nv_bfloat16 *>(g.y)[at] = __float2bfloat16_rn(v);
     else if (g.out == SPICE_OUT_F32) static_cast<float *>(g.y)[at] = v;
@@ -107,196 +123,319 @@ __device__ __forceinline__ void store1(const GemmE4m3Args &g, size_t at, float v
 }
 
 // ------------------------------------------------------------------------------------------------ few rows a group
-// A block multiplies 16 weight rows (SwiGLU: 16 gate rows and their up rows) with the rows of one group, eight or sixteen at a
-// time; its warps share the blocks of the reduction.  Both operands are read in pieces of 16 bytes, so the order of the reduction
-// inside a 64-byte piece is the same for both and does not matter.  SwiGLU: eight blocks of a cluster hold the 128 columns of an
-// output block and exchange their largest values.
-constexpr int FEW_WARPS = 8, FEW_CLUSTER = 8;
+// The weights stream through a ring in shared memory at the rate of HBM, and eight warps multiply them with up to 32 tokens in
+// warp-wide products: a warp has 32 weight rows (SwiGLU: 16 gate rows and their up rows) and all the tokens, so that only a stage's
+// operands pass through shared memory and no sums do.  (On tcgen05 the sums of every block would have to come back from tensor
+// memory, a round trip of 1.0 us for two blocks, twice what a block of weights takes to arrive.)  Persistent over (group, 256
+// weight rows, up to 32 tokens); where those are fewer than the SMs, the CTAs of a cluster share the reduction of one and add up
+// through distributed shared memory.
+constexpr int ST_WARPS = 8, ST_THREADS = ST_WARPS * 32 + 32, ST_MAX_SPLIT = 8;
+constexpr int ST_W_BYTES = 256 * BK;
+constexpr int ST_RED_PITCH = 260;                 // fp32 sums of a token's 256 weight rows, padded against bank conflicts
 
-__device__ __forceinline__ int4 load_once(const int4 *p) {
-    int4 v;
-    asm volatile("ld.global.cs.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-    return v;
+template <int NT>
+struct StreamShape {
+    static constexpr int TOKENS = NT * 8, STAGE_BYTES = ST_W_BYTES + TOKENS * BK, STAGES = 6;
+};
+template <int NT>
+struct StreamShared {
+    float xs[StreamShape<NT>::STAGES][StreamShape<NT>::TOKENS];
+    float peak[ST_WARPS][StreamShape<NT>::TOKENS];    // SwiGLU: largest magnitude of a token's columns, per warp
+    int32_t first[MAX_GROUPS + 1];                    // tiles before each group
+    alignas(8) unsigned long long full[6], empty[6];
+    int abort_flag;
+};
+template <int NT>
+constexpr size_t stream_smem() {
+    return sizeof(StreamShared<NT>) + (size_t)StreamShape<NT>::STAGES * StreamShape<NT>::STAGE_BYTES + 1024;
 }
-__device__ __forceinline__ int4 load_again(const int4 *p) {
-    int4 v;
-    asm volatile("ld.global.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-    return v;
+static_assert(stream_smem<4>() <= 232448, "what a block can have");
+static_assert(32 * ST_RED_PITCH * 4 <= 6 * ST_W_BYTES, "the sums fit in the ring");
+
+// Tiles before each group, by one warp: per group (its rows / `rows`, rounded up) x n_tiles; a group whose offsets are not in
+// order or out of range has none.
+__device__ __forceinline__ void count_tiles(const GemmE4m3Args &g, int rows, int32_t *first) {
+    const int lane = threadIdx.x & 31;
+    int carry = 0;
+    for (int base = 0; base < g.G; base += 32) {
+        const int i = base + lane;
+        int b = 0, e = g.T, tiles = 0;
+        if (i < g.G && g.offset) {
+            b = load_s32(g.offset + i);
+            e = load_s32(g.offset + i + 1);
+        }
+        if (i < g.G) {
+            if (b < 0 || e < b || e > g.T) {
+                if (blockIdx.x == 0 && g.status) atomicMax(g.status, (int)SPICE_ERR_BAD_TABLE);
+            } else {
+                tiles = (e - b + rows - 1) / rows * g.n_tiles;
+            }
+        }
+        int incl = tiles;
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const int v = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += v;
+        }
+        if (i < g.G) first[i] = carry + incl - tiles;
+        carry += __shfl_sync(0xffffffffu, incl, 31);
+    }
+    if (lane == 0) first[g.G] = carry;
 }
+
+struct Tile {
+    int group, t0, rows, nt;   // first token, tokens, weight tile
+};
+
 __device__ __forceinline__ void mma_e4m3(float (&d)[4], int a0, int a1, int a2, int a3, int b0, int b1) {
     asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// The slot-th group that has rows: its number, or -1; groups whose offsets are not in order or out of range have none.
-__device__ __forceinline__ int find_group(const GemmE4m3Args &g, int slot, int32_t *off, int &begin, int &rows) {
-    for (int i = threadIdx.x; i <= g.G; i += blockDim.x) off[i] = load_s32(g.offset + i);
-    __syncthreads();
-    auto bad = [&](int i) { return off[i] < 0 || off[i + 1] < off[i] || off[i + 1] > g.T; };
-    if (blockIdx.x == 0 && slot == 0 && g.status)
-        for (int i = threadIdx.x; i < g.G; i += blockDim.x)
-            if (bad(i)) atomicMax(g.status, (int)SPICE_ERR_BAD_TABLE);
-    const int lane = threadIdx.x & 31;
-    int seen = 0;
-    for (int base = 0; base < g.G; base += 32) {
-        const int i = base + lane;
-        uint32_t mask = __ballot_sync(0xffffffffu, i < g.G && !bad(i) && off[i + 1] > off[i]);
-        const int here = __popc(mask);
-        if (seen + here > slot) {
-            for (int s = slot - seen; s > 0; --s) mask &= mask - 1;
-            const int found = base + __ffs(mask) - 1;
-            begin = off[found];
-            rows = off[found + 1] - begin;
-            return found;
-        }
-        seen += here;
-    }
-    return -1;
+__device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t (&v)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(addr));
 }
 
-template <int NT, bool SWIGLU>
-__global__ void __launch_bounds__(FEW_WARPS * 32) gemm_e4m3_few_kernel(const uint8_t *x, const uint8_t *w, const GemmE4m3Args g) {
-    constexpr int RT = SWIGLU ? 2 : 1, UN = NT * RT > 2 ? 1 : 2;
-    __shared__ float red[FEW_WARPS][NT * 8][RT * 16 + 4];   // (padded: the 8 rows of a warp's store fall into different banks)
-    __shared__ int32_t off[MAX_GROUPS + 1];
-    __shared__ float peak[NT * 8];                          // SwiGLU: largest magnitude of each token's 16 columns
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int gq = lane >> 2, c = lane & 3;
-    const int n0 = blockIdx.x * 16;
-    grid_dependency();
-    int group = 0, begin = 0, rows = g.T;
-    if (g.offset) {
-        group = find_group(g, blockIdx.y, off, begin, rows);
-        if (group < 0) return;                              // (the same for every block of a cluster)
-    }
-    const int w_rows = SWIGLU ? 2 * g.n : g.n, row_blocks = (w_rows + 127) / 128;
-    const int4 *wr[RT][2];
-    const float *ws[RT];
-#pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        const int first = r * g.n + n0;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int row = first + gq + (n0 + 8 * h < g.n ? 8 * h : 0);   // (n is a multiple of 8)
-            wr[r][h] = reinterpret_cast<const int4 *>(w + ((size_t)group * w_rows + row) * g.k);
+template <int NT, bool SWIGLU, bool SPLIT>
+__global__ void __launch_bounds__(ST_THREADS, 1)
+    gemm_e4m3_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const GemmE4m3Args g) {
+    using Shape = StreamShape<NT>;
+    constexpr uint32_t STAGES = Shape::STAGES;
+    extern __shared__ __align__(16) unsigned char smem_raw[];   // (aligned to 1024 by hand: the swizzled tiles)
+    unsigned char *ring = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    StreamShared<NT> &sh = *reinterpret_cast<StreamShared<NT> *>(ring + STAGES * Shape::STAGE_BYTES);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    volatile int *abort_flag = &sh.abort_flag;
+    const int split = SPLIT ? g.split : 1, rank = SPLIT ? (int)cluster_rank() : 0;
+
+    if (threadIdx.x == 0) {
+        for (uint32_t s = 0; s < STAGES; ++s) {
+            mbar_init(smem_u32(&sh.full[s]), 33);           // the copies, and the scales that a warp fetches
+            mbar_init(smem_u32(&sh.empty[s]), ST_WARPS);
         }
-        ws[r] = g.ws + ((size_t)group * row_blocks + first / 128) * g.kb;
+        sh.abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_proxy_async();
     }
-    const int nv = g.k >> 4;
-    for (int t0 = 0; t0 < rows; t0 += NT * 8) {
-        const int m = min(rows - t0, NT * 8), row0 = begin + t0;
-        const int4 *x4 = reinterpret_cast<const int4 *>(x) + (size_t)row0 * nv;
-        const float *xs = g.xs + (size_t)row0 * g.kb;
-        float acc[RT][NT][4];
+    grid_dependency();
+    if (warp == ST_WARPS) count_tiles(g, Shape::TOKENS, sh.first);
+    __syncthreads();
+    const int n_items = sh.first[g.G];
+    const int team = blockIdx.x / split, teams = gridDim.x / split;
+    const int kb0 = g.kb * rank / split, kbs = g.kb * (rank + 1) / split - kb0;
+    const uint32_t ring0 = smem_u32(ring), full0 = smem_u32(&sh.full[0]), empty0 = smem_u32(&sh.empty[0]);
+    auto find = [&](int item, int &group) {
+        while (item >= sh.first[group + 1]) ++group;
+        const int begin = g.offset ? load_s32(g.offset + group) : 0, m = (g.offset ? load_s32(g.offset + group + 1) : g.T) - begin;
+        const int parts = (m + Shape::TOKENS - 1) / Shape::TOKENS, in = item - sh.first[group];
+        const int t0 = in % parts * Shape::TOKENS;
+        return Tile{group, begin + t0, min(Shape::TOKENS, m - t0), in / parts};
+    };
+
+    if (warp == ST_WARPS) {
+        uint32_t s = 0, phase = 1, filled = 0, limit = g.wait_limit;
+        int group = 0;
+        for (int item = team; item < n_items && limit != 0; item += teams) {
+            const Tile t = find(item, group);
+            const int w0 = SWIGLU ? 2 * t.group * g.n + t.nt * 128 : t.group * g.n + t.nt * 256, w1 = SWIGLU ? w0 + g.n : w0 + 128;
+            for (int b = kb0; b < kb0 + kbs; ++b) {
+                mbar_wait_quick(empty0 + s * 8, phase, abort_flag, limit);
+                if (limit == 0) break;
+                const uint32_t dst = ring0 + s * Shape::STAGE_BYTES, full = full0 + s * 8;
+                if (lane == 0) {
+                    mbar_expect_tx(full, Shape::STAGE_BYTES);
+                    tma_load_2d(dst, &map_w, b * BK, w0, full);
+                    tma_load_2d(dst + ST_W_BYTES / 2, &map_w, b * BK, w1, full);
+                    tma_load_2d(dst + ST_W_BYTES, &map_x, b * BK, t.t0, full);
+                }
 #pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-            for (int i = 0; i < NT; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[r][i][j] = 0.0f;
-        const int4 zero = make_int4(0, 0, 0, 0);
-        for (int b0 = warp; b0 < g.kb; b0 += FEW_WARPS * UN) {
-            int4 a[UN][RT][2][2], bx[UN][2][NT];
-            float sx[UN][NT][2], sw[UN][RT];
-#pragma unroll
-            for (int u = 0; u < UN; ++u) {
-                const int b = b0 + u * FEW_WARPS;
-#pragma unroll
-                for (int p = 0; p < 2; ++p) {
-                    const int v = b * 8 + p * 4 + c;
-                    const bool in = b < g.kb && v < nv;
-#pragma unroll
-                    for (int r = 0; r < RT; ++r)
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) a[u][r][p][h] = in ? load_once(wr[r][h] + v) : zero;
+                for (int c = lane; c < Shape::TOKENS; c += 32) {   // (of tokens that are not there: zeros)
+                    const float *from = g.xs + (size_t)(t.t0 + min(c, t.rows - 1)) * g.kb + b;
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(&sh.xs[s][c])), "l"(from), "r"(c < t.rows ? 4 : 0) : "memory");
+                }
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(full) : "memory");
+                filled = min(filled + 1, STAGES);
+                if (++s == STAGES) {
+                    s = 0;
+                    phase ^= 1;
                 }
             }
+        }
+        // everything that was ordered has landed before the CTA ends
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        if (lane == 0)
+            for (uint32_t left = filled; left > 0; --left) {
+                const uint32_t back = s >= left ? 0u : 1u;   // the stage filled `left` blocks ago: in this round of the ring, or the one before
+                if (!mbar_drain(full0 + (s + back * STAGES - left) * 8, phase ^ 1 ^ back)) {
+                    *abort_flag = 1;
+                    break;
+                }
+            }
+        __syncwarp();
+        if (SPLIT) {
+            cluster_sync();
+            cluster_sync();
+        }
+    } else {
+        const int r4 = lane >> 2, c2 = 2 * (lane & 3);
+        const int row_blocks = ((SWIGLU ? 2 * g.n : g.n) + 127) / 128;
+        // rows of this warp in a stage: its two tiles of 16
+        const int wr0 = SWIGLU ? warp * 16 : warp * 32, wr1 = SWIGLU ? 128 + warp * 16 : warp * 32 + 16;
+        // lane's row and 16-byte piece in a load of four 8 x 16 byte matrices (A: rows 0-7, 8-15, then the next 16 bytes; B: 16 bytes
+        // after 16 bytes); rows of 128 bytes, pieces swizzled by the row
+        const int ar = (lane & 7) + (lane & 8), ac = lane >> 4, br = lane & 7, bc = lane >> 3;
+        uint32_t s = 0, phase = 0, limit = g.wait_limit;
+        int group = 0;
+        for (int item = team; item < n_items; item += teams) {
+            const Tile t = find(item, group);
+            const int nb = SWIGLU ? t.nt : min(t.nt * 2 + warp / 4, row_blocks - 1);
+            const float *ws = g.ws + ((size_t)t.group * row_blocks + nb) * g.kb + kb0, *wu = ws + (size_t)(g.n / 128) * g.kb;
+            float acc[2][NT][4];
 #pragma unroll
-            for (int u = 0; u < UN; ++u) {
-                const int b = b0 + u * FEW_WARPS;
+            for (int r = 0; r < 2; ++r)
 #pragma unroll
-                for (int p = 0; p < 2; ++p) {
-                    const int v = b * 8 + p * 4 + c;
+                for (int i = 0; i < NT; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[r][i][j] = 0.0f;
+            float w_next = load_f32(ws), u_next = SWIGLU ? load_f32(wu) : 0.0f;
+#pragma unroll 1
+            for (int b = 0; b < kbs; ++b) {
+                const float sw[2] = {w_next, SWIGLU ? u_next : w_next};
+                const int ahead = min(b + 1, kbs - 1);
+                w_next = load_f32(ws + ahead);
+                if (SWIGLU) u_next = load_f32(wu + ahead);
+                mbar_wait_quick(full0 + s * 8, phase, abort_flag, limit);
+                const uint32_t wt = ring0 + s * Shape::STAGE_BYTES, xt = wt + ST_W_BYTES + br * BK;
+                uint32_t a[2][4][4];
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) ldmatrix4(wt + ((r ? wr1 : wr0) + ar) * BK + (((2 * k + ac) ^ (ar & 7)) << 4), a[r][k]);
+#pragma unroll
+                for (int i = 0; i < NT; ++i) {
+                    uint32_t lo[4], hi[4];
+                    ldmatrix4(xt + i * 8 * BK + ((bc ^ br) << 4), lo);
+                    ldmatrix4(xt + i * 8 * BK + (((4 + bc) ^ br) << 4), hi);
+                    const float2 sx = *reinterpret_cast<const float2 *>(&sh.xs[s][i * 8 + c2]);
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                        mma_e4m3(d, a[r][0][0], a[r][0][1], a[r][0][2], a[r][0][3], lo[0], lo[1]);
+                        mma_e4m3(d, a[r][1][0], a[r][1][1], a[r][1][2], a[r][1][3], lo[2], lo[3]);
+                        mma_e4m3(d, a[r][2][0], a[r][2][1], a[r][2][2], a[r][2][3], hi[0], hi[1]);
+                        mma_e4m3(d, a[r][3][0], a[r][3][1], a[r][3][2], a[r][3][3], hi[2], hi[3]);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) acc[r][i][j] = fmaf(d[j], (j & 1 ? sx.y : sx.x) * sw[r], acc[r][i][j]);
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(empty0 + s * 8);
+                if (++s == STAGES) {
+                    s = 0;
+                    phase ^= 1;
+                }
+            }
+            const bool ok = limit != 0;
+            if constexpr (SPLIT) {
+                // ---- one item per cluster: sums as [token][256 weight rows] over the ring, which nobody fills any more
+                asm volatile("bar.sync 1, 256;" ::: "memory");   // (all have read their last stage)
+                float *red = reinterpret_cast<float *>(ring);
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
 #pragma unroll
                     for (int i = 0; i < NT; ++i)
-                        bx[u][p][i] = b < g.kb && v < nv && i * 8 + gq < m ? load_again(x4 + (size_t)(i * 8 + gq) * nv + v) : zero;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) red[(i * 8 + c2 + (j & 1)) * ST_RED_PITCH + (r ? wr1 : wr0) + r4 + (j >> 1) * 8] = acc[r][i][j];
+                cluster_sync();
+                // every CTA finishes some of the tokens, a warp a token at a time; its lanes have four neighbouring rows each
+                for (int c = rank + warp * split; c < t.rows; c += ST_WARPS * split) {
+                    float4 v[2];
+#pragma unroll
+                    for (int z = 0; z < 2; ++z) {
+                        const uint32_t at = smem_u32(red + c * ST_RED_PITCH + z * 128 + lane * 4);
+                        v[z] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                        for (int p = 0; p < split; ++p) {
+                            float4 o;
+                            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(o.x), "=f"(o.y), "=f"(o.z), "=f"(o.w) : "r"(map_to_cta(at, (uint32_t)p)));
+                            v[z] = make_float4(v[z].x + o.x, v[z].y + o.y, v[z].z + o.z, v[z].w + o.w);
+                        }
+                    }
+                    if constexpr (SWIGLU) {
+                        const float a[4] = {silu_times(v[0].x, v[1].x), silu_times(v[0].y, v[1].y), silu_times(v[0].z, v[1].z), silu_times(v[0].w, v[1].w)};
+                        float big = max_magnitude(max_magnitude(max_magnitude(fabsf(a[0]), a[1]), a[2]), a[3]);
+#pragma unroll
+                        for (int o = 16; o > 0; o >>= 1) big = max_magnitude(big, __shfl_xor_sync(0xffffffffu, big, o));
+                        const OutScale q(big);
+                        if (ok) {
+                            *reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(g.y) + (size_t)(t.t0 + c) * g.n + t.nt * 128 + lane * 4) =
+                                code2(a[0], a[1], q.r) | code2(a[2], a[3], q.r) << 16;
+                            if (lane == 0) g.ys[(size_t)(t.t0 + c) * (g.n / 128) + t.nt] = q.scale;
+                        }
+                    } else if (ok) {
+#pragma unroll
+                        for (int z = 0; z < 2; ++z) {
+                            const int col = t.nt * 256 + z * 128 + lane * 4;
+                            if (col < g.n) store4(g, (size_t)(t.t0 + c) * g.n + col, v[z]);
+                        }
+                    }
                 }
+                cluster_sync();   // nobody leaves while a peer reads its sums
+            } else if constexpr (SWIGLU) {
+#pragma unroll
+                for (int i = 0; i < NT; ++i) {
+                    float big[2] = {0.0f, 0.0f};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        acc[0][i][j] = silu_times(acc[0][i][j], acc[1][i][j]);
+                        big[j & 1] = max_magnitude(big[j & 1], acc[0][i][j]);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                        for (int o = 4; o < 32; o *= 2) big[j] = max_magnitude(big[j], __shfl_xor_sync(0xffffffffu, big[j], o));
+                        if (lane < 4) sh.peak[warp][i * 8 + c2 + j] = big[j];
+                    }
+                }
+                asm volatile("bar.sync 1, 256;" ::: "memory");
 #pragma unroll
                 for (int i = 0; i < NT; ++i)
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        const int t = i * 8 + 2 * c + j;
-                        sx[u][i][j] = b < g.kb && t < m ? load_f32(xs + (size_t)t * g.kb + b) : 0.0f;
-                    }
+                        const int c = i * 8 + c2 + j;
+                        if (i * 8 >= t.rows) break;
+                        float big = sh.peak[0][c];
 #pragma unroll
-                for (int r = 0; r < RT; ++r) sw[u][r] = b < g.kb ? load_f32(ws[r] + b) : 0.0f;
-            }
-#pragma unroll
-            for (int u = 0; u < UN; ++u)
-#pragma unroll
-                for (int r = 0; r < RT; ++r)
-#pragma unroll
-                    for (int i = 0; i < NT; ++i) {
-                        float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                        for (int p = 0; p < 2; ++p) {
-                            const int4 a0 = a[u][r][p][0], a1 = a[u][r][p][1], bb = bx[u][p][i];
-                            mma_e4m3(d, a0.x, a1.x, a0.y, a1.y, bb.x, bb.y);
-                            mma_e4m3(d, a0.z, a1.z, a0.w, a1.w, bb.z, bb.w);
+                        for (int p = 1; p < ST_WARPS; ++p) big = max_magnitude(big, sh.peak[p][c]);
+                        const OutScale q(big);
+                        if (ok && c < t.rows) {
+                            uint8_t *to = static_cast<uint8_t *>(g.y) + (size_t)(t.t0 + c) * g.n + t.nt * 128 + warp * 16 + r4;
+                            const uint32_t two = code2(acc[0][i][j], acc[0][i][j + 2], q.r);
+                            to[0] = (uint8_t)two;
+                            to[8] = (uint8_t)(two >> 8);
+                            if (warp == 0 && r4 == 0) g.ys[(size_t)(t.t0 + c) * (g.n / 128) + t.nt] = q.scale;
                         }
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) acc[r][i][j] = fmaf(d[j], sx[u][i][j & 1] * sw[u][r], acc[r][i][j]);
                     }
-        }
+                asm volatile("bar.sync 1, 256;" ::: "memory");   // (all have read the magnitudes)
+            } else if (ok) {
 #pragma unroll
-        for (int r = 0; r < RT; ++r)
+                for (int r = 0; r < 2; ++r)
 #pragma unroll
-            for (int i = 0; i < NT; ++i) {   // rows gq, gq + 8 x tokens 2c, 2c + 1
-                red[warp][i * 8 + 2 * c][r * 16 + gq] = acc[r][i][0];
-                red[warp][i * 8 + 2 * c + 1][r * 16 + gq] = acc[r][i][1];
-                red[warp][i * 8 + 2 * c][r * 16 + gq + 8] = acc[r][i][2];
-                red[warp][i * 8 + 2 * c + 1][r * 16 + gq + 8] = acc[r][i][3];
-            }
-        __syncthreads();
-        constexpr int ITEMS = NT * 8 * 16;   // one per thread at most
-        static_assert(ITEMS <= FEW_WARPS * 32, "an output per thread");
-        const int t = threadIdx.x / 16, r = threadIdx.x % 16;
-        float v = 0.0f, u = 0.0f;
-        if (threadIdx.x < ITEMS) {
+                    for (int i = 0; i < NT; ++i)
 #pragma unroll
-            for (int q = 0; q < FEW_WARPS; ++q) {
-                v += red[q][t][r];
-                if (SWIGLU) u += red[q][t][16 + r];
+                        for (int j = 0; j < 4; ++j) {
+                            const int c = i * 8 + c2 + (j & 1), col = t.nt * 256 + (r ? wr1 : wr0) + r4 + (j >> 1) * 8;
+                            if (c < t.rows && col < g.n) store1(g, (size_t)(t.t0 + c) * g.n + col, acc[r][i][j]);
+                        }
             }
         }
-        if constexpr (!SWIGLU) {
-            if (threadIdx.x < ITEMS && t < m && n0 + r < g.n) store1(g, (size_t)(row0 + t) * g.n + n0 + r, v);
-            __syncthreads();   // the sums have been read
-        } else {
-            v = silu_times(v, u);
-            float big = fabsf(v);
-#pragma unroll
-            for (int o = 8; o > 0; o >>= 1) big = max_magnitude(big, __shfl_xor_sync(0xffffffffu, big, o));
-            if (threadIdx.x < ITEMS && r == 0) peak[t] = big;
+        if (SPLIT && team >= n_items) {   // (there is an item for every cluster unless offsets were bad)
             cluster_sync();
-            if (threadIdx.x < ITEMS) {
-                const uint32_t at = smem_u32(&peak[t]);
-#pragma unroll
-                for (uint32_t p = 0; p < FEW_CLUSTER; ++p) {
-                    float o;
-                    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o) : "r"(map_to_cta(at, p)));
-                    big = max_magnitude(big, o);
-                }
-                const OutScale s(big);
-                if (t < m) {
-                    static_cast<uint8_t *>(g.y)[(size_t)(row0 + t) * g.n + n0 + r] = (uint8_t)code2(v, 0.0f, s.r);
-                    if (r == 0 && n0 % 128 == 0) g.ys[(size_t)(row0 + t) * (g.n / 128) + n0 / 128] = s.scale;
-                }
-            }
-            cluster_sync();    // nobody writes its next values, or leaves, while a peer reads
+            cluster_sync();
         }
     }
+    __syncthreads();
+    if (threadIdx.x == 0 && sh.abort_flag && g.status) atomicMax(g.status, (int)SPICE_ERR_TIMEOUT);
 }
 
 // ------------------------------------------------------------------------------------------------ more rows
@@ -320,10 +459,6 @@ struct PairShared {
 constexpr size_t PR_SMEM_BYTES = sizeof(PairShared) + (size_t)PR_STAGES * PR_STAGE_BYTES + 1024;
 static_assert(PR_SMEM_BYTES <= 232448, "what a block can have");
 
-struct Tile {
-    int group, t0, rows, nt;   // first token, tokens, weight tile
-};
-
 // Tiles are numbered group by group; within a group sweeps of up to PR_GROUP_M token tiles, the token tile fastest, so that
 // pairs working at the same time share both operands in L2.  The group only moves forward.
 __device__ __forceinline__ Tile find_tile(const PairShared &sh, const GemmE4m3Args &g, int tile, int &group) {
@@ -339,7 +474,9 @@ __device__ __forceinline__ Tile find_tile(const PairShared &sh, const GemmE4m3Ar
 // could fall two uses of a stage behind, and the parity of a barrier would no longer tell it which use is meant.
 __device__ __forceinline__ int copied(int rows, int rank) { return (min(max(rows - rank * 128, 1), 128) + 15) & ~15; }
 
-template <bool SWIGLU>
+// SPLIT: the reduction of a tile is shared by the g.split pairs of a cluster (one tile per cluster, one group): each pair leaves its
+// sums in its shared memory and finishes its share of the tokens with those of the others.
+template <bool SWIGLU, bool SPLIT>
 __global__ void __launch_bounds__(PR_THREADS, 1)
     gemm_e4m3_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x128,
                           const __grid_constant__ CUtensorMap map_x16, const GemmE4m3Args g) {
@@ -347,7 +484,8 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
     unsigned char *ring = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     PairShared &sh = *reinterpret_cast<PairShared *>(ring + PR_STAGES * PR_STAGE_BYTES);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int rank = (int)cluster_rank();
+    const int rank = (int)(cluster_rank() & 1u), part = SPLIT ? (int)(cluster_rank() >> 1) : 0;
+    const uint32_t leader = 2 * part, pair_mask = 3u << leader;
     volatile int *abort_flag = &sh.abort_flag;
 
     if (threadIdx.x == 0) {
@@ -368,40 +506,15 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::);
     }
     grid_dependency();
-    if (warp == 2) {   // tiles before each group; a group whose offsets are not in order or out of range has none
-        int carry = 0;
-        for (int base = 0; base < g.G; base += 32) {
-            const int i = base + lane;
-            int b = 0, e = g.T, tiles = 0;
-            if (i < g.G && g.offset) {
-                b = load_s32(g.offset + i);
-                e = load_s32(g.offset + i + 1);
-            }
-            if (i < g.G) {
-                if (b < 0 || e < b || e > g.T) {
-                    if (blockIdx.x == 0 && g.status) atomicMax(g.status, (int)SPICE_ERR_BAD_TABLE);
-                } else {
-                    tiles = (e - b + PR_TILE - 1) / PR_TILE * g.n_tiles;
-                }
-            }
-            int incl = tiles;
-#pragma unroll
-            for (int o = 1; o < 32; o *= 2) {
-                const int v = __shfl_up_sync(0xffffffffu, incl, o);
-                if (lane >= o) incl += v;
-            }
-            if (i < g.G) sh.first[i] = carry + incl - tiles;
-            carry += __shfl_sync(0xffffffffu, incl, 31);
-        }
-        if (lane == 0) sh.first[g.G] = carry;
-    }
+    if (warp == 2) count_tiles(g, PR_TILE, sh.first);
     tc_fence_before();
     __syncthreads();
     cluster_sync();   // both CTAs' barriers exist before either signals the other's
     tc_fence_after();
     const uint32_t tmem_base = sh.tmem_base;
     const int n_tiles = sh.first[g.G];
-    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    const int pair = SPLIT ? blockIdx.x / (2 * g.split) : blockIdx.x >> 1, pairs = SPLIT ? n_tiles : gridDim.x >> 1;
+    const int kb_first = SPLIT ? g.kb * part / g.split : 0, kb_last = SPLIT ? g.kb * (part + 1) / g.split : g.kb;
 
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(PR_REGS_HELPERS));
@@ -416,10 +529,10 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
                 const int row = warp != 0 ? t.t0 + rank * 128 : SWIGLU ? (2 * t.group + rank) * g.n + t.nt * 128 : t.group * g.n + t.nt * PR_TILE + rank * 128;
                 const int x_rows = copied(t.rows, rank);
                 const uint32_t bytes = 2 * PR_HALF_BYTES + (x_rows + copied(t.rows, rank ^ 1)) * BK;
-                for (int k0 = 0; k0 < g.k; k0 += BK) {
+                for (int k0 = kb_first * BK; k0 < kb_last * BK; k0 += BK) {
                     mbar_wait_quick(empty0 + s * 8, phase, abort_flag, limit);
                     if (limit == 0) break;
-                    const uint32_t full = map_to_cta(full0 + s * 8, 0), dst = smem_u32(ring) + s * PR_STAGE_BYTES;
+                    const uint32_t full = map_to_cta(full0 + s * 8, leader), dst = smem_u32(ring) + s * PR_STAGE_BYTES;
                     if (warp == 0) {
                         if (rank == 0) mbar_expect_tx(full0 + s * 8, bytes);
                         tma_load_2d_pair(dst + PR_HALF_BYTES, &map_w, k0, row, full);
@@ -455,7 +568,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
             const uint64_t desc0 = make_desc(smem_u32(ring));
             uint32_t s = buf, phase = 0, tmem_phase = 1, limit = g.wait_limit;
             // blocks of all this pair's tiles that are this warp's
-            const uint32_t total = (uint32_t)(n_tiles > pair ? (n_tiles - pair + pairs - 1) / pairs : 0) * (uint32_t)g.kb;
+            const uint32_t total = (uint32_t)(n_tiles > pair ? (n_tiles - pair + pairs - 1) / pairs : 0) * (uint32_t)(kb_last - kb_first);
             for (uint32_t left = (total + 1 - buf) / 2; left > 0; --left) {
                 mbar_wait_quick(tmem_empty, tmem_phase, abort_flag, limit);
                 mbar_wait_quick(full0 + s * 8, phase, abort_flag, limit);
@@ -464,8 +577,8 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
                 const uint64_t da = desc0 + s * (PR_STAGE_BYTES >> 4), db = da + (PR_HALF_BYTES >> 4);
 #pragma unroll
                 for (int k = 0; k < BK / 32; ++k) tc_mma_f8_pair(d_tmem, da + 2 * k, db + 2 * k, idesc, k ? 1u : 0u);
-                tc_commit_pair(empty0 + s * 8, 3u);
-                tc_commit_pair(tmem_full, 3u);
+                tc_commit_pair(empty0 + s * 8, pair_mask);
+                tc_commit_pair(tmem_full, pair_mask);
                 tmem_phase ^= 1;
                 s += 2;
                 if (s >= PR_STAGES) {
@@ -483,7 +596,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
         // block of weight rows: a thread's sums of a block all have the same scale.
         const int q = warp & 3, h = warp >= 8 ? 1 : 0;
         const int row_blocks = ((SWIGLU ? 2 * g.n : g.n) + 127) / 128;
-        const uint32_t full0 = smem_u32(&sh.tmem_full[0]), empty0 = map_to_cta(smem_u32(&sh.tmem_empty[0]), 0);
+        const uint32_t full0 = smem_u32(&sh.tmem_full[0]), empty0 = map_to_cta(smem_u32(&sh.tmem_empty[0]), leader);
         const uint32_t tm0 = tmem_base + ((uint32_t)(q * 32) << 16) + h * (SWIGLU ? 64 : 128);
         uint32_t it = 0;
         uint32_t limit = g.wait_limit;   // 0 after an expired wait: a warp only keeps the others' barriers
@@ -498,12 +611,12 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
             uint64_t acc[64];   // two columns each
 #pragma unroll
             for (int i = 0; i < 64; ++i) acc[i] = 0;
-            float x = load_f32(xs), w = load_f32(ws), u = SWIGLU ? load_f32(wu) : 0.0f;   // a block ahead
+            float x = load_f32(xs + kb_first), w = load_f32(ws + kb_first), u = SWIGLU ? load_f32(wu + kb_first) : 0.0f;   // a block ahead
 #pragma unroll 1
-            for (int kb = 0; kb < g.kb; ++kb, ++it) {
+            for (int kb = kb_first; kb < kb_last; ++kb, ++it) {
                 const uint32_t buf = it & 1, tm = tm0 + buf * PR_TILE;
                 const float sw = x * w, su = SWIGLU ? x * u : sw;
-                const int ahead = min(kb + 1, g.kb - 1);
+                const int ahead = min(kb + 1, kb_last - 1);
                 x = load_f32(xs + ahead);
                 w = load_f32(ws + ahead);
                 if (SWIGLU) u = load_f32(wu + ahead);
@@ -528,6 +641,17 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
                 } else {
                     mbar_arrive_cluster_tmem(empty0 + buf * 8, lane);
                 }
+            }
+            if constexpr (SPLIT) {
+                // sums as [column][128 tokens] over the ring (the last products are over)
+                float *sums = reinterpret_cast<float *>(ring) + q * 32 + lane;
+#pragma unroll
+                for (int i = 0; i < 64; ++i) {
+                    const int c = 2 * i + (SWIGLU ? h * 64 + (i >= 32 ? 64 : 0) : h * 128);
+                    sums[c * 128] = low(acc[i]);
+                    sums[c * 128 + 128] = high(acc[i]);
+                }
+                continue;
             }
             // a thread writes its token's columns, whole sectors at a time
             const bool in = limit != 0 && lane < rows;
@@ -600,7 +724,64 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
     tc_fence_before();
     __syncthreads();
     if (threadIdx.x == 0 && sh.abort_flag && g.status) atomicMax(g.status, (int)SPICE_ERR_TIMEOUT);
-    cluster_sync();   // the pair's MMAs, copies and signals are over in both CTAs
+    cluster_sync();   // the pair's MMAs, copies and signals are over in both CTAs; SPLIT: everybody's sums are there
+    if constexpr (SPLIT) {
+        if (warp >= 4 && pair < n_tiles) {
+            // a warp finishes 32 columns (SwiGLU: 16 gate columns and their up columns) of 32 tokens at a time
+            const int w8 = warp - 4, c0 = SWIGLU ? w8 * 16 : w8 * 32;
+            const int quarters = 4 / g.split;
+            const bool ok = *abort_flag == 0;
+            int group = 0;
+            const Tile t = find_tile(sh, g, pair, group);
+            for (int q = part * quarters; q < (part + 1) * quarters; ++q) {
+                const int rows = t.rows - rank * 128 - q * 32;
+                if (rows <= 0) break;
+                const int row = t.t0 + rank * 128 + q * 32 + lane;
+                const uint32_t at = smem_u32(ring) + (uint32_t)(c0 * 128 + q * 32 + lane) * 4u;
+                float v[32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] = 0.0f;
+                for (int p = 0; p < g.split; ++p) {
+                    const uint32_t peer = map_to_cta(at, (uint32_t)(2 * p + rank));
+                    float o[32];
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o[i]) : "r"(peer + (uint32_t)((SWIGLU && i >= 16 ? 112 : 0) + i) * 512u));
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] += o[i];
+                }
+                if constexpr (SWIGLU) {
+                    float big = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        v[i] = silu_times(v[i], v[16 + i]);
+                        big = max_magnitude(big, v[i]);
+                    }
+                    float (*peak)[32] = reinterpret_cast<float (*)[32]>(&sh.peak[0][0]);
+                    peak[w8][lane] = big;
+                    asm volatile("bar.sync 1, 256;" ::: "memory");
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) big = max_magnitude(big, peak[i][lane]);
+                    const OutScale s(big);
+                    asm volatile("bar.sync 1, 256;" ::: "memory");   // (all have read before one writes again)
+                    if (ok && lane < rows) {
+                        uint32_t c[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) c[i] = code2(v[4 * i], v[4 * i + 1], s.r) | code2(v[4 * i + 2], v[4 * i + 3], s.r) << 16;
+                        *reinterpret_cast<uint4 *>(static_cast<uint8_t *>(g.y) + (size_t)row * g.n + t.nt * 128 + c0) = make_uint4(c[0], c[1], c[2], c[3]);
+                        if (w8 == 0) g.ys[(size_t)row * (g.n / 128) + t.nt] = s.scale;
+                    }
+                } else if (ok && lane < rows) {
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4) {
+                        const int col = t.nt * PR_TILE + c0 + i;
+                        if (col < g.n) store4(g, (size_t)row * g.n + col, make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]));
+                    }
+                }
+            }
+        }
+        cluster_sync();   // nobody leaves while a peer reads its sums
+    }
     tc_fence_after();
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512));
 }
@@ -608,45 +789,134 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
 // ------------------------------------------------------------------------------------------------ host side
 std::atomic<uint32_t> wait_limit{WAIT_LIMIT};   // (SPICE_OPT_E4M3_WAIT_LIMIT)
 
-// What a device is told once: the dynamic shared memory limits.
-bool prepare_device(int dev) {
-    static std::atomic<bool> ready[64];
-    if (ready[dev].load(std::memory_order_acquire)) return true;
-    auto raise = [](const void *kernel, size_t bytes) {
-        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess;
+template <typename F>
+void for_each_stream_kernel(F f) {
+    auto of = [&](auto nt) {
+        constexpr int NT = decltype(nt)::value;
+        f((const void *)gemm_e4m3_stream_kernel<NT, false, false>, stream_smem<NT>());
+        f((const void *)gemm_e4m3_stream_kernel<NT, true, false>, stream_smem<NT>());
+        f((const void *)gemm_e4m3_stream_kernel<NT, false, true>, stream_smem<NT>());
+        f((const void *)gemm_e4m3_stream_kernel<NT, true, true>, stream_smem<NT>());
     };
-    if (!raise((const void *)gemm_e4m3_pair_kernel<false>, PR_SMEM_BYTES) || !raise((const void *)gemm_e4m3_pair_kernel<true>, PR_SMEM_BYTES))
-        return false;
-    ready[dev].store(true, std::memory_order_release);
-    return true;
+    of(std::integral_constant<int, 1>{});
+    of(std::integral_constant<int, 2>{});
+    of(std::integral_constant<int, 4>{});
+}
+
+// What a device is asked once: dynamic shared memory limits are raised, and how many clusters of c CTAs run at the same time when
+// an SM holds one CTA.
+struct DeviceFacts {
+    std::atomic<bool> ready;
+    int clusters[ST_MAX_SPLIT + 1];
+};
+const DeviceFacts *device_facts(int dev, int sms) {
+    static DeviceFacts facts[64];
+    static std::mutex mutex;
+    DeviceFacts &f = facts[dev];
+    if (f.ready.load(std::memory_order_acquire)) return &f;
+    std::lock_guard<std::mutex> lock(mutex);
+    if (f.ready.load(std::memory_order_relaxed)) return &f;
+    bool ok = true;
+    auto raise = [&](const void *kernel, size_t bytes) {
+        ok = ok && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == cudaSuccess;
+    };
+    for_each_stream_kernel(raise);
+    raise((const void *)gemm_e4m3_pair_kernel<false, false>, PR_SMEM_BYTES);
+    raise((const void *)gemm_e4m3_pair_kernel<true, false>, PR_SMEM_BYTES);
+    raise((const void *)gemm_e4m3_pair_kernel<false, true>, PR_SMEM_BYTES);
+    raise((const void *)gemm_e4m3_pair_kernel<true, true>, PR_SMEM_BYTES);
+    for (int c = 2; ok && c <= ST_MAX_SPLIT; c *= 2) {   // (the larger of the two kernels)
+        cudaLaunchConfig_t lc{};
+        lc.gridDim = dim3((unsigned)(c * sms), 1, 1);
+        lc.blockDim = dim3(PR_THREADS, 1, 1);
+        lc.dynamicSmemBytes = PR_SMEM_BYTES;
+        cudaLaunchAttribute at[1];
+        at[0].id = cudaLaunchAttributeClusterDimension;
+        at[0].val.clusterDim.x = (unsigned)c;
+        at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+        lc.attrs = at;
+        lc.numAttrs = 1;
+        ok = cudaOccupancyMaxActiveClusters(&f.clusters[c], gemm_e4m3_pair_kernel<false, true>, &lc) == cudaSuccess;
+    }
+    if (!ok) return nullptr;
+    f.ready.store(true, std::memory_order_release);
+    return &f;
+}
+
+template <int NT, bool SWIGLU>
+bool launch_stream(GemmE4m3Args g, const CUtensorMap &map_w, const uint8_t *x, int64_t most, const DeviceFacts *facts, int sms, cudaStream_t st) {
+    CUtensorMap map_x;
+    if (!tc_encode_map2_bytes(&map_x, x, (uint64_t)g.T, (uint64_t)g.k, StreamShape<NT>::TOKENS)) return false;
+    // a cluster takes one item, so all of them have to run at once
+    g.split = 1;
+    for (int c = 2; c <= ST_MAX_SPLIT; c *= 2)
+        if (most <= facts->clusters[c] && g.kb >= 2 * c) g.split = c;
+    if (g.split > 1)
+        return launch_early(gemm_e4m3_stream_kernel<NT, SWIGLU, true>, dim3((unsigned)(most * g.split)), ST_THREADS, stream_smem<NT>(), st, g.split, map_w, map_x, g);
+    return launch_early(gemm_e4m3_stream_kernel<NT, SWIGLU, false>, dim3((unsigned)std::min<int64_t>(sms, most)), ST_THREADS, stream_smem<NT>(), st, 1, map_w,
+                        map_x, g);
 }
 
 template <bool SWIGLU>
 spice_status launch_gemm_e4m3(GemmE4m3Args g, const uint8_t *x, const uint8_t *w, cudaStream_t st) {
     int dev = 0;
     const int sms = current_device_sms(&dev);
-    if (sms <= 0 || !prepare_device(dev)) return SPICE_ERR_CUDA;
+    if (sms <= 0) return SPICE_ERR_CUDA;
+    const DeviceFacts *facts = device_facts(dev, sms);
+    if (!facts) return SPICE_ERR_CUDA;
     const int w_rows = SWIGLU ? 2 * g.n : g.n;
     const int used = std::min(g.G, g.T);   // groups that can have rows
     const int rows = (g.T + used - 1) / used;
-    if (rows <= 16) {
-        const dim3 grid((unsigned)((g.n + 15) / 16), (unsigned)used);
-        auto *kernel = rows <= 4 ? gemm_e4m3_few_kernel<1, SWIGLU> : gemm_e4m3_few_kernel<2, SWIGLU>;
-        return launch_early(kernel, grid, FEW_WARPS * 32, 0, st, SWIGLU ? FEW_CLUSTER : 1, x, w, g) ? SPICE_OK : SPICE_ERR_CUDA;
+    // Few rows: streamed weights, at the rate of HBM as long as the warp-wide products (400 per cycle and SM) keep up.  Streamed / by
+    // pairs of CTAs, us, dense 2048 x 2816, 3584 x 20480, SwiGLU 5632 x 2048:  16 tokens 6.8/12.4, 18.9/29, 8.1/13;  32 tokens 9.6/13,
+    // 28.9/30.8, 11.1/12.9;  64 tokens 14.7/14.7, 56/34, 19.4/13.4.  64 groups of 2048 x 1408, SwiGLU 2816 x 2048:  96 rows 34.6/49,
+    // 65/94;  400 rows 38.8/50, 80/103;  768 rows 57/51, 116/103.
+    if (g.G == 1 ? g.T <= 32 : rows <= 8) {
+        CUtensorMap map_w;
+        if (!tc_encode_map2_bytes(&map_w, w, (uint64_t)g.G * w_rows, (uint64_t)g.k, 128)) return SPICE_ERR_CUDA;
+        g.n_tiles = SWIGLU ? g.n / 128 : (g.n + 255) / 256;
+        auto most = [&](int tokens) {   // items there can be
+            return g.G == 1 ? (int64_t)((g.T + tokens - 1) / tokens) * g.n_tiles : ((int64_t)g.T / tokens + used) * g.n_tiles;
+        };
+        if (most(8) > 0x3fffffff) return SPICE_ERR_UNSUPPORTED_SHAPE;
+        const int wide = g.G == 1 ? g.T : 2 * rows;   // (groups have unequal shares; a large one takes several items)
+        const bool ok = wide <= 8 ? launch_stream<1, SWIGLU>(g, map_w, x, most(8), facts, sms, st)
+                        : wide <= 16 ? launch_stream<2, SWIGLU>(g, map_w, x, most(16), facts, sms, st)
+                                     : launch_stream<4, SWIGLU>(g, map_w, x, most(32), facts, sms, st);
+        return ok ? SPICE_OK : SPICE_ERR_CUDA;
     }
     g.n_tiles = SWIGLU ? g.n / 128 : (g.n + PR_TILE - 1) / PR_TILE;
     const int row_bytes = SWIGLU ? 1 : g.out == SPICE_OUT_BF16 ? 2 : 4;
     g.sectors = ((reinterpret_cast<uintptr_t>(g.y) | (uintptr_t)g.n * row_bytes) & 31u) == 0;
-    const int64_t most = ((int64_t)g.T / PR_TILE + g.G) * g.n_tiles;   // tiles there can be
+    const int64_t most = (g.G == 1 ? ((int64_t)g.T + PR_TILE - 1) / PR_TILE : (int64_t)g.T / PR_TILE + used) * g.n_tiles;   // tiles there can be
     if (most > 0x3fffffff) return SPICE_ERR_UNSUPPORTED_SHAPE;
     CUtensorMap map_w, map_x128, map_x16;
     if (!tc_encode_map2_bytes(&map_w, w, (uint64_t)g.G * w_rows, (uint64_t)g.k, 128) ||
         !tc_encode_map2_bytes(&map_x128, x, (uint64_t)g.T, (uint64_t)g.k, 128) ||
         !tc_encode_map2_bytes(&map_x16, x, (uint64_t)g.T, (uint64_t)g.k, 16))
         return SPICE_ERR_CUDA;
-    const int pairs = (int)std::min<int64_t>(sms / 2, most);
-    return launch_early(gemm_e4m3_pair_kernel<SWIGLU>, dim3(2 * (unsigned)pairs), PR_THREADS, PR_SMEM_BYTES, st, 2, map_w, map_x128, map_x16,
-                        g) ? SPICE_OK : SPICE_ERR_CUDA;
+    // Fewer tiles than pairs: two or four pairs share a tile's reduction, as long as all the clusters run at once and the reduction is
+    // long: 470 ns a block against a start of 4.5 us, or 12 with the sums of the cluster (77 x 3584 x 20480 with one / two / four
+    // pairs to a tile: 82 / 52 / 34.5 us; 77 x 2048 x 2816 15.5 / 16.4 / 15.6).
+    int share = 1;
+    int64_t best = 4500 + 470 * (int64_t)g.kb;
+    for (int s = 2; s <= 4 && g.G == 1; s *= 2) {
+        const int64_t ns = 12000 + 470 * (int64_t)((g.kb + s - 1) / s);
+        if (most <= facts->clusters[2 * s] && ns < best) {
+            best = ns;
+            share = s;
+        }
+    }
+    bool ok;
+    if (share > 1) {
+        g.split = share;
+        ok = launch_early(gemm_e4m3_pair_kernel<SWIGLU, true>, dim3((unsigned)(2 * share * most)), PR_THREADS, PR_SMEM_BYTES, st, 2 * share, map_w, map_x128,
+                          map_x16, g);
+    } else {
+        const int pairs = (int)std::min<int64_t>(sms / 2, most);
+        ok = launch_early(gemm_e4m3_pair_kernel<SWIGLU, false>, dim3(2 * (unsigned)pairs), PR_THREADS, PR_SMEM_BYTES, st, 2, map_w, map_x128, map_x16, g);
+    }
+    return ok ? SPICE_OK : SPICE_ERR_CUDA;
 }
 
 bool misaligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
