@@ -37,6 +37,11 @@ __device__ __forceinline__ uint4 load16(const uint4 *p) {   // (not as constant:
     asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
     return v;
 }
+__device__ __forceinline__ uint4 load16_once(const uint4 *p) {   // (nobody reads it again)
+    uint4 v;
+    asm volatile("ld.global.cs.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
 __device__ __forceinline__ int32_t load4(const int32_t *p) {
     int32_t v;
     asm volatile("ld.global.s32 %0, [%1];" : "=r"(v) : "l"(p));
@@ -134,18 +139,18 @@ __global__ void __launch_bounds__(SMALL_THREADS) sort_small_kernel(const SortArg
 // ------------------------------------------------------------------------------------------------ many entries
 // A cluster counts: each of its warps owns a run of consecutive entries and a row of counters in shared memory; a first pass
 // counts, prefix sums over experts, blocks and warps turn the counters into places, a second pass hands the places out.
-constexpr int SORT_CTAS = 8, SORT_THREADS = 1024, SORT_WARPS = SORT_THREADS / 32;
+constexpr int SORT_CTAS = 8, SORT_THREADS = 1024, SORT_WARPS = SORT_THREADS / 32, SORT_KEPT = 8;
 
 __global__ void __launch_bounds__(SORT_THREADS, 1) sort_cluster_kernel(const SortArgs a) {
     extern __shared__ int32_t smem[];
-    int32_t *mine = smem;                          // [warps][N] counters
-    int32_t *total = smem + SORT_WARPS * a.N;      // [N] of this block
+    const int pitch = a.N | 1;                     // (odd: a column of counters falls into different banks)
+    int32_t *mine = smem;                          // [warps][pitch] counters
+    int32_t *total = smem + SORT_WARPS * pitch;    // [N] of this block
     __shared__ int32_t part[SORT_WARPS];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cta = blockIdx.x;
-    int32_t *own = mine + warp * a.N;
+    int32_t *own = mine + warp * pitch;
+    for (int i = lane; i < a.N; i += 32) own[i] = 0;
     grid_dependency();
-    for (int i = threadIdx.x; i < SORT_WARPS * a.N; i += SORT_THREADS) mine[i] = 0;
-    __syncthreads();
     const int share = (((a.n + SORT_CTAS * SORT_WARPS - 1) / (SORT_CTAS * SORT_WARPS)) + 31) & ~31;
     const int64_t from = (int64_t)(cta * SORT_WARPS + warp) * share;
     const int first = (int)min(from, (int64_t)a.n), last = (int)min(from + share, (int64_t)a.n);
@@ -153,21 +158,34 @@ __global__ void __launch_bounds__(SORT_THREADS, 1) sort_cluster_kernel(const Sor
         const int v = i < last ? load4(a.idx + i) : -1;
         return v >= 0 && v < a.N ? v : -1;
     };
-    for (int i = first; i < last; i += 32) {
-        const int e = expert(i + lane);
-        const uint32_t same = __match_any_sync(0xffffffffu, e);
-        if (e >= 0 && (same & ((1u << lane) - 1)) == 0) own[e] += __popc(same);
+    // the first entries of a warp stay in registers for the second pass
+    int e[SORT_KEPT];
+#pragma unroll
+    for (int u = 0; u < SORT_KEPT; ++u) e[u] = expert(first + u * 32 + lane);
+    __syncwarp();
+    uint32_t kept_same[SORT_KEPT];
+    auto count = [&](int v) {
+        const uint32_t same = __match_any_sync(0xffffffffu, v);
+        if (v >= 0 && (same & ((1u << lane) - 1)) == 0) own[v] += __popc(same);
         __syncwarp();
-    }
+        return same;
+    };
+#pragma unroll
+    for (int u = 0; u < SORT_KEPT; ++u)
+        if (first + u * 32 < last) kept_same[u] = count(e[u]);
+    for (int i = first + SORT_KEPT * 32; i < last; i += 32) count(expert(i + lane));
     __syncthreads();
-    if (threadIdx.x < a.N) {                       // counters of an expert: what the warps before have
-        int sum = 0;
-        for (int w = 0; w < SORT_WARPS; ++w) {
-            const int c = mine[w * a.N + threadIdx.x];
-            mine[w * a.N + threadIdx.x] = sum;
-            sum += c;
+    // counters of an expert: what the warps before have
+    for (int x = warp; x < a.N; x += SORT_WARPS) {
+        const int c = mine[lane * pitch + x];
+        int incl = c;
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const int v = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += v;
         }
-        total[threadIdx.x] = sum;
+        mine[lane * pitch + x] = incl - c;
+        if (lane == 31) total[x] = incl;
     }
     tcdev::cluster_sync();
     int before = 0, all = 0;                       // entries of this thread's expert in earlier blocks, and in all
@@ -189,39 +207,62 @@ __global__ void __launch_bounds__(SORT_THREADS, 1) sort_cluster_kernel(const Sor
     }
     if (lane == 31) part[warp] = incl;
     tcdev::cluster_sync();                         // (also: nobody's totals are needed any more)
-    int base = incl - all, kept = 0;
-    for (int w = 0; w < SORT_WARPS; ++w) {
-        if (w < warp) base += part[w];
-        kept += part[w];
-    }
+    const int sums = part[lane];
+    const int n_kept = warp_sum(sums), base = incl - all + warp_sum(lane < warp ? sums : 0);
     if (threadIdx.x < a.N) {
         if (cta == 0) a.offset[threadIdx.x] = base;
         total[threadIdx.x] = base + before;
     }
-    if (cta == 0 && threadIdx.x == 0) a.offset[a.N] = kept;
+    if (cta == 0 && threadIdx.x == 0) a.offset[a.N] = n_kept;
     __syncthreads();
-    for (int i = first; i < last; i += 32) {
-        const int e = expert(i + lane);
-        const uint32_t same = __match_any_sync(0xffffffffu, e), below = same & ((1u << lane) - 1);
-        const int c = e >= 0 ? own[e] : 0;
+    auto place = [&](int i, int v, uint32_t same) {
+        const uint32_t below = same & ((1u << lane) - 1);
+        const int c = v >= 0 ? own[v] : 0;
         __syncwarp();
-        if (e >= 0 && below == 0) own[e] = c + __popc(same);
+        if (v >= 0 && below == 0) own[v] = c + __popc(same);
         __syncwarp();
-        if (i + lane < last) {
-            const int p = e >= 0 ? total[e] + c + __popc(below) : -1;
-            a.pos[i + lane] = p;
-            if (p >= 0) a.entry[p] = i + lane;
+        if (i < last) {
+            const int p = v >= 0 ? total[v] + c + __popc(below) : -1;
+            a.pos[i] = p;
+            if (p >= 0) a.entry[p] = i;
         }
+    };
+#pragma unroll
+    for (int u = 0; u < SORT_KEPT; ++u)
+        if (first + u * 32 < last) place(first + u * 32 + lane, e[u], kept_same[u]);
+    for (int i = first + SORT_KEPT * 32; i < last; i += 32) {
+        const int v = expert(i + lane);
+        place(i + lane, v, __match_any_sync(0xffffffffu, v));
     }
-    for (int i = kept + cta * SORT_THREADS + threadIdx.x; i < a.n; i += SORT_CTAS * SORT_THREADS) a.entry[i] = -1;
+    for (int i = n_kept + cta * SORT_THREADS + threadIdx.x; i < a.n; i += SORT_CTAS * SORT_THREADS) a.entry[i] = -1;
 }
 
+// A thread has one 16-byte piece (or scale) of a token.
 __global__ void __launch_bounds__(256) gather_kernel(const SortArgs a) {
-    __shared__ int32_t place[32];
     grid_dependency();
-    if (threadIdx.x < a.K) place[threadIdx.x] = load4(a.pos + (size_t)blockIdx.x * a.K + threadIdx.x);
-    __syncthreads();
-    gather_row(a, blockIdx.x, place);
+    const int per = a.vecs + a.ns;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= (int64_t)a.T * per) return;
+    const int t = (int)(i / per), v = (int)(i - (int64_t)t * per);
+    const int32_t *pos = a.pos + (size_t)t * a.K;
+    constexpr int U = 8;
+    if (v < a.vecs) {
+        const uint4 x = load16(a.x + (size_t)t * a.vecs + v);
+        for (int k0 = 0; k0 < a.K; k0 += U) {
+            int p[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) p[u] = k0 + u < a.K ? load4(pos + k0 + u) : -1;
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (p[u] >= 0) a.rows[(size_t)p[u] * a.vecs + v] = x;
+        }
+    } else {
+        const float x = load4(a.xs + (size_t)t * a.ns + v - a.vecs);
+        for (int k = 0; k < a.K; ++k) {
+            const int p = load4(pos + k);
+            if (p >= 0) a.rs[(size_t)p * a.ns + v - a.vecs] = x;
+        }
+    }
 }
 
 // ------------------------------------------------------------------------------------------------ back
@@ -237,6 +278,11 @@ struct CombineRowsArgs {
 template <bool F32>
 struct Eight {
     uint4 v[F32 ? 2 : 1];
+    __device__ __forceinline__ void load_once(const void *p, size_t at) {
+        const uint4 *q = reinterpret_cast<const uint4 *>(static_cast<const char *>(p) + at * (F32 ? 4 : 2));
+        v[0] = load16_once(q);
+        if constexpr (F32) v[1] = load16_once(q + 1);
+    }
     __device__ __forceinline__ void load(const void *p, size_t at) {
         const uint4 *q = reinterpret_cast<const uint4 *>(static_cast<const char *>(p) + at * (F32 ? 4 : 2));
         v[0] = load16(q);
@@ -263,9 +309,11 @@ __device__ __forceinline__ void store8(void *p, size_t at, const float (&f)[8]) 
     }
 }
 
-// A thread sums eight columns of a token; the rows of four entries are on their way at once.
-template <bool F32>
-__global__ void __launch_bounds__(256) combine_rows_kernel(const CombineRowsArgs a) {
+// A thread sums eight columns of a token; the rows of U entries are on their way at once.  Many tokens: two and as many blocks as fit
+// (4096 x 6 x 2048: 19.7 us, 0.92 of the measured copy rate; six and five blocks 20.4; with the rows kept in L2 22 to 25).  Few: the
+// shortest chain (17 x 8 x 3584: 2.0 us, with two at a time 2.6).
+template <bool F32, int U>
+__global__ void __launch_bounds__(256, U == 2 ? (F32 ? 5 : 8) : 1) combine_rows_kernel(const CombineRowsArgs a) {
     grid_dependency();
     const int t = blockIdx.x, col = (blockIdx.y * blockDim.x + threadIdx.x) * 8;
     if (col >= a.d) return;
@@ -274,7 +322,6 @@ __global__ void __launch_bounds__(256) combine_rows_kernel(const CombineRowsArgs
     float f[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) f[j] = 0.0f;
-    constexpr int U = 4;
     for (int k0 = 0; k0 < a.K; k0 += U) {
         Eight<F32> r[U];
         float g[U];
@@ -284,7 +331,7 @@ __global__ void __launch_bounds__(256) combine_rows_kernel(const CombineRowsArgs
             const int p = k0 + u < a.K ? load4(pos + k0 + u) : -1;
             in[u] = p >= 0 && p < a.n_rows;
             g[u] = in[u] && gate ? load4(gate + k0 + u) : 1.0f;
-            if (in[u]) r[u].load(a.rows, (size_t)p * a.d + col);
+            if (in[u]) r[u].load_once(a.rows, (size_t)p * a.d + col);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
@@ -317,52 +364,99 @@ struct CombineGradArgs {
     int32_t n, K, d, n_rows;
 };
 
-// W warps per entry: its row of the gradient, and the product of dy with its row.
-template <int W, bool DY32, bool ROW32>
-__global__ void __launch_bounds__(256) combine_grad_kernel(const CombineGradArgs a) {
+// A block per entry, for few of them: its row of the gradient, and the product of dy with its row.
+template <bool DY32, bool ROW32>
+__global__ void __launch_bounds__(256) grad_entry_kernel(const CombineGradArgs a) {
     __shared__ float part[8];
     grid_dependency();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int i = W == 1 ? blockIdx.x * 8 + warp : blockIdx.x;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, i = blockIdx.x;
+    const int p = load4(a.pos + i);
     float sum = 0.0f;
-    if (i < a.n) {
-        const int p = load4(a.pos + i);
-        if (p >= 0 && p < a.n_rows) {
-            const float g = a.gate ? load4(a.gate + i) : 1.0f;
-            const size_t from = (size_t)(i / a.K) * a.d, to = (size_t)p * a.d;
-            const int step = (W == 1 ? 32 : 256) * 8;
+    if (p >= 0 && p < a.n_rows) {
+        const float g = a.gate ? load4(a.gate + i) : 1.0f;
+        const size_t from = (size_t)(i / a.K) * a.d, to = (size_t)p * a.d;
 #pragma unroll 4
-            for (int col = (W == 1 ? lane : threadIdx.x) * 8; col < a.d; col += step) {
-                Eight<DY32> dy;
-                Eight<ROW32> r;
-                dy.load(a.dy, from + col);
-                if (a.d_gate) r.load(a.rows, to + col);
-                if (a.d_rows) {
-                    float f[8];
+        for (int col = threadIdx.x * 8; col < a.d; col += 256 * 8) {
+            Eight<DY32> dy;
+            Eight<ROW32> r;
+            dy.load(a.dy, from + col);
+            if (a.d_gate) r.load(a.rows, to + col);
+            if (a.d_rows) {
+                float f[8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) f[j] = g * dy[j];
-                    store8<ROW32>(a.d_rows, to + col, f);
-                }
-                if (a.d_gate) {
+                for (int j = 0; j < 8; ++j) f[j] = g * dy[j];
+                store8<ROW32>(a.d_rows, to + col, f);
+            }
+            if (a.d_gate) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) sum = fmaf(dy[j], r[j], sum);
-                }
+                for (int j = 0; j < 8; ++j) sum = fmaf(dy[j], r[j], sum);
             }
         }
     }
     if (!a.d_gate) return;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if constexpr (W == 1) {
-        if (lane == 0 && i < a.n) a.d_gate[i] = sum;
-    } else {
-        if (lane == 0) part[warp] = sum;
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            float s = 0.0f;
-            for (int w = 0; w < 8; ++w) s += part[w];
-            a.d_gate[i] = s;
+    if (lane == 0) part[warp] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        float s = 0.0f;
+        for (int w = 0; w < 8; ++w) s += part[w];
+        a.d_gate[i] = s;
+    }
+}
+
+// A block per token, for many: dy is read once for all of the token's entries, three of which are on their way at once, with as many
+// blocks as fit (4096 x 6 x 2048: 35.8 us, 0.94 of the measured copy rate; four at a time and five blocks 43).
+template <bool DY32, bool ROW32>
+__global__ void __launch_bounds__(256, ROW32 || DY32 ? 4 : 8) grad_token_kernel(const CombineGradArgs a) {
+    __shared__ float part[8][32];
+    grid_dependency();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t = blockIdx.x;
+    const int32_t *pos = a.pos + (size_t)t * a.K;
+    const float *gate = a.gate ? a.gate + (size_t)t * a.K : nullptr;
+    for (int c0 = 0; c0 < a.d; c0 += blockDim.x * 8) {
+        const int col = c0 + threadIdx.x * 8;
+        const bool in = col < a.d;
+        Eight<DY32> dy;
+        if (in) dy.load(a.dy, (size_t)t * a.d + col);
+        constexpr int U = ROW32 ? 2 : 3;
+        for (int k0 = 0; k0 < a.K; k0 += U) {
+            Eight<ROW32> r[U];
+            int p[U];
+            float g[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                p[u] = k0 + u < a.K ? load4(pos + k0 + u) : -1;
+                p[u] = p[u] < a.n_rows ? p[u] : -1;
+                g[u] = gate && k0 + u < a.K ? load4(gate + k0 + u) : 1.0f;
+                if (in && p[u] >= 0 && a.d_gate) r[u].load(a.rows, (size_t)p[u] * a.d + col);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (in && p[u] >= 0 && a.d_rows) {
+                    float f[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) f[j] = g[u] * dy[j];
+                    store8<ROW32>(a.d_rows, (size_t)p[u] * a.d + col, f);
+                }
+                if (!a.d_gate || k0 + u >= a.K) continue;
+                float sum = 0.0f;
+                if (in && p[u] >= 0) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) sum = fmaf(dy[j], r[u][j], sum);
+                }
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                if (lane == 0) part[warp][k0 + u] = c0 ? part[warp][k0 + u] + sum : sum;
+            }
         }
+    }
+    if (!a.d_gate) return;
+    __syncthreads();
+    if (threadIdx.x < a.K) {
+        float s = 0.0f;
+        for (int w = 0; w < (int)blockDim.x / 32; ++w) s += part[w][threadIdx.x];
+        a.d_gate[(size_t)t * a.K + threadIdx.x] = s;
     }
 }
 
@@ -390,13 +484,15 @@ extern "C" spice_status spice_sort_tokens(const int32_t *idx, int32_t T, int32_t
         misaligned4(x_scale) || misaligned4(rows_scale))
         return SPICE_ERR_INVALID_ARG;
     const SortArgs a{idx, offset, pos, entry, T, top_k, n_experts, T * top_k, static_cast<const uint4 *>(x), static_cast<uint4 *>(rows),
-                     row_bytes / 16, x_scale, rows_scale, scale_cols};
+                     x ? row_bytes / 16 : 0, x_scale, rows_scale, x_scale ? scale_cols : 0};
     if (a.n <= SMALL_N) return launch_early(sort_small_kernel, dim3((unsigned)T), SMALL_THREADS, 0, st, 1, a) ? SPICE_OK : SPICE_ERR_CUDA;
-    const size_t smem = (size_t)(SORT_WARPS + 1) * n_experts * 4;
+    const int64_t gather_blocks = ((int64_t)T * (a.vecs + a.ns) + 255) / 256;
+    if (gather_blocks > 0x7fffffffLL) return SPICE_ERR_UNSUPPORTED_SHAPE;
+    const size_t smem = (size_t)(SORT_WARPS * (n_experts | 1) + n_experts) * 4;
     if (smem > 48 * 1024 && cudaFuncSetAttribute(sort_cluster_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
         return SPICE_ERR_CUDA;
     if (!launch_early(sort_cluster_kernel, dim3(SORT_CTAS), SORT_THREADS, smem, st, SORT_CTAS, a)) return SPICE_ERR_CUDA;
-    if (rows && !launch_early(gather_kernel, dim3((unsigned)T), 256, 0, st, 1, a)) return SPICE_ERR_CUDA;
+    if (rows && !launch_early(gather_kernel, dim3((unsigned)gather_blocks), 256, 0, st, 1, a)) return SPICE_ERR_CUDA;
     return SPICE_OK;
 }
 
@@ -413,7 +509,11 @@ extern "C" spice_status spice_combine_tokens(const void *rows, int32_t rows_type
     const CombineRowsArgs a{rows, pos, gate, y, top_k, d, n_rows, out};
     const int vecs = d / 8, threads = std::min(256, (vecs + 31) & ~31);
     const dim3 grid((unsigned)T, (unsigned)((vecs + threads - 1) / threads));
-    auto *kernel = rows_type == SPICE_OUT_F32 ? combine_rows_kernel<true> : combine_rows_kernel<false>;
+    const int sms = current_device_sms();
+    if (sms <= 0) return SPICE_ERR_CUDA;
+    const bool many = (int64_t)grid.x * grid.y >= 4 * sms;
+    auto *kernel = rows_type == SPICE_OUT_F32 ? (many ? combine_rows_kernel<true, 2> : combine_rows_kernel<true, 4>)
+                                              : (many ? combine_rows_kernel<false, 2> : combine_rows_kernel<false, 8>);
     return launch_early(kernel, grid, threads, 0, static_cast<cudaStream_t>(stream), 1, a) ? SPICE_OK : SPICE_ERR_CUDA;
 }
 
@@ -431,12 +531,15 @@ extern "C" spice_status spice_combine_tokens_grad(const void *dy, int32_t dy_typ
         return SPICE_ERR_INVALID_ARG;
     const CombineGradArgs a{dy, rows, pos, gate, d_rows, d_gate, T * top_k, top_k, d, n_rows};
     if (!d_rows && !d_gate) return SPICE_OK;   // (no rows)
-    const bool wide = a.n < 1024;   // few entries: a block for each
     const bool d32 = dy_type == SPICE_OUT_F32, r32 = rows_type == SPICE_OUT_F32;
-    auto *kernel = wide ? (d32 ? (r32 ? combine_grad_kernel<8, true, true> : combine_grad_kernel<8, true, false>)
-                               : (r32 ? combine_grad_kernel<8, false, true> : combine_grad_kernel<8, false, false>))
-                        : (d32 ? (r32 ? combine_grad_kernel<1, true, true> : combine_grad_kernel<1, true, false>)
-                               : (r32 ? combine_grad_kernel<1, false, true> : combine_grad_kernel<1, false, false>));
-    const unsigned blocks = (unsigned)(wide ? a.n : (a.n + 7) / 8);
-    return launch_early(kernel, dim3(blocks), 256, 0, static_cast<cudaStream_t>(stream), 1, a) ? SPICE_OK : SPICE_ERR_CUDA;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (a.n < 2048) {
+        auto *kernel = d32 ? (r32 ? grad_entry_kernel<true, true> : grad_entry_kernel<true, false>)
+                           : (r32 ? grad_entry_kernel<false, true> : grad_entry_kernel<false, false>);
+        return launch_early(kernel, dim3((unsigned)a.n), 256, 0, st, 1, a) ? SPICE_OK : SPICE_ERR_CUDA;
+    }
+    auto *kernel = d32 ? (r32 ? grad_token_kernel<true, true> : grad_token_kernel<true, false>)
+                       : (r32 ? grad_token_kernel<false, true> : grad_token_kernel<false, false>);
+    const int threads = std::min(256, (d / 8 + 31) & ~31);
+    return launch_early(kernel, dim3((unsigned)T), threads, 0, st, 1, a) ? SPICE_OK : SPICE_ERR_CUDA;
 }
