@@ -440,7 +440,7 @@ __global__ void __launch_bounds__(ST_THREADS, 1)
 
 // ------------------------------------------------------------------------------------------------ more rows
 constexpr int PR_THREADS = 384, PR_EPI_WARPS = 8;
-constexpr uint32_t PR_STAGES = 6;
+constexpr uint32_t PR_STAGES = 4;                // (six are no faster)
 constexpr int PR_TILE = 256;                      // tokens of a pair's tile (128 per CTA), and its accumulator columns
 constexpr int PR_HALF_BYTES = 128 * BK;           // a CTA's half of one operand
 constexpr int PR_STAGE_BYTES = 2 * PR_HALF_BYTES;
@@ -456,7 +456,9 @@ struct PairShared {
     uint32_t tmem_base;
     int abort_flag;
 };
-constexpr size_t PR_SMEM_BYTES = sizeof(PairShared) + (size_t)PR_STAGES * PR_STAGE_BYTES + 1024;
+constexpr int PR_OUT_WARP = 32 * 256;             // an epilogue warp's results on their way out: two boxes of 32 rows x 128 bytes
+constexpr size_t PR_SMEM_BYTES = sizeof(PairShared) + (size_t)PR_STAGES * PR_STAGE_BYTES + PR_EPI_WARPS * PR_OUT_WARP + 1024;
+static_assert(PR_TILE * 128 * 4 <= PR_STAGES * PR_STAGE_BYTES, "the sums of a shared tile fit in the ring");
 static_assert(PR_SMEM_BYTES <= 232448, "what a block can have");
 
 // Tiles are numbered group by group; within a group sweeps of up to PR_GROUP_M token tiles, the token tile fastest, so that
@@ -479,10 +481,11 @@ __device__ __forceinline__ int copied(int rows, int rank) { return (min(max(rows
 template <bool SWIGLU, bool SPLIT>
 __global__ void __launch_bounds__(PR_THREADS, 1)
     gemm_e4m3_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x128,
-                          const __grid_constant__ CUtensorMap map_x16, const GemmE4m3Args g) {
+                          const __grid_constant__ CUtensorMap map_x16, const __grid_constant__ CUtensorMap map_y, const GemmE4m3Args g) {
     extern __shared__ __align__(16) unsigned char smem_raw[];   // (aligned to 1024 by hand: the swizzled tiles)
     unsigned char *ring = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    PairShared &sh = *reinterpret_cast<PairShared *>(ring + PR_STAGES * PR_STAGE_BYTES);
+    unsigned char *out = ring + PR_STAGES * PR_STAGE_BYTES;
+    PairShared &sh = *reinterpret_cast<PairShared *>(out + PR_EPI_WARPS * PR_OUT_WARP);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)(cluster_rank() & 1u), part = SPLIT ? (int)(cluster_rank() >> 1) : 0;
     const uint32_t leader = 2 * part, pair_mask = 3u << leader;
@@ -629,7 +632,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
                         const int off = (SWIGLU && ch >= 4 ? 64 : 0) + ch * 16;
                         tc_ld16(tm + off, v);
                         tc_wait_ld();
-                        asm volatile("" : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]));
+                        tc_pin16(v);
                         if (ch == 7) {   // the last columns are in registers: the buffer is free
                             tc_fence_before();
                             mbar_arrive_cluster_tmem(empty0 + buf * 8, lane);
@@ -653,7 +656,6 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
                 }
                 continue;
             }
-            // a thread writes its token's columns, whole sectors at a time
             const bool in = limit != 0 && lane < rows;
             if constexpr (SWIGLU) {
                 // activations into the gate columns' sums; a block is the columns of both warps of the quarter
@@ -680,6 +682,45 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
                             c[i] = code2(low(a), high(a), s.r) | code2(low(b), high(b), s.r) << 16;
                         }
                         store_sector(to + k * 32, c, g.sectors);
+                    }
+                }
+            } else if (limit != 0 && rows >= 32 && g.out != SPICE_OUT_F32_ADD) {
+                // 32 whole rows go out by copies from shared memory, 128 bytes of them at a time (rows of 128 bytes, pieces swizzled
+                // by the row), while the next tile is multiplied: stored by the threads themselves a tile's end took 1.5 us longer
+                const int col0 = t.nt * PR_TILE + h * 128, size = g.out == SPICE_OUT_BF16 ? 2 : 4;
+                const uint32_t to = smem_u32(out) + (uint32_t)(warp - 4) * PR_OUT_WARP, at = to + lane * 128;
+#pragma unroll
+                for (int z = 0; z < 2; ++z) {
+                    if (g.out == SPICE_OUT_BF16 && z) break;     // (fp32: half of the columns at a time)
+                    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                    __syncwarp();
+#pragma unroll
+                    for (int b = 0; b < 2; ++b)
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            uint32_t v[4];
+                            if (g.out == SPICE_OUT_BF16) {
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) v[i] = pack2(low(acc[b * 32 + k * 4 + i]), high(acc[b * 32 + k * 4 + i]));
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < 2; ++i) {
+                                    const uint64_t a = acc[z * 32 + b * 16 + k * 2 + i];
+                                    v[2 * i] = (uint32_t)a;
+                                    v[2 * i + 1] = (uint32_t)(a >> 32);
+                                }
+                            }
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + b * 4096 + ((uint32_t)(k ^ (lane & 7)) << 4)), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+                        }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) {
+                        const int x0 = col0 * size + z * 256;
+                        for (int b = 0; b < 2; ++b)
+                            if (x0 + b * 128 < g.n * size)
+                                asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];"
+                                             ::"l"(reinterpret_cast<uint64_t>(&map_y)), "r"(x0 + b * 128), "r"(row), "r"(to + b * 4096) : "memory");
+                        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                     }
                 }
             } else if (in) {
@@ -721,6 +762,7 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
             }
         }
     }
+    if (warp >= 4 && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");   // (results on their way out)
     tc_fence_before();
     __syncthreads();
     if (threadIdx.x == 0 && sh.abort_flag && g.status) atomicMax(g.status, (int)SPICE_ERR_TIMEOUT);
@@ -890,10 +932,11 @@ spice_status launch_gemm_e4m3(GemmE4m3Args g, const uint8_t *x, const uint8_t *w
     g.sectors = ((reinterpret_cast<uintptr_t>(g.y) | (uintptr_t)g.n * row_bytes) & 31u) == 0;
     const int64_t most = (g.G == 1 ? ((int64_t)g.T + PR_TILE - 1) / PR_TILE : (int64_t)g.T / PR_TILE + used) * g.n_tiles;   // tiles there can be
     if (most > 0x3fffffff) return SPICE_ERR_UNSUPPORTED_SHAPE;
-    CUtensorMap map_w, map_x128, map_x16;
+    CUtensorMap map_w, map_x128, map_x16, map_y;
     if (!tc_encode_map2_bytes(&map_w, w, (uint64_t)g.G * w_rows, (uint64_t)g.k, 128) ||
         !tc_encode_map2_bytes(&map_x128, x, (uint64_t)g.T, (uint64_t)g.k, 128) ||
-        !tc_encode_map2_bytes(&map_x16, x, (uint64_t)g.T, (uint64_t)g.k, 16))
+        !tc_encode_map2_bytes(&map_x16, x, (uint64_t)g.T, (uint64_t)g.k, 16) ||
+        !tc_encode_map2_bytes(&map_y, g.y, (uint64_t)g.T, (uint64_t)g.n * row_bytes, 32))
         return SPICE_ERR_CUDA;
     // Fewer tiles than pairs: two or four pairs share a tile's reduction, as long as all the clusters run at once and the reduction is
     // long: 470 ns a block against a start of 4.5 us, or 12 with the sums of the cluster (77 x 3584 x 20480 with one / two / four
@@ -911,10 +954,10 @@ spice_status launch_gemm_e4m3(GemmE4m3Args g, const uint8_t *x, const uint8_t *w
     if (share > 1) {
         g.split = share;
         ok = launch_early(gemm_e4m3_pair_kernel<SWIGLU, true>, dim3((unsigned)(2 * share * most)), PR_THREADS, PR_SMEM_BYTES, st, 2 * share, map_w, map_x128,
-                          map_x16, g);
+                          map_x16, map_y, g);
     } else {
         const int pairs = (int)std::min<int64_t>(sms / 2, most);
-        ok = launch_early(gemm_e4m3_pair_kernel<SWIGLU, false>, dim3(2 * (unsigned)pairs), PR_THREADS, PR_SMEM_BYTES, st, 2, map_w, map_x128, map_x16, g);
+        ok = launch_early(gemm_e4m3_pair_kernel<SWIGLU, false>, dim3(2 * (unsigned)pairs), PR_THREADS, PR_SMEM_BYTES, st, 2, map_w, map_x128, map_x16, map_y, g);
     }
     return ok ? SPICE_OK : SPICE_ERR_CUDA;
 }
