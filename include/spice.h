@@ -386,7 +386,7 @@ spice_status spice_quantize_e4m3_blocks(const spice_bf16 *w, int64_t count, int6
 
 /* Product of such rows with such weights, dense or by groups of rows:
  *     y[t,j] = sum_b x_scale[t,b] w_scale[g][j/128,b] * ( sum over i in block b of x_q[t,i] w_q[g][j,i] ),   g the group of row t
- * Blocks are summed on the tensor cores, scaled and added up in fp32.
+ * Blocks are summed on the tensor cores, scaled by x_scale * w_scale (rounded to fp32) and added up in fp32.
  *   x_q [T, k] uint8 with x_scale [T, ceil(k/128)] fp32;  w_q [n_groups, n, k] with w_scale [n_groups, ceil(n/128), ceil(k/128)].
  *   Any scales are taken, not only those of the quantiser.
  *   offset [n_groups + 1] int32, device: group g has the rows offset[g] .. offset[g+1]-1; rows of y outside of all groups are
@@ -394,7 +394,7 @@ spice_status spice_quantize_e4m3_blocks(const spice_bf16 *w, int64_t count, int6
  *   empty, and SPICE_ERR_BAD_TABLE is reported.
  *   out, y [T, n]: as in spice_gemm_i8.  device_status: optional device int32 which the caller has set to 0: raised to
  *   SPICE_ERR_BAD_TABLE or SPICE_ERR_TIMEOUT (a bounded wait inside the kernel expired: the outputs are undefined then).
- *   k a multiple of 16, n a multiple of 8; T, n, k up to 2^24, n_groups up to 1024, n_groups * n below 2^31
+ *   y is device memory (bulk copies write it).  k a multiple of 16, n a multiple of 8; T, n, k up to 2^24, n_groups up to 1024, n_groups * n below 2^31
  *   (SPICE_ERR_UNSUPPORTED_SHAPE).  x_q, w_q and y 16-byte aligned.  For a given T and n_groups a row's bits do not depend on
  *   how the rows are spread over the groups. */
 spice_status spice_gemm_e4m3_blocks(const uint8_t *x_q, const float *x_scale, const uint8_t *w_q, const float *w_scale,

@@ -472,14 +472,14 @@ def _block_operands(f, x_q, x_scale, w_q, w_scale, offset):
 
 def spice_gemm_e4m3_blocks(x_q, x_scale, w_q, w_scale, y, offset=None, accumulate=False, device_status=None, stream=None) -> None:
     """x_q [T,k] uint8, x_scale [T,ceil(k/128)] fp32, w_q [n,k] uint8 with w_scale [ceil(n/128),ceil(k/128)], or with offset [G+1]
-    int32 w_q [G,n,k] and w_scale [G,...] -> y [T,n] bf16 or fp32; accumulate: y fp32 is added to.  x_q and w_q live on the device.
-    device_status: zeroed int32 tensor of one element that receives bad offsets and an expired wait."""
+    int32 w_q [G,n,k] and w_scale [G,...] -> y [T,n] bf16 or fp32; accumulate: y fp32 is added to.  x_q, w_q and y live on the
+    device (bulk copies).  device_status: zeroed int32 tensor of one element that receives bad offsets and an expired wait."""
     f = "spice_gemm_e4m3_blocks"
     ptrs, G, T, n, k, dev = _block_operands(f, x_q, x_scale, w_q, w_scale, offset)
     out = _row_type(f, y)
     if accumulate and out == OUT_BF16:
         raise SpiceError(f"{f}: only an fp32 y is added to")
-    _call_on(dev, f, stream, *ptrs, G, T, n, k, OUT_F32_ADD if accumulate else out, _addr(f, y, y.dtype, (T, n), dev),
+    _call_on(dev, f, stream, *ptrs, G, T, n, k, OUT_F32_ADD if accumulate else out, _addr(f, y, y.dtype, (T, n), dev, False),
              _addr(f, device_status, torch.int32, (1,), dev))
 
 

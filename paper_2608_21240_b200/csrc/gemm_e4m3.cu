@@ -457,9 +457,11 @@ struct PairShared {
     int abort_flag;
 };
 constexpr int PR_OUT_WARP = 32 * 256;             // an epilogue warp's results on their way out: two boxes of 32 rows x 128 bytes
-constexpr size_t PR_SMEM_BYTES = sizeof(PairShared) + (size_t)PR_STAGES * PR_STAGE_BYTES + PR_EPI_WARPS * PR_OUT_WARP + 1024;
+// All the shared memory there is: a CTA of another kernel beside this one, which holds all of tensor memory, could wait for columns
+// that the CTAs of its own cluster need to reach their barriers, on either side.
+constexpr size_t PR_SMEM_BYTES = 232448;
+static_assert(sizeof(PairShared) + (size_t)PR_STAGES * PR_STAGE_BYTES + PR_EPI_WARPS * PR_OUT_WARP + 1024 <= PR_SMEM_BYTES, "what a block can have");
 static_assert(PR_TILE * 128 * 4 <= PR_STAGES * PR_STAGE_BYTES, "the sums of a shared tile fit in the ring");
-static_assert(PR_SMEM_BYTES <= 232448, "what a block can have");
 
 // Tiles are numbered group by group; within a group sweeps of up to PR_GROUP_M token tiles, the token tile fastest, so that
 // pairs working at the same time share both operands in L2.  The group only moves forward.
@@ -920,7 +922,7 @@ spice_status launch_gemm_e4m3(GemmE4m3Args g, const uint8_t *x, const uint8_t *w
         auto most = [&](int tokens) {   // items there can be
             return g.G == 1 ? (int64_t)((g.T + tokens - 1) / tokens) * g.n_tiles : ((int64_t)g.T / tokens + used) * g.n_tiles;
         };
-        if (most(8) > 0x3fffffff) return SPICE_ERR_UNSUPPORTED_SHAPE;
+        if (most(8) > 0x3fffffff || (most(8) / sms + 1) * g.kb > 0x7fffffff) return SPICE_ERR_UNSUPPORTED_SHAPE;
         const int wide = g.G == 1 ? g.T : 2 * rows;   // (groups have unequal shares; a large one takes several items)
         const bool ok = wide <= 8 ? launch_stream<1, SWIGLU>(g, map_w, x, most(8), facts, sms, st)
                         : wide <= 16 ? launch_stream<2, SWIGLU>(g, map_w, x, most(16), facts, sms, st)
@@ -931,7 +933,7 @@ spice_status launch_gemm_e4m3(GemmE4m3Args g, const uint8_t *x, const uint8_t *w
     const int row_bytes = SWIGLU ? 1 : g.out == SPICE_OUT_BF16 ? 2 : 4;
     g.sectors = ((reinterpret_cast<uintptr_t>(g.y) | (uintptr_t)g.n * row_bytes) & 31u) == 0;
     const int64_t most = (g.G == 1 ? ((int64_t)g.T + PR_TILE - 1) / PR_TILE : (int64_t)g.T / PR_TILE + used) * g.n_tiles;   // tiles there can be
-    if (most > 0x3fffffff) return SPICE_ERR_UNSUPPORTED_SHAPE;
+    if (most > 0x3fffffff || (most / (sms / 2) + 1) * g.kb > 0x7fffffff) return SPICE_ERR_UNSUPPORTED_SHAPE;
     CUtensorMap map_w, map_x128, map_x16, map_y;
     if (!tc_encode_map2_bytes(&map_w, w, (uint64_t)g.G * w_rows, (uint64_t)g.k, 128) ||
         !tc_encode_map2_bytes(&map_x128, x, (uint64_t)g.T, (uint64_t)g.k, 128) ||

@@ -189,7 +189,7 @@ def test_dense_product(T, n, k):
     check(T, n, k)
 
 
-@pytest.mark.parametrize("T,n,k", [(1, 2048, 2816), (7, 136, 144), (77, 264, 1040), (257, 264, 144), (700, 520, 528)])
+@pytest.mark.parametrize("T,n,k", [(1, 2048, 2816), (7, 136, 144), (77, 264, 1040), (257, 264, 144), (700, 520, 528), (77, 264, 8208), (30, 72, 8208)])
 @pytest.mark.parametrize("out", ["bf16", "add"])
 def test_other_outputs(T, n, k, out):
     check(T, n, k, out)
@@ -321,11 +321,16 @@ def check_swiglu(T, inter, k, G=0, first=0, tail=0, std=0.03):
     got = q.view(E4M3).to(f64)
     low, high = nearest(u - du), nearest(u + du)
     assert ((low <= got) & (got <= high)).all()
-    assert float((low != high).double().mean()) < 0.5             # (the interval says something: most values have no choice)
+    # The interval says something: most values have no choice.  (Its width against a code's step, 2 slack(k) A / |e| of each factor against
+    # 2^-4 to 2^-3, grows with k: A / |e| like k^0.5, the worst case of the sums like k.  From k = 8208 on it is a percent and more for a
+    # typical factor and ten times that for one in ten: there the check is that of the intervals above alone.)
+    if k <= 4096:
+        assert float((low != high).double().mean()) < 0.5
 
 
 @pytest.mark.parametrize("T,inter,k", [(1, 128, 16), (1, 1408, 2048), (3, 256, 144), (8, 2816, 528), (16, 384, 1040), (17, 128, 48), (33, 256, 2048), (100, 640, 528),
-                                       (256, 128, 144), (257, 384, 272), (513, 256, 1408), (1500, 1408, 256), (4000, 1408, 144)])
+                                       (256, 128, 144), (257, 384, 272), (513, 256, 1408), (1500, 1408, 256), (4000, 1408, 144),
+                                       (40, 256, 8192), (300, 128, 16400), (25, 128, 8208)])
 def test_swiglu(T, inter, k):
     check_swiglu(T, inter, k)
 
@@ -402,7 +407,7 @@ def test_captured_calls_on_two_streams(T, G):
             assert torch.equal(v, ref)
 
 
-@pytest.mark.parametrize("T,n,k,G", [(300, 512, 2048, 0), (700, 2048, 528, 0), (2600, 512, 528, 9)])
+@pytest.mark.parametrize("T,n,k,G", [(300, 512, 2048, 0), (700, 2048, 528, 0), (2600, 512, 528, 9), (64, 256, 8192, 0), (12, 512, 2048, 0), (96, 512, 528, 16)])
 def test_expired_waits_are_reported(T, n, k, G):
     """With waits that give up at once, a call ends by itself, reports it, and writes nothing behind its rows; the next call is as
     always."""
