@@ -7,9 +7,10 @@
 // in the tensor cores' operands and added in their fp32 accumulators; every block's sum is multiplied by its two scales and
 // added in fp32 registers, so no scale is rounded into an operand and long reductions are sums of fp32 sums.
 //
-// Two kernels.  Few rows a group: every weight byte is used for few products and the call is bound by streaming the weights:
-// they go from global memory straight into the registers of warp-wide products.  Otherwise pairs of CTAs (cta_group::2) work on
-// tiles of 256 tokens x 256 weight rows, persistent.
+// Three kernels.  Few rows a group: every weight byte is used for few products and the call is bound by streaming the weights,
+// through a ring in shared memory into warp-wide products.  A few tokens and few weights: neither ring nor clusters, whose start
+// and sums would cost more than the call.  Otherwise pairs of CTAs (cta_group::2) work on tiles of 256 tokens x 256 weight rows,
+// persistent.
 #include <cuda_fp8.h>
 
 #include <algorithm>
@@ -126,9 +127,11 @@ __device__ __forceinline__ void store1(const GemmE4m3Args &g, size_t at, float v
 // The weights stream through a ring in shared memory at the rate of HBM, and eight warps multiply them with up to 32 tokens in
 // warp-wide products: a warp has 32 weight rows (SwiGLU: 16 gate rows and their up rows) and all the tokens, so that only a stage's
 // operands pass through shared memory and no sums do.  (On tcgen05 the sums of every block would have to come back from tensor
-// memory, a round trip of 1.0 us for two blocks, twice what a block of weights takes to arrive.)  Persistent over (group, 256
-// weight rows, up to 32 tokens); where those are fewer than the SMs, the CTAs of a cluster share the reduction of one and add up
-// through distributed shared memory.
+// memory, 0.47 us a block, more than a block of weights takes to arrive.)  Persistent over (group, 256 weight rows, up to 32
+// tokens); where those are fewer than the SMs, the CTAs of a cluster share the reduction of one and add up through distributed
+// shared memory.  96 rows over 64 groups: SwiGLU 1408 x 2048 60 us, 0.88 of the measured copy rate; product 2048 x 1408 33 us.
+// From 16 tokens on the products of a block (400 a cycle and SM) take longer than its weights: 3584 x 20480 with 1 / 16 / 32 tokens
+// 15.9 / 18.9 / 28.8 us.
 constexpr int ST_WARPS = 8, ST_THREADS = ST_WARPS * 32 + 32, ST_MAX_SPLIT = 8;
 constexpr int ST_W_BYTES = 256 * BK;
 constexpr int ST_RED_PITCH = 260;                 // fp32 sums of a token's 256 weight rows, padded against bank conflicts
@@ -438,9 +441,109 @@ __global__ void __launch_bounds__(ST_THREADS, 1)
     if (threadIdx.x == 0 && sh.abort_flag && g.status) atomicMax(g.status, (int)SPICE_ERR_TIMEOUT);
 }
 
+// ------------------------------------------------------------------------------------------------ a few tokens and few weights
+// A block multiplies 16 weight rows with the rows of one group (eight at most); its warps share the blocks of the reduction, two at
+// a time, straight from global memory.  Both operands are read in pieces of 16 bytes, so the order of the reduction inside a 64-byte
+// piece is the same for both and does not matter.  Bound by launch and memory latency.
+constexpr int FEW_WARPS = 8, FEW_TOKENS = 8, FEW_BLOCKS = 2;
+
+__device__ __forceinline__ int4 load16(const int4 *p) {
+    int4 v;
+    asm volatile("ld.global.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+
+// The slot-th group that has rows: its number, or -1; groups whose offsets are not in order or out of range have none.
+__device__ __forceinline__ int find_group(const GemmE4m3Args &g, int slot, const int32_t *off) {
+    const int lane = threadIdx.x & 31;
+    for (int base = 0, seen = 0; base < g.G; base += 32) {
+        const int i = base + lane;
+        uint32_t mask = __ballot_sync(0xffffffffu, i < g.G && off[i] >= 0 && off[i + 1] > off[i] && off[i + 1] <= g.T);
+        const int here = __popc(mask);
+        if (seen + here > slot) {
+            for (int s = slot - seen; s > 0; --s) mask &= mask - 1;
+            return base + __ffs(mask) - 1;
+        }
+        seen += here;
+    }
+    return -1;
+}
+
+__global__ void __launch_bounds__(FEW_WARPS * 32) gemm_e4m3_few_kernel(const uint8_t *x, const uint8_t *w, const GemmE4m3Args g) {
+    __shared__ float red[FEW_WARPS][FEW_TOKENS][20];   // (16, padded: the rows of a warp's store fall into different banks)
+    __shared__ int32_t off[MAX_GROUPS + 1];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int r8 = lane >> 2, c = lane & 3;
+    const int n0 = blockIdx.x * 16;
+    grid_dependency();
+    if (g.offset) {
+        for (int i = threadIdx.x; i <= g.G; i += FEW_WARPS * 32) off[i] = load_s32(g.offset + i);
+        __syncthreads();
+        if (g.status && blockIdx.x == 0 && blockIdx.y == 0)
+            for (int i = threadIdx.x; i < g.G; i += FEW_WARPS * 32)
+                if (off[i] < 0 || off[i + 1] < off[i] || off[i + 1] > g.T) atomicMax(g.status, (int)SPICE_ERR_BAD_TABLE);
+    }
+    // (one group a block, unless offsets overlap)
+    for (int slot = blockIdx.y;; slot += gridDim.y) {
+        const int group = g.offset ? find_group(g, slot, off) : slot == 0 ? 0 : -1;
+        if (group < 0) return;
+        const int begin = g.offset ? off[group] : 0, rows = g.offset ? off[group + 1] - begin : g.T;
+        const int nv = g.k >> 4, row_blocks = (g.n + 127) / 128;
+        const int4 *wr[2], *xr = reinterpret_cast<const int4 *>(x) + (size_t)(begin + r8) * nv;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)   // (n is a multiple of 8)
+            wr[h] = reinterpret_cast<const int4 *>(w) + ((size_t)group * g.n + n0 + r8 + (n0 + 8 * h < g.n ? 8 * h : 0)) * nv;
+        const float *ws = g.ws + ((size_t)group * row_blocks + n0 / 128) * g.kb, *xs = g.xs + (size_t)begin * g.kb;
+        float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        const int4 zero = make_int4(0, 0, 0, 0);
+        for (int b0 = warp; b0 < g.kb; b0 += FEW_WARPS * FEW_BLOCKS) {
+            int4 a[FEW_BLOCKS][2][2], bx[FEW_BLOCKS][2];
+            float sx[FEW_BLOCKS][2], sw[FEW_BLOCKS];
+#pragma unroll
+            for (int u = 0; u < FEW_BLOCKS; ++u) {
+                const int b = b0 + u * FEW_WARPS;
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    const int v = b * 8 + p * 4 + c;
+                    const bool in = v < nv;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) a[u][p][h] = in ? load16(wr[h] + v) : zero;
+                    bx[u][p] = in && r8 < rows ? load16(xr + v) : zero;
+                }
+#pragma unroll
+                for (int j = 0; j < 2; ++j) sx[u][j] = b < g.kb && 2 * c + j < rows ? load_f32(xs + (size_t)(2 * c + j) * g.kb + b) : 0.0f;
+                sw[u] = b < g.kb ? load_f32(ws + b) : 0.0f;
+            }
+#pragma unroll
+            for (int u = 0; u < FEW_BLOCKS; ++u) {
+                float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    const int4 a0 = a[u][p][0], a1 = a[u][p][1], bb = bx[u][p];
+                    mma_e4m3(d, a0.x, a1.x, a0.y, a1.y, bb.x, bb.y);
+                    mma_e4m3(d, a0.z, a1.z, a0.w, a1.w, bb.z, bb.w);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[j] = fmaf(d[j], sx[u][j & 1] * sw[u], acc[j]);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) red[warp][2 * c + (j & 1)][r8 + 8 * (j >> 1)] = acc[j];
+        __syncthreads();
+        const int t = threadIdx.x / 16, r = threadIdx.x % 16;
+        if (t < rows && n0 + r < g.n) {
+            float v = 0.0f;
+#pragma unroll
+            for (int q = 0; q < FEW_WARPS; ++q) v += red[q][t][r];
+            store1(g, (size_t)(begin + t) * g.n + n0 + r, v);
+        }
+        __syncthreads();   // the sums have been read
+    }
+}
+
 // ------------------------------------------------------------------------------------------------ more rows
 constexpr int PR_THREADS = 384, PR_EPI_WARPS = 8;
-constexpr uint32_t PR_STAGES = 4;                // (six are no faster)
+constexpr uint32_t PR_STAGES = 4;                 // (six are no faster)
 constexpr int PR_TILE = 256;                      // tokens of a pair's tile (128 per CTA), and its accumulator columns
 constexpr int PR_HALF_BYTES = 128 * BK;           // a CTA's half of one operand
 constexpr int PR_STAGE_BYTES = 2 * PR_HALF_BYTES;
@@ -478,6 +581,11 @@ __device__ __forceinline__ Tile find_tile(const PairShared &sh, const GemmE4m3Ar
 // could fall two uses of a stage behind, and the parity of a barrier would no longer tell it which use is meant.
 __device__ __forceinline__ int copied(int rows, int rank) { return (min(max(rows - rank * 128, 1), 128) + 15) & ~15; }
 
+// A block of the reduction is 128 x 128 values of both operands per CTA; its 256 x 256 sums come back from tensor memory, are scaled
+// and added in registers, a token per thread, while the other accumulator is multiplied into.  24576 rows over 64 groups of very
+// different sizes: product 2048 x 1408 104 us, SwiGLU 1408 x 2048 203 us, a third of the multiplied rows being padding of the last
+// tile of a group; the copies alone take 72 and 128 us, the matrix instructions 41 and 91.  With half accumulators (four of 128
+// columns) 111 and 203, with 16 epilogue warps 131 and 242.
 // SPLIT: the reduction of a tile is shared by the g.split pairs of a cluster (one tile per cluster, one group): each pair leaves its
 // sums in its shared memory and finishes its share of the tokens with those of the others.
 template <bool SWIGLU, bool SPLIT>
@@ -911,6 +1019,16 @@ spice_status launch_gemm_e4m3(GemmE4m3Args g, const uint8_t *x, const uint8_t *w
     const int w_rows = SWIGLU ? 2 * g.n : g.n;
     const int used = std::min(g.G, g.T);   // groups that can have rows
     const int rows = (g.T + used - 1) / used;
+    if constexpr (!SWIGLU) {
+        // A few tokens: until the reduction takes more than two turns of the warps, or the weights that can be touched take long enough
+        // for the ring to pay.  Without / with the ring, us, one token: 512 x 1024 2.0/4.3, 2048 x 2048 3.8/5.0, 8192 x 2048 5.4/7.4,
+        // 5000 x 4096 7.5/8.3, 2048 x 8192 10.3/8.0, 20480 x 3584 17.5/16.3; 2048 x 1408 of 64 groups, 2 / 8 rows 4.8/7.6, 9.5/10.7;
+        // 4096 x 2048 of 8, 4 / 8 rows 10.3/10.6, 17.4/15.3.  (SwiGLU needs clusters for its blocks of 128 all the same: no gain.)
+        if (g.T <= FEW_TOKENS && g.kb <= 2 * FEW_WARPS * FEW_BLOCKS && (int64_t)used * g.n * g.k <= (32 << 20)) {
+            const dim3 grid((unsigned)((g.n + 15) / 16), (unsigned)used);
+            return launch_early(gemm_e4m3_few_kernel, grid, FEW_WARPS * 32, 0, st, 1, x, w, g) ? SPICE_OK : SPICE_ERR_CUDA;
+        }
+    }
     // Few rows: streamed weights, at the rate of HBM as long as the warp-wide products (400 per cycle and SM) keep up.  Streamed / by
     // pairs of CTAs, us, dense 2048 x 2816, 3584 x 20480, SwiGLU 5632 x 2048:  16 tokens 6.8/12.4, 18.9/29, 8.1/13;  32 tokens 9.6/13,
     // 28.9/30.8, 11.1/12.9;  64 tokens 14.7/14.7, 56/34, 19.4/13.4.  64 groups of 2048 x 1408, SwiGLU 2816 x 2048:  96 rows 34.6/49,

@@ -183,7 +183,7 @@ int launch_decode_tc(const DecodeParams &p, float *part_split, int n_ctas, int m
 int launch_quantize_e4m3_rows(const __nv_bfloat16 *w, size_t rows, int cols, uint8_t *q, float *scale, cudaStream_t st);
 
 
-// polls after which a wait inside the products of 8-bit integers gives up (gemm_i8.cu)
+// polls after which a wait inside the products of 8-bit integers gives up (gemm_i8.cu), and of E4M3 blocks (gemm_e4m3.cu)
 void set_gemm_i8_wait_limit(uint32_t polls);
 void set_gemm_e4m3_wait_limit(uint32_t polls);
 

@@ -217,6 +217,39 @@ def test_groups_at_the_ends_and_all_rows_in_one(T):
         compare(y[rows], e[rows], A[rows], 272, "f32")
 
 
+# (up to eight tokens, on both sides of what is multiplied without a ring: 32 blocks of the reduction, 32 MiB of weights)
+@pytest.mark.parametrize("T,n,k", [(1, 512, 1024), (8, 24, 4096), (5, 200, 2064), (8, 2056, 2064), (4, 40, 4112), (8, 264, 8208), (7, 8184, 4096),
+                                   (8, 8200, 4096)])
+@pytest.mark.parametrize("out", ["bf16", "f32", "add"])
+def test_up_to_eight_tokens(T, n, k, out):
+    check(T, n, k, out)
+
+
+@pytest.mark.parametrize("n,k", [(136, 272), (72, 4096), (264, 5136)])
+@pytest.mark.parametrize("bounds", [[0, 0, 0, 8, 8, 8, 8], [0] * 6 + [8], [0] + [8] * 6, [0, 1, 2, 3, 4, 5, 8], [2, 2, 3, 3, 5, 6, 6], [8] * 7, [0] * 7])
+def test_up_to_eight_tokens_in_groups(n, k, bounds):
+    x, xs, w, ws = operands(8, n, k, 6, n)
+    y = run(x, xs, w, ws, "f32", bounds)
+    e, A = exact(x, xs, w, ws, bounds)
+    rows = torch.zeros(8, dtype=torch.bool, device="cuda")
+    rows[bounds[0]:bounds[-1]] = True
+    assert (y[~rows] == 3).all()
+    compare(y[rows], e[rows], A[rows], k, "f32")
+
+
+def test_up_to_eight_tokens_in_many_groups_and_bad_ones():
+    T, n, k = 8, 136, 528
+    x, xs, w, ws = operands(T, n, k, 1, 3)
+    e, A = exact(x, xs, w, ws, [0, T])
+    for G in (8, 40, 1024):
+        many, scales = w.expand(G, -1, -1).contiguous(), ws.expand(G, -1, -1).contiguous()
+        compare(run(x, xs, many, scales, "f32", split(T, G, G)), e, A, k, "f32")
+        compare(run(x, xs, many, scales, "f32", [0, T] * (G // 2) + [T], status=5), e, A, k, "f32")   # more groups with rows than rows
+        y = run(x, xs, many, scales, "f32", [0, 3, T + 1, 5] + [T] * (G - 3), status=5)
+        compare(y[[0, 1, 2, 5, 6, 7]], e[[0, 1, 2, 5, 6, 7]], A[[0, 1, 2, 5, 6, 7]], k, "f32")
+        assert (y[3:5] == 3).all()
+
+
 @pytest.mark.parametrize("T", [30, 800])
 def test_bad_offsets_are_reported_and_their_groups_left_out(T):
     x, xs, w, ws = operands(T, 72, 144, 4, T)
