@@ -442,12 +442,17 @@ __global__ void __launch_bounds__(ST_THREADS, 1)
 }
 
 // ------------------------------------------------------------------------------------------------ a few tokens and few weights
-// A block multiplies 16 weight rows with the rows of one group (eight at most); its warps share the blocks of the reduction, two at
-// a time, straight from global memory.  Both operands are read in pieces of 16 bytes, so the order of the reduction inside a 64-byte
-// piece is the same for both and does not matter.  Bound by launch and memory latency.
+// A block multiplies 16 weight rows with the rows of one group (eight at most); a warp has two blocks of the reduction, straight from
+// global memory.  Both operands are read in pieces of 16 bytes, so the order of the reduction inside a 64-byte piece is the same for
+// both and does not matter.  Bound by launch and memory latency: all loads of a call are on their way at once.
 constexpr int FEW_WARPS = 8, FEW_TOKENS = 8, FEW_BLOCKS = 2;
 
-__device__ __forceinline__ int4 load16(const int4 *p) {
+__device__ __forceinline__ int4 load_once(const int4 *p) {
+    int4 v;
+    asm volatile("ld.global.cs.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ int4 load_again(const int4 *p) {
     int4 v;
     asm volatile("ld.global.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
     return v;
@@ -483,61 +488,64 @@ __global__ void __launch_bounds__(FEW_WARPS * 32) gemm_e4m3_few_kernel(const uin
             for (int i = threadIdx.x; i < g.G; i += FEW_WARPS * 32)
                 if (off[i] < 0 || off[i + 1] < off[i] || off[i + 1] > g.T) atomicMax(g.status, (int)SPICE_ERR_BAD_TABLE);
     }
-    // (one group a block, unless offsets overlap)
-    for (int slot = blockIdx.y;; slot += gridDim.y) {
-        const int group = g.offset ? find_group(g, slot, off) : slot == 0 ? 0 : -1;
-        if (group < 0) return;
-        const int begin = g.offset ? off[group] : 0, rows = g.offset ? off[group + 1] - begin : g.T;
-        const int nv = g.k >> 4, row_blocks = (g.n + 127) / 128;
-        const int4 *wr[2], *xr = reinterpret_cast<const int4 *>(x) + (size_t)(begin + r8) * nv;
+    // (there are T blocks: where offsets overlap, groups may be left out.  A loop over them costs registers, and 12 for 9 us)
+    const int group = g.offset ? find_group(g, blockIdx.y, off) : 0;
+    if (group < 0) return;
+    const int begin = g.offset ? off[group] : 0, rows = g.offset ? off[group + 1] - begin : g.T;
+    const int nv = g.k >> 4, row_blocks = (g.n + 127) / 128;
+    const int4 *wr[2], *xr = reinterpret_cast<const int4 *>(x) + (size_t)(begin + r8) * nv;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)   // (n is a multiple of 8)
-            wr[h] = reinterpret_cast<const int4 *>(w) + ((size_t)group * g.n + n0 + r8 + (n0 + 8 * h < g.n ? 8 * h : 0)) * nv;
-        const float *ws = g.ws + ((size_t)group * row_blocks + n0 / 128) * g.kb, *xs = g.xs + (size_t)begin * g.kb;
-        float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        const int4 zero = make_int4(0, 0, 0, 0);
-        for (int b0 = warp; b0 < g.kb; b0 += FEW_WARPS * FEW_BLOCKS) {
-            int4 a[FEW_BLOCKS][2][2], bx[FEW_BLOCKS][2];
-            float sx[FEW_BLOCKS][2], sw[FEW_BLOCKS];
+    for (int h = 0; h < 2; ++h)   // (n is a multiple of 8)
+        wr[h] = reinterpret_cast<const int4 *>(w) + ((size_t)group * g.n + n0 + r8 + (n0 + 8 * h < g.n ? 8 * h : 0)) * nv;
+    const float *ws = g.ws + ((size_t)group * row_blocks + n0 / 128) * g.kb, *xs = g.xs + (size_t)begin * g.kb;
+    float acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    const int4 zero = make_int4(0, 0, 0, 0);
+    int4 a[FEW_BLOCKS][2][2], bx[FEW_BLOCKS][2];
+    float sx[FEW_BLOCKS][2], sw[FEW_BLOCKS];
 #pragma unroll
-            for (int u = 0; u < FEW_BLOCKS; ++u) {
-                const int b = b0 + u * FEW_WARPS;
+    for (int u = 0; u < FEW_BLOCKS; ++u) {
+        const int b = warp + u * FEW_WARPS;
 #pragma unroll
-                for (int p = 0; p < 2; ++p) {
-                    const int v = b * 8 + p * 4 + c;
-                    const bool in = v < nv;
+        for (int p = 0; p < 2; ++p) {
+            const int v = b * 8 + p * 4 + c;
+            const bool in = v < nv;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) a[u][p][h] = in ? load16(wr[h] + v) : zero;
-                    bx[u][p] = in && r8 < rows ? load16(xr + v) : zero;
-                }
+            for (int h = 0; h < 2; ++h) a[u][p][h] = in ? load_once(wr[h] + v) : zero;
+        }
+    }
 #pragma unroll
-                for (int j = 0; j < 2; ++j) sx[u][j] = b < g.kb && 2 * c + j < rows ? load_f32(xs + (size_t)(2 * c + j) * g.kb + b) : 0.0f;
-                sw[u] = b < g.kb ? load_f32(ws + b) : 0.0f;
-            }
+    for (int u = 0; u < FEW_BLOCKS; ++u) {
+        const int b = warp + u * FEW_WARPS;
 #pragma unroll
-            for (int u = 0; u < FEW_BLOCKS; ++u) {
-                float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int p = 0; p < 2; ++p) {
-                    const int4 a0 = a[u][p][0], a1 = a[u][p][1], bb = bx[u][p];
-                    mma_e4m3(d, a0.x, a1.x, a0.y, a1.y, bb.x, bb.y);
-                    mma_e4m3(d, a0.z, a1.z, a0.w, a1.w, bb.z, bb.w);
-                }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[j] = fmaf(d[j], sx[u][j & 1] * sw[u], acc[j]);
-            }
+        for (int p = 0; p < 2; ++p) {
+            const int v = b * 8 + p * 4 + c;
+            bx[u][p] = v < nv && r8 < rows ? load_again(xr + v) : zero;
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) red[warp][2 * c + (j & 1)][r8 + 8 * (j >> 1)] = acc[j];
-        __syncthreads();
-        const int t = threadIdx.x / 16, r = threadIdx.x % 16;
-        if (t < rows && n0 + r < g.n) {
-            float v = 0.0f;
+        for (int j = 0; j < 2; ++j) sx[u][j] = b < g.kb && 2 * c + j < rows ? load_f32(xs + (size_t)(2 * c + j) * g.kb + b) : 0.0f;
+        sw[u] = b < g.kb ? load_f32(ws + b) : 0.0f;
+    }
 #pragma unroll
-            for (int q = 0; q < FEW_WARPS; ++q) v += red[q][t][r];
-            store1(g, (size_t)(begin + t) * g.n + n0 + r, v);
+    for (int u = 0; u < FEW_BLOCKS; ++u) {
+        float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            const int4 a0 = a[u][p][0], a1 = a[u][p][1], bb = bx[u][p];
+            mma_e4m3(d, a0.x, a1.x, a0.y, a1.y, bb.x, bb.y);
+            mma_e4m3(d, a0.z, a1.z, a0.w, a1.w, bb.z, bb.w);
         }
-        __syncthreads();   // the sums have been read
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[j] = fmaf(d[j], sx[u][j & 1] * sw[u], acc[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) red[warp][2 * c + (j & 1)][r8 + 8 * (j >> 1)] = acc[j];
+    __syncthreads();
+    const int t = threadIdx.x / 16, r = threadIdx.x % 16;
+    if (t < rows && n0 + r < g.n) {
+        float v = 0.0f;
+#pragma unroll
+        for (int q = 0; q < FEW_WARPS; ++q) v += red[q][t][r];
+        store1(g, (size_t)(begin + t) * g.n + n0 + r, v);
     }
 }
 
@@ -1020,11 +1028,11 @@ spice_status launch_gemm_e4m3(GemmE4m3Args g, const uint8_t *x, const uint8_t *w
     const int used = std::min(g.G, g.T);   // groups that can have rows
     const int rows = (g.T + used - 1) / used;
     if constexpr (!SWIGLU) {
-        // A few tokens: until the reduction takes more than two turns of the warps, or the weights that can be touched take long enough
-        // for the ring to pay.  Without / with the ring, us, one token: 512 x 1024 2.0/4.3, 2048 x 2048 3.8/5.0, 8192 x 2048 5.4/7.4,
-        // 5000 x 4096 7.5/8.3, 2048 x 8192 10.3/8.0, 20480 x 3584 17.5/16.3; 2048 x 1408 of 64 groups, 2 / 8 rows 4.8/7.6, 9.5/10.7;
-        // 4096 x 2048 of 8, 4 / 8 rows 10.3/10.6, 17.4/15.3.  (SwiGLU needs clusters for its blocks of 128 all the same: no gain.)
-        if (g.T <= FEW_TOKENS && g.kb <= 2 * FEW_WARPS * FEW_BLOCKS && (int64_t)used * g.n * g.k <= (32 << 20)) {
+        // A few tokens and few weights that can be touched: no ring.  Without / with it, us, one token: 512 x 1024 1.8/4.2,
+        // 2048 x 2048 3.9/5.1, 8192 x 2048 5.8/7.3, 16384 x 2048 9.6/10.1 (in turns of two blocks also 2048 x 4096 6.8/6.4, 2048 x 8192
+        // 10.3/8.0);  2048 x 1408 of 64 groups, 1 / 2 / 8 rows: 4.6/6.5, 5.2/7.7, 9.9/10.9;  4096 x 2048 of 8, 8 rows (64 MiB): 17.5/15.3.
+        // (SwiGLU needs clusters for its blocks of 128 columns all the same: no gain.)
+        if (g.T <= FEW_TOKENS && g.kb <= FEW_WARPS * FEW_BLOCKS && (int64_t)used * g.n * g.k <= (32 << 20)) {
             const dim3 grid((unsigned)((g.n + 15) / 16), (unsigned)used);
             return launch_early(gemm_e4m3_few_kernel, grid, FEW_WARPS * 32, 0, st, 1, x, w, g) ? SPICE_OK : SPICE_ERR_CUDA;
         }

@@ -217,9 +217,9 @@ def test_groups_at_the_ends_and_all_rows_in_one(T):
         compare(y[rows], e[rows], A[rows], 272, "f32")
 
 
-# (up to eight tokens, on both sides of what is multiplied without a ring: 32 blocks of the reduction, 32 MiB of weights)
+# (up to eight tokens, on both sides of what is multiplied without a ring: 16 blocks of the reduction, 32 MiB of weights)
 @pytest.mark.parametrize("T,n,k", [(1, 512, 1024), (8, 24, 4096), (5, 200, 2064), (8, 2056, 2064), (4, 40, 4112), (8, 264, 8208), (7, 8184, 4096),
-                                   (8, 8200, 4096)])
+                                   (8, 8200, 4096), (8, 24, 2048), (3, 2056, 2032), (7, 16384, 2048), (8, 16392, 2048), (8, 136, 1040), (2, 72, 16)])
 @pytest.mark.parametrize("out", ["bf16", "f32", "add"])
 def test_up_to_eight_tokens(T, n, k, out):
     check(T, n, k, out)
