@@ -591,7 +591,7 @@ __device__ __forceinline__ int copied(int rows, int rank) { return (min(max(rows
 
 // A block of the reduction is 128 x 128 values of both operands per CTA; its 256 x 256 sums come back from tensor memory, are scaled
 // and added in registers, a token per thread, while the other accumulator is multiplied into.  24576 rows over 64 groups of very
-// different sizes: product 2048 x 1408 104 us, SwiGLU 1408 x 2048 203 us, a third of the multiplied rows being padding of the last
+// different sizes: product 2048 x 1408 101 to 104 us, SwiGLU 1408 x 2048 199 to 203 us (1400 TFLOP/s), a third of the multiplied rows being padding of the last
 // tile of a group; the copies alone take 72 and 128 us, the matrix instructions 41 and 91.  With half accumulators (four of 128
 // columns) 111 and 203, with 16 epilogue warps 131 and 242.
 // SPLIT: the reduction of a tile is shared by the g.split pairs of a cluster (one tile per cluster, one group): each pair leaves its
