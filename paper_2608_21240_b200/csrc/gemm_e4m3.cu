@@ -200,6 +200,50 @@ __device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t (&v)[4]) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(addr));
 }
 
+// A token whose sums lie in the shared memory of several CTAs of the cluster, part p in CTA p * step + base at the address `at`: 256
+// weight rows (SwiGLU: 128 gate rows and their up rows).  By a warp: its lanes have four neighbouring rows each, and all parts of them
+// (up to four) are on their way at once.
+template <bool SWIGLU>
+__device__ __forceinline__ void finish_token(const GemmE4m3Args &g, uint32_t at, int parts, int step, int base, size_t token, int nt, bool ok, int lane) {
+    float4 v[2];
+    v[0] = v[1] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int p0 = 0; p0 < parts; p0 += 4) {
+        float4 o[4][2];
+#pragma unroll
+        for (int p = 0; p < 4; ++p)
+#pragma unroll
+            for (int z = 0; z < 2; ++z) {
+                o[p][z] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (p0 + p < parts)
+                    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                                 : "=f"(o[p][z].x), "=f"(o[p][z].y), "=f"(o[p][z].z), "=f"(o[p][z].w)
+                                 : "r"(map_to_cta(at + z * 512 + lane * 16, (uint32_t)((p0 + p) * step + base))));
+            }
+#pragma unroll
+        for (int p = 0; p < 4; ++p)
+#pragma unroll
+            for (int z = 0; z < 2; ++z) v[z] = make_float4(v[z].x + o[p][z].x, v[z].y + o[p][z].y, v[z].z + o[p][z].z, v[z].w + o[p][z].w);
+    }
+    if constexpr (SWIGLU) {
+        const float a[4] = {silu_times(v[0].x, v[1].x), silu_times(v[0].y, v[1].y), silu_times(v[0].z, v[1].z), silu_times(v[0].w, v[1].w)};
+        float big = max_magnitude(max_magnitude(max_magnitude(fabsf(a[0]), a[1]), a[2]), a[3]);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) big = max_magnitude(big, __shfl_xor_sync(0xffffffffu, big, o));
+        const OutScale q(big);
+        if (ok) {
+            *reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(g.y) + token * g.n + nt * 128 + lane * 4) =
+                code2(a[0], a[1], q.r) | code2(a[2], a[3], q.r) << 16;
+            if (lane == 0) g.ys[token * (g.n / 128) + nt] = q.scale;
+        }
+    } else if (ok) {
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+            const int col = nt * 256 + z * 128 + lane * 4;
+            if (col < g.n) store4(g, token * g.n + col, v[z]);
+        }
+    }
+}
+
 template <int NT, bool SWIGLU, bool SPLIT>
 __global__ void __launch_bounds__(ST_THREADS, 1)
     gemm_e4m3_stream_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const GemmE4m3Args g) {
@@ -351,38 +395,9 @@ __global__ void __launch_bounds__(ST_THREADS, 1)
 #pragma unroll
                         for (int j = 0; j < 4; ++j) red[(i * 8 + c2 + (j & 1)) * ST_RED_PITCH + (r ? wr1 : wr0) + r4 + (j >> 1) * 8] = acc[r][i][j];
                 cluster_sync();
-                // every CTA finishes some of the tokens, a warp a token at a time; its lanes have four neighbouring rows each
-                for (int c = rank + warp * split; c < t.rows; c += ST_WARPS * split) {
-                    float4 v[2];
-#pragma unroll
-                    for (int z = 0; z < 2; ++z) {
-                        const uint32_t at = smem_u32(red + c * ST_RED_PITCH + z * 128 + lane * 4);
-                        v[z] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                        for (int p = 0; p < split; ++p) {
-                            float4 o;
-                            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(o.x), "=f"(o.y), "=f"(o.z), "=f"(o.w) : "r"(map_to_cta(at, (uint32_t)p)));
-                            v[z] = make_float4(v[z].x + o.x, v[z].y + o.y, v[z].z + o.z, v[z].w + o.w);
-                        }
-                    }
-                    if constexpr (SWIGLU) {
-                        const float a[4] = {silu_times(v[0].x, v[1].x), silu_times(v[0].y, v[1].y), silu_times(v[0].z, v[1].z), silu_times(v[0].w, v[1].w)};
-                        float big = max_magnitude(max_magnitude(max_magnitude(fabsf(a[0]), a[1]), a[2]), a[3]);
-#pragma unroll
-                        for (int o = 16; o > 0; o >>= 1) big = max_magnitude(big, __shfl_xor_sync(0xffffffffu, big, o));
-                        const OutScale q(big);
-                        if (ok) {
-                            *reinterpret_cast<uint32_t *>(static_cast<uint8_t *>(g.y) + (size_t)(t.t0 + c) * g.n + t.nt * 128 + lane * 4) =
-                                code2(a[0], a[1], q.r) | code2(a[2], a[3], q.r) << 16;
-                            if (lane == 0) g.ys[(size_t)(t.t0 + c) * (g.n / 128) + t.nt] = q.scale;
-                        }
-                    } else if (ok) {
-#pragma unroll
-                        for (int z = 0; z < 2; ++z) {
-                            const int col = t.nt * 256 + z * 128 + lane * 4;
-                            if (col < g.n) store4(g, (size_t)(t.t0 + c) * g.n + col, v[z]);
-                        }
-                    }
-                }
+                // every CTA finishes some of the tokens, a warp a token at a time
+                for (int c = rank + warp * split; c < t.rows; c += ST_WARPS * split)
+                    finish_token<SWIGLU>(g, smem_u32(red + c * ST_RED_PITCH), split, 1, 0, (size_t)(t.t0 + c), t.nt, ok, lane);
                 cluster_sync();   // nobody leaves while a peer reads its sums
             } else if constexpr (SWIGLU) {
 #pragma unroll
@@ -572,7 +587,7 @@ constexpr int PR_OUT_WARP = 32 * 256;             // an epilogue warp's results 
 // that the CTAs of its own cluster need to reach their barriers, on either side.
 constexpr size_t PR_SMEM_BYTES = 232448;
 static_assert(sizeof(PairShared) + (size_t)PR_STAGES * PR_STAGE_BYTES + PR_EPI_WARPS * PR_OUT_WARP + 1024 <= PR_SMEM_BYTES, "what a block can have");
-static_assert(PR_TILE * 128 * 4 <= PR_STAGES * PR_STAGE_BYTES, "the sums of a shared tile fit in the ring");
+static_assert(128 * ST_RED_PITCH * 4 <= PR_STAGES * PR_STAGE_BYTES + PR_EPI_WARPS * PR_OUT_WARP, "the sums of a shared tile fit before PairShared");
 
 // Tiles are numbered group by group; within a group sweeps of up to PR_GROUP_M token tiles, the token tile fastest, so that
 // pairs working at the same time share both operands in L2.  The group only moves forward.
@@ -764,14 +779,12 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
                 }
             }
             if constexpr (SPLIT) {
-                // sums as [column][128 tokens] over the ring (the last products are over)
-                float *sums = reinterpret_cast<float *>(ring) + q * 32 + lane;
+                // sums as [128 tokens][256 weight rows] over the ring and what follows it (the last products are over)
+                float *sums = reinterpret_cast<float *>(ring) + (q * 32 + lane) * ST_RED_PITCH;
 #pragma unroll
-                for (int i = 0; i < 64; ++i) {
-                    const int c = 2 * i + (SWIGLU ? h * 64 + (i >= 32 ? 64 : 0) : h * 128);
-                    sums[c * 128] = low(acc[i]);
-                    sums[c * 128 + 128] = high(acc[i]);
-                }
+                for (int i = 0; i < 64; i += 2)
+                    *reinterpret_cast<float4 *>(sums + 2 * i + (SWIGLU ? h * 64 + (i >= 32 ? 64 : 0) : h * 128)) =
+                        make_float4(low(acc[i]), high(acc[i]), low(acc[i + 1]), high(acc[i + 1]));
                 continue;
             }
             const bool in = limit != 0 && lane < rows;
@@ -887,58 +900,13 @@ __global__ void __launch_bounds__(PR_THREADS, 1)
     cluster_sync();   // the pair's MMAs, copies and signals are over in both CTAs; SPLIT: everybody's sums are there
     if constexpr (SPLIT) {
         if (warp >= 4 && pair < n_tiles) {
-            // a warp finishes 32 columns (SwiGLU: 16 gate columns and their up columns) of 32 tokens at a time
-            const int w8 = warp - 4, c0 = SWIGLU ? w8 * 16 : w8 * 32;
-            const int quarters = 4 / g.split;
+            // every CTA of the cluster finishes some of the tokens, a warp a token at a time
+            const int ctas = 2 * g.split;
             const bool ok = *abort_flag == 0;
             int group = 0;
             const Tile t = find_tile(sh, g, pair, group);
-            for (int q = part * quarters; q < (part + 1) * quarters; ++q) {
-                const int rows = t.rows - rank * 128 - q * 32;
-                if (rows <= 0) break;
-                const int row = t.t0 + rank * 128 + q * 32 + lane;
-                const uint32_t at = smem_u32(ring) + (uint32_t)(c0 * 128 + q * 32 + lane) * 4u;
-                float v[32];
-#pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = 0.0f;
-                for (int p = 0; p < g.split; ++p) {
-                    const uint32_t peer = map_to_cta(at, (uint32_t)(2 * p + rank));
-                    float o[32];
-#pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(o[i]) : "r"(peer + (uint32_t)((SWIGLU && i >= 16 ? 112 : 0) + i) * 512u));
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] += o[i];
-                }
-                if constexpr (SWIGLU) {
-                    float big = 0.0f;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        v[i] = silu_times(v[i], v[16 + i]);
-                        big = max_magnitude(big, v[i]);
-                    }
-                    float (*peak)[32] = reinterpret_cast<float (*)[32]>(&sh.peak[0][0]);
-                    peak[w8][lane] = big;
-                    asm volatile("bar.sync 1, 256;" ::: "memory");
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) big = max_magnitude(big, peak[i][lane]);
-                    const OutScale s(big);
-                    asm volatile("bar.sync 1, 256;" ::: "memory");   // (all have read before one writes again)
-                    if (ok && lane < rows) {
-                        uint32_t c[4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) c[i] = code2(v[4 * i], v[4 * i + 1], s.r) | code2(v[4 * i + 2], v[4 * i + 3], s.r) << 16;
-                        *reinterpret_cast<uint4 *>(static_cast<uint8_t *>(g.y) + (size_t)row * g.n + t.nt * 128 + c0) = make_uint4(c[0], c[1], c[2], c[3]);
-                        if (w8 == 0) g.ys[(size_t)row * (g.n / 128) + t.nt] = s.scale;
-                    }
-                } else if (ok && lane < rows) {
-#pragma unroll
-                    for (int i = 0; i < 32; i += 4) {
-                        const int col = t.nt * PR_TILE + c0 + i;
-                        if (col < g.n) store4(g, (size_t)row * g.n + col, make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]));
-                    }
-                }
-            }
+            for (int c = (int)cluster_rank() + (warp - 4) * ctas; c < t.rows; c += PR_EPI_WARPS * ctas)
+                finish_token<SWIGLU>(g, smem_u32(ring) + (c & 127) * (ST_RED_PITCH * 4), g.split, 2, c >> 7, (size_t)(t.t0 + c), t.nt, ok, lane);
         }
         cluster_sync();   // nobody leaves while a peer reads its sums
     }
@@ -1067,12 +1035,13 @@ spice_status launch_gemm_e4m3(GemmE4m3Args g, const uint8_t *x, const uint8_t *w
         !tc_encode_map2_bytes(&map_y, g.y, (uint64_t)g.T, (uint64_t)g.n * row_bytes, 32))
         return SPICE_ERR_CUDA;
     // Fewer tiles than pairs: two or four pairs share a tile's reduction, as long as all the clusters run at once and the reduction is
-    // long: 470 ns a block against a start of 4.5 us, or 12 with the sums of the cluster (77 x 3584 x 20480 with one / two / four
-    // pairs to a tile: 82 / 52 / 34.5 us; 77 x 2048 x 2816 15.5 / 16.4 / 15.6).
+    // long: 470 ns a block against a start of 4.5 us, or 6.8 with the cluster and 26 ns for a token's sums.  With one / two / four pairs
+    // to a tile, us: 77 x 3584 x 20480 81 / 48 / 30, 256 tokens 76 / 57 / 37;  2048 x 2816 with 33 tokens 14.2 / 12.4 / 10.6, with 77
+    // 15.4 / 13.5 / 12.5, with 256 15.4 / 17.4 / 16.6;  512 x 1024 with 77 8.5 / 9.6 / 9.4;  400 x 2048 x 8192 33.8 / 29.2.
     int share = 1;
     int64_t best = 4500 + 470 * (int64_t)g.kb;
     for (int s = 2; s <= 4 && g.G == 1; s *= 2) {
-        const int64_t ns = 12000 + 470 * (int64_t)((g.kb + s - 1) / s);
+        const int64_t ns = 6800 + 26 * std::min(g.T, PR_TILE) + 470 * (int64_t)((g.kb + s - 1) / s);
         if (most <= facts->clusters[2 * s] && ns < best) {
             best = ns;
             share = s;
