@@ -1006,9 +1006,9 @@ spice_status launch_gemm_e4m3(GemmE4m3Args g, const uint8_t *x, const uint8_t *w
         }
     }
     // Few rows: streamed weights, at the rate of HBM as long as the warp-wide products (400 per cycle and SM) keep up.  Streamed / by
-    // pairs of CTAs, us, dense 2048 x 2816, 3584 x 20480, SwiGLU 5632 x 2048:  16 tokens 6.8/12.4, 18.9/29, 8.1/13;  32 tokens 9.6/13,
-    // 28.9/30.8, 11.1/12.9;  64 tokens 14.7/14.7, 56/34, 19.4/13.4.  64 groups of 2048 x 1408, SwiGLU 2816 x 2048:  96 rows 34.6/49,
-    // 65/94;  400 rows 38.8/50, 80/103;  768 rows 57/51, 116/103.
+    // pairs of CTAs, us, dense 2048 x 2816, 3584 x 20480, SwiGLU 2816 x 2048:  16 tokens 6.8/10.0, 18.6/26.7, 8.0/11.6;  32 tokens
+    // 9.4/10.6, 28.6/27.5, 11.0/12.0;  64 tokens (when it took them) 14.7/12.0, 56/29.5, -/13.3.  64 groups of 2048 x 1408, SwiGLU
+    // 1408 x 2048:  96 rows 34.6/49, 65/94;  400 rows 38.8/50, 80/103;  768 rows 57/51, 116/103.
     if (g.G == 1 ? g.T <= 32 : rows <= 8) {
         CUtensorMap map_w;
         if (!tc_encode_map2_bytes(&map_w, w, (uint64_t)g.G * w_rows, (uint64_t)g.k, 128)) return SPICE_ERR_CUDA;
