@@ -283,7 +283,7 @@ __global__ void __launch_bounds__(ST_THREADS, 1)
     if (warp == ST_WARPS) {
         uint32_t s = 0, phase = 1, filled = 0, limit = g.wait_limit;
         int group = 0;
-        for (int item = team; item < n_items && limit != 0; item += teams) {
+        for (int item = team; item < n_items && (SPLIT || limit != 0); item += teams) {
             const Tile t = find(item, group);
             const int w0 = SWIGLU ? 2 * t.group * g.n + t.nt * 128 : t.group * g.n + t.nt * 256, w1 = SWIGLU ? w0 + g.n : w0 + 128;
             for (int b = kb0; b < kb0 + kbs; ++b) {
@@ -308,6 +308,11 @@ __global__ void __launch_bounds__(ST_THREADS, 1)
                     phase ^= 1;
                 }
             }
+            if (SPLIT) {   // the sums lie in the ring between these two: the next item is ordered behind them
+                __syncwarp();
+                cluster_sync();
+                cluster_sync();
+            }
         }
         // everything that was ordered has landed before the CTA ends
         asm volatile("cp.async.wait_all;" ::: "memory");
@@ -319,11 +324,6 @@ __global__ void __launch_bounds__(ST_THREADS, 1)
                     break;
                 }
             }
-        __syncwarp();
-        if (SPLIT) {
-            cluster_sync();
-            cluster_sync();
-        }
     } else {
         const int r4 = lane >> 2, c2 = 2 * (lane & 3);
         const int row_blocks = ((SWIGLU ? 2 * g.n : g.n) + 127) / 128;
@@ -385,7 +385,10 @@ __global__ void __launch_bounds__(ST_THREADS, 1)
             }
             const bool ok = limit != 0;
             if constexpr (SPLIT) {
-                // ---- one item per cluster: sums as [token][256 weight rows] over the ring, which nobody fills any more
+                // ---- sums as [token][256 weight rows] over the ring, which is filled again behind the second barrier only.  A cluster has
+                // one item; where groups overlap there are more items than clusters.  Every warp of every CTA passes two cluster barriers
+                // per item, also after an expired wait, and all CTAs of a cluster count the same items: none waits for an arrival that
+                // does not come.
                 asm volatile("bar.sync 1, 256;" ::: "memory");   // (all have read their last stage)
                 float *red = reinterpret_cast<float *>(ring);
 #pragma unroll
@@ -398,7 +401,8 @@ __global__ void __launch_bounds__(ST_THREADS, 1)
                 // every CTA finishes some of the tokens, a warp a token at a time
                 for (int c = rank + warp * split; c < t.rows; c += ST_WARPS * split)
                     finish_token<SWIGLU>(g, smem_u32(red + c * ST_RED_PITCH), split, 1, 0, (size_t)(t.t0 + c), t.nt, ok, lane);
-                cluster_sync();   // nobody leaves while a peer reads its sums
+                if (item + teams < n_items) fence_proxy_async();   // (copies will write where the sums were)
+                cluster_sync();   // nobody leaves, or fills the ring, while a peer reads its sums
             } else if constexpr (SWIGLU) {
 #pragma unroll
                 for (int i = 0; i < NT; ++i) {
@@ -446,10 +450,6 @@ __global__ void __launch_bounds__(ST_THREADS, 1)
                             if (c < t.rows && col < g.n) store1(g, (size_t)(t.t0 + c) * g.n + col, acc[r][i][j]);
                         }
             }
-        }
-        if (SPLIT && team >= n_items) {   // (there is an item for every cluster unless offsets were bad)
-            cluster_sync();
-            cluster_sync();
         }
     }
     __syncthreads();
