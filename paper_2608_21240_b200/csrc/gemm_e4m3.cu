@@ -283,6 +283,18 @@ __global__ void __launch_bounds__(ST_THREADS, 1)
     if (warp == ST_WARPS) {
         uint32_t s = 0, phase = 1, filled = 0, limit = g.wait_limit;
         int group = 0;
+        auto land = [&]() {   // everything that was ordered has landed
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            if (lane == 0)
+                for (uint32_t left = filled; left > 0; --left) {
+                    const uint32_t back = s >= left ? 0u : 1u;   // the stage filled `left` blocks ago: in this round of the ring, or the one before
+                    if (!mbar_drain(full0 + (s + back * STAGES - left) * 8, phase ^ 1 ^ back)) {
+                        *abort_flag = 1;
+                        break;
+                    }
+                }
+            __syncwarp();
+        };
         for (int item = team; item < n_items && (SPLIT || limit != 0); item += teams) {
             const Tile t = find(item, group);
             const int w0 = SWIGLU ? 2 * t.group * g.n + t.nt * 128 : t.group * g.n + t.nt * 256, w1 = SWIGLU ? w0 + g.n : w0 + 128;
@@ -309,21 +321,13 @@ __global__ void __launch_bounds__(ST_THREADS, 1)
                 }
             }
             if (SPLIT) {   // the sums lie in the ring between these two: the next item is ordered behind them
-                __syncwarp();
+                land();
+                filled = 0;
                 cluster_sync();
                 cluster_sync();
             }
         }
-        // everything that was ordered has landed before the CTA ends
-        asm volatile("cp.async.wait_all;" ::: "memory");
-        if (lane == 0)
-            for (uint32_t left = filled; left > 0; --left) {
-                const uint32_t back = s >= left ? 0u : 1u;   // the stage filled `left` blocks ago: in this round of the ring, or the one before
-                if (!mbar_drain(full0 + (s + back * STAGES - left) * 8, phase ^ 1 ^ back)) {
-                    *abort_flag = 1;
-                    break;
-                }
-            }
+        if (!SPLIT) land();   // before the CTA ends
     } else {
         const int r4 = lane >> 2, c2 = 2 * (lane & 3);
         const int row_blocks = ((SWIGLU ? 2 * g.n : g.n) + 127) / 128;
