@@ -391,8 +391,8 @@ spice_status spice_quantize_e4m3_blocks(const spice_bf16 *w, int64_t count, int6
  *   Any scales are taken, not only those of the quantiser.
  *   offset [n_groups + 1] int32, device: group g has the rows offset[g] .. offset[g+1]-1; rows of y outside of all groups are
  *   left as they are.  NULL with n_groups = 1: all T rows.  A group whose offsets are not in order, or outside 0 .. T, counts as
- *   empty, and SPICE_ERR_BAD_TABLE is reported (rows that then are in several groups: any of these may have written them, or
- *   none).
+ *   empty, and SPICE_ERR_BAD_TABLE is reported.  Rows that then are in one group only are that group's; of rows in several, any of
+ *   these may have written an element, or none (added outputs: any number of them may have been added).
  *   out, y [T, n]: as in spice_gemm_i8.  device_status: optional device int32 which the caller has set to 0: raised to
  *   SPICE_ERR_BAD_TABLE or SPICE_ERR_TIMEOUT (a bounded wait inside the kernel expired: the outputs are undefined then).
  *   y is device memory (bulk copies write it).  k a multiple of 16, n a multiple of 8; T, n, k up to 2^24, n_groups up to 1024, n_groups * n below 2^31

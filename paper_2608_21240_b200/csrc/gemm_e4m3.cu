@@ -477,12 +477,30 @@ __device__ __forceinline__ int4 load_again(const int4 *p) {
     return v;
 }
 
-// The slot-th group that has rows: its number, or -1; groups whose offsets are not in order or out of range have none.
+// The slot-th group that has a row which no group before it has: its number, or -1; groups whose offsets are not in order or out
+// of range have no rows.  There are no more of these groups than rows, so a block for each row is enough; all rows of a group that is
+// passed over belong to others too.  Groups overlap only behind offsets that fall.
 __device__ __forceinline__ int find_group(const GemmE4m3Args &g, int slot, const int32_t *off) {
     const int lane = threadIdx.x & 31;
+    uint32_t taken = 0;   // rows of the groups before, a bit each
+    bool falls = false;
     for (int base = 0, seen = 0; base < g.G; base += 32) {
-        const int i = base + lane;
-        uint32_t mask = __ballot_sync(0xffffffffu, i < g.G && off[i] >= 0 && off[i + 1] > off[i] && off[i + 1] <= g.T);
+        const int i = base + lane, b = i < g.G ? off[i] : 0, e = i < g.G ? off[i + 1] : 0;
+        uint32_t own = b >= 0 && e > b && e <= g.T ? (1u << e) - (1u << b) : 0u;
+        falls = falls || __any_sync(0xffffffffu, e < b);
+        const uint32_t all = taken | __reduce_or_sync(0xffffffffu, own);
+        if (falls) {
+            uint32_t before = own;
+#pragma unroll
+            for (int o = 1; o < 32; o *= 2) {
+                const uint32_t v = __shfl_up_sync(0xffffffffu, before, o);
+                if (lane >= o) before |= v;
+            }
+            before = __shfl_up_sync(0xffffffffu, before, 1);
+            own &= ~(taken | (lane > 0 ? before : 0u));
+        }
+        taken = all;
+        uint32_t mask = __ballot_sync(0xffffffffu, own != 0);
         const int here = __popc(mask);
         if (seen + here > slot) {
             for (int s = slot - seen; s > 0; --s) mask &= mask - 1;
@@ -507,7 +525,7 @@ __global__ void __launch_bounds__(FEW_WARPS * 32) gemm_e4m3_few_kernel(const uin
             for (int i = threadIdx.x; i < g.G; i += FEW_WARPS * 32)
                 if (off[i] < 0 || off[i + 1] < off[i] || off[i + 1] > g.T) atomicMax(g.status, (int)SPICE_ERR_BAD_TABLE);
     }
-    // (there are T blocks: where offsets overlap, groups may be left out.  A loop over them costs registers, and 12 for 9 us)
+    // (a loop over more groups than a block for each row costs registers, and 12 for 9 us)
     const int group = g.offset ? find_group(g, blockIdx.y, off) : 0;
     if (group < 0) return;
     const int begin = g.offset ? off[group] : 0, rows = g.offset ? off[group + 1] - begin : g.T;

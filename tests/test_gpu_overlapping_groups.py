@@ -41,8 +41,9 @@ class Calls:
         assert all((o[T:] == o[T, 0]).all() for o in outs)
         return [o[:T] for o in outs]
 
-    def check(self, bounds, status=BAD_TABLE):
+    def check(self, bounds):
         T, G = self.T, self.G
+        status = BAD_TABLE if any(not 0 <= a <= b <= T for a, b in zip(bounds, bounds[1:])) else 0
         untouched = self.run([T] * (G + 1))
         of_kind = [self.run([0] * (g + 1) + [T] * (G - g)) for g in range(min(KINDS, G))]
         assert not torch.equal(of_kind[0][0], untouched[0])
@@ -87,6 +88,30 @@ def test_groups_out_of_order_that_do_not_overlap(op, T, G, n, k):
     c = Calls(op, T, G, n, k)
     c.check([T // 2, T, 0, T // 2 - 3, T // 2 - 1, T + 5, -7, 3, T // 2])
     c.check([5, 9, 0, T, 2, 2, 1, 0, T - 1])
+
+
+# (up to eight tokens: a block for each row, straight from global memory)
+@pytest.mark.parametrize("G,n,k", [(18, 136, 528), (40, 72, 272), (1024, 24, 144)])
+def test_up_to_eight_tokens_of_more_groups_than_blocks(G, n, k):
+    c = Calls("product", 8, G, n, k)
+    c.check([0, 1] * (G // 2) + [8])                          # row 0 over and over, then the others
+    c.check([7, 8] * (G // 2 - 1) + [0, 8, 3])
+    c.check([0, 8] * (G // 2) + [8])
+    c.check([3, 5] * (G // 2 - 2) + [0, 2, 1, 4, 8])
+
+
+@pytest.mark.parametrize("T", [1, 5, 8, 26])
+@pytest.mark.parametrize("G", [3, 17, 70])
+def test_any_offsets(T, G):
+    c = Calls("product", T, G, 72, 400)
+    g = torch.Generator().manual_seed(T + G)
+    for i in range(12):
+        bounds = torch.randint(-1 if i % 2 else 0, T + 1 + i % 2, (G + 1,), generator=g).tolist()
+        if i % 3 == 0:                                         # in order but for one offset or two
+            bounds = sorted(max(0, min(T, b)) for b in bounds)
+            for j in torch.randint(0, G + 1, (2,), generator=g).tolist():
+                bounds[j] = int(torch.randint(0, T + 1, (1,), generator=g))
+        c.check(bounds)
 
 
 @pytest.mark.parametrize("op,n", [("product", 136), ("swiglu", 128)])
