@@ -41,6 +41,7 @@ struct GemmE4m3Args {
     int32_t *status;         // optional
     uint32_t wait_limit;     // polls after which a wait inside a kernel gives up
     int32_t n_tiles;         // tiles along n
+    uint32_t most_tiles;     // tiles of a call, at most: groups that overlap can have more of them than an index holds
     int32_t split;           // some rows a group: CTAs of a cluster that share a reduction
     int32_t sectors;         // rows of y begin on 32-byte boundaries
 };
@@ -156,13 +157,15 @@ static_assert(stream_smem<4>() <= 232448, "what a block can have");
 static_assert(32 * ST_RED_PITCH * 4 <= 6 * ST_W_BYTES, "the sums fit in the ring");
 
 // Tiles before each group, by one warp: per group (its rows / `rows`, rounded up) x n_tiles; a group whose offsets are not in
-// order or out of range has none.
+// order or out of range has none.  Sums stop at g.most_tiles, which is 2^30 at most: only groups that overlap get there (512 of
+// 1024 groups with all rows each, say), and what is behind it is left out.
 __device__ __forceinline__ void count_tiles(const GemmE4m3Args &g, int rows, int32_t *first) {
     const int lane = threadIdx.x & 31;
-    int carry = 0;
+    uint32_t carry = 0;
     for (int base = 0; base < g.G; base += 32) {
         const int i = base + lane;
-        int b = 0, e = g.T, tiles = 0;
+        int b = 0, e = g.T;
+        uint32_t tiles = 0;
         if (i < g.G && g.offset) {
             b = load_s32(g.offset + i);
             e = load_s32(g.offset + i + 1);
@@ -174,16 +177,17 @@ __device__ __forceinline__ void count_tiles(const GemmE4m3Args &g, int rows, int
                 tiles = (e - b + rows - 1) / rows * g.n_tiles;
             }
         }
-        int incl = tiles;
+        uint32_t incl = min(tiles, g.most_tiles);
 #pragma unroll
         for (int o = 1; o < 32; o *= 2) {
-            const int v = __shfl_up_sync(0xffffffffu, incl, o);
-            if (lane >= o) incl += v;
+            const uint32_t v = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl = min(incl + v, g.most_tiles);
         }
-        if (i < g.G) first[i] = carry + incl - tiles;
-        carry += __shfl_sync(0xffffffffu, incl, 31);
+        incl = min(incl + carry, g.most_tiles);
+        if (i < g.G) first[i + 1] = (int)incl;
+        carry = __shfl_sync(0xffffffffu, incl, 31);
     }
-    if (lane == 0) first[g.G] = carry;
+    if (lane == 0) first[0] = 0;
 }
 
 struct Tile {
@@ -1076,6 +1080,7 @@ spice_status launch_gemm_e4m3(GemmE4m3Args g, const uint8_t *x, const uint8_t *w
                           map_x16, map_y, g);
     } else {
         const int pairs = (int)std::min<int64_t>(sms / 2, most);
+        g.most_tiles = (uint32_t)std::min<int64_t>(g.most_tiles, (int64_t)(0x7fffffff / g.kb) * pairs);   // (a pair counts its blocks in 32 bits)
         ok = launch_early(gemm_e4m3_pair_kernel<SWIGLU, false>, dim3(2 * (unsigned)pairs), PR_THREADS, PR_SMEM_BYTES, st, 2, map_w, map_x128, map_x16, map_y, g);
     }
     return ok ? SPICE_OK : SPICE_ERR_CUDA;
@@ -1098,6 +1103,7 @@ spice_status call_gemm_e4m3(const uint8_t *x_q, const float *x_scale, const uint
         misaligned4(x_scale) || misaligned4(w_scale) || misaligned4(offset) || misaligned4(y_scale) || misaligned4(device_status))
         return SPICE_ERR_INVALID_ARG;
     GemmE4m3Args g{};
+    g.most_tiles = 1u << 30;
     g.xs = x_scale;
     g.ws = w_scale;
     g.offset = offset;
