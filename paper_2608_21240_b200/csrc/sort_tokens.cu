@@ -139,7 +139,8 @@ __global__ void __launch_bounds__(SMALL_THREADS) sort_small_kernel(const SortArg
 // ------------------------------------------------------------------------------------------------ many entries
 // A cluster counts: each of its warps owns a run of consecutive entries and a row of counters in shared memory; a first pass
 // counts, prefix sums over experts, blocks and warps turn the counters into places, a second pass hands the places out.
-constexpr int SORT_CTAS = 8, SORT_THREADS = 1024, SORT_WARPS = SORT_THREADS / 32, SORT_KEPT = 8;
+constexpr int SORT_CTAS = 8, SORT_THREADS = 1024, SORT_WARPS = SORT_THREADS / 32, SORT_KEPT = 8, SORT_EXPERTS = 1024;
+constexpr size_t sort_smem(int experts) { return (size_t)(SORT_WARPS * (experts | 1) + experts) * 4; }
 
 __global__ void __launch_bounds__(SORT_THREADS, 1) sort_cluster_kernel(const SortArgs a) {
     extern __shared__ int32_t smem[];
@@ -463,6 +464,18 @@ __global__ void __launch_bounds__(256, ROW32 || DY32 ? 4 : 8) grad_token_kernel(
 bool misaligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
 constexpr int64_t MAX_ENTRIES = 1 << 28;
 
+// Raises the cluster kernel's limit on the current device to what the most experts take.  The limit belongs to the kernel, not to a
+// call: all threads set the same value, so that none lowers it between another's setting and launch.
+bool raise_sort_smem() {
+    static std::atomic<bool> raised[64];
+    int dev = 0;
+    if (current_device_sms(&dev) <= 0) return false;
+    if (raised[dev].load(std::memory_order_acquire)) return true;
+    if (cudaFuncSetAttribute(sort_cluster_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sort_smem(SORT_EXPERTS)) != cudaSuccess) return false;
+    raised[dev].store(true, std::memory_order_release);
+    return true;
+}
+
 }  // namespace
 
 }  // namespace spice
@@ -474,7 +487,7 @@ extern "C" spice_status spice_sort_tokens(const int32_t *idx, int32_t T, int32_t
                                           const float *x_scale, int32_t scale_cols, float *rows_scale, void *stream) {
     Range range_("spice_sort_tokens");
     if (T < 0 || top_k < 1 || n_experts < 1 || !offset || misaligned4(offset)) return SPICE_ERR_INVALID_ARG;
-    if (n_experts > 1024 || top_k > 32 || (int64_t)T * top_k > MAX_ENTRIES) return SPICE_ERR_UNSUPPORTED_SHAPE;
+    if (n_experts > SORT_EXPERTS || top_k > 32 || (int64_t)T * top_k > MAX_ENTRIES) return SPICE_ERR_UNSUPPORTED_SHAPE;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (T == 0) return SPICE_OK;
     if (!x != !rows || (!x && (x_scale || rows_scale)) || !x_scale != !rows_scale || (x && (row_bytes < 16 || row_bytes % 16)) ||
@@ -488,9 +501,8 @@ extern "C" spice_status spice_sort_tokens(const int32_t *idx, int32_t T, int32_t
     if (a.n <= SMALL_N) return launch_early(sort_small_kernel, dim3((unsigned)T), SMALL_THREADS, 0, st, 1, a) ? SPICE_OK : SPICE_ERR_CUDA;
     const int64_t gather_blocks = ((int64_t)T * (a.vecs + a.ns) + 255) / 256;
     if (gather_blocks > 0x7fffffffLL) return SPICE_ERR_UNSUPPORTED_SHAPE;
-    const size_t smem = (size_t)(SORT_WARPS * (n_experts | 1) + n_experts) * 4;
-    if (smem > 48 * 1024 && cudaFuncSetAttribute(sort_cluster_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
-        return SPICE_ERR_CUDA;
+    const size_t smem = sort_smem(n_experts);
+    if (smem > 48 * 1024 && !raise_sort_smem()) return SPICE_ERR_CUDA;
     if (!launch_early(sort_cluster_kernel, dim3(SORT_CTAS), SORT_THREADS, smem, st, SORT_CTAS, a)) return SPICE_ERR_CUDA;
     if (rows && !launch_early(gather_kernel, dim3((unsigned)gather_blocks), 256, 0, st, 1, a)) return SPICE_ERR_CUDA;
     return SPICE_OK;
