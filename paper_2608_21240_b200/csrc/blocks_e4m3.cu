@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const BlockArgs a) {
 __global__ void __launch_bounds__(256) quantize_squares_kernel(const BlockArgs a) {
     __shared__ uint32_t part[8];
     grid_dependency();
-    const int row_blocks = (a.rows + 127) / 128;
+    const int row_blocks = a.rows / 128 + (a.rows % 128 != 0);   // (rows + 127 may not fit)
     const int64_t rb = blockIdx.x / a.kb;
     const int col = (int)(blockIdx.x - rb * a.kb) * 128 + (threadIdx.x & 15) * 8;
     const int64_t matrix = rb / row_blocks;

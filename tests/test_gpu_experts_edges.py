@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from paper_2608_21240_b200 import binding as B
+from tests.test_gpu_e4m3_blocks import plain_quantiser
 from tests.test_gpu_sort_tokens import make_idx, plain_sort
 
 pytestmark = pytest.mark.gpu
@@ -40,3 +41,33 @@ def test_sorts_of_different_numbers_of_experts_from_several_threads():
     for t in threads:
         t.join()
     assert not failed, failed
+
+
+def test_quantiser_of_the_most_rows():
+    """2^31 - 1 rows: the places of blocks and rows fill 32 bits.  All zeros but for some blocks at the ends and in the middle."""
+    rows = 2 ** 31 - 1
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("needs 52 GB of device memory")
+    w = torch.zeros(rows, 8, dtype=bf, device="cuda")
+    q = torch.full((rows, 8), 0x55, dtype=u8, device="cuda")
+    blocks = 2 ** 24
+    scale = torch.full((blocks, 1), -3.0, device="cuda")
+    filled = [0, 1, blocks // 2, blocks - 2, blocks - 1]
+    for i in filled:
+        part = w[i * 128:(i + 1) * 128]
+        part.copy_(torch.randn(part.shape, device="cuda"))
+    B.spice_quantize_e4m3_blocks(w, q, scale, 128)
+    torch.cuda.synchronize()
+    for i in filled:
+        want_q, want_s = plain_quantiser(w[i * 128:(i + 1) * 128], 128)
+        assert torch.equal(q[i * 128:(i + 1) * 128].view(torch.float8_e4m3fn).double(), want_q)
+        assert abs(float(scale[i]) - float(want_s)) <= 2.0 ** -24 * float(want_s)
+        q[i * 128:(i + 1) * 128] = 0
+        scale[i] = 1
+    assert (scale == 1).all()
+    flat = q.view(-1)
+    for a in range(0, flat.numel(), 1 << 32):
+        assert not flat[a:a + (1 << 32)].any()
+    del w, q, scale, flat
+    torch.cuda.empty_cache()
