@@ -62,7 +62,7 @@ __device__ __forceinline__ void gather_row(const SortArgs &a, int t, const int32
             if (pos[k] >= 0) a.rows[(size_t)pos[k] * a.vecs + v] = x;
     }
     if (!a.xs) return;
-    for (int v = threadIdx.x; v < a.ns; v += blockDim.x) {
+    for (uint32_t v = threadIdx.x; v < (uint32_t)a.ns; v += blockDim.x) {   // (up to 2^31 - 1 scales: the step behind them has to fit)
         const float x = load4(a.xs + (size_t)t * a.ns + v);
         for (int k = 0; k < a.K; ++k)
             if (pos[k] >= 0) a.rs[(size_t)pos[k] * a.ns + v] = x;
@@ -499,7 +499,7 @@ extern "C" spice_status spice_sort_tokens(const int32_t *idx, int32_t T, int32_t
     const SortArgs a{idx, offset, pos, entry, T, top_k, n_experts, T * top_k, static_cast<const uint4 *>(x), static_cast<uint4 *>(rows),
                      x ? row_bytes / 16 : 0, x_scale, rows_scale, x_scale ? scale_cols : 0};
     if (a.n <= SMALL_N) return launch_early(sort_small_kernel, dim3((unsigned)T), SMALL_THREADS, 0, st, 1, a) ? SPICE_OK : SPICE_ERR_CUDA;
-    const int64_t gather_blocks = ((int64_t)T * (a.vecs + a.ns) + 255) / 256;
+    const int64_t gather_blocks = ((int64_t)T * ((int64_t)a.vecs + a.ns) + 255) / 256;   // (fewer than 2^31: a sum that does not fit an int is refused)
     if (gather_blocks > 0x7fffffffLL) return SPICE_ERR_UNSUPPORTED_SHAPE;
     const size_t smem = sort_smem(n_experts);
     if (smem > 48 * 1024 && !raise_sort_smem()) return SPICE_ERR_CUDA;

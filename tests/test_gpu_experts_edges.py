@@ -71,3 +71,24 @@ def test_quantiser_of_the_most_rows():
         assert not flat[a:a + (1 << 32)].any()
     del w, q, scale, flat
     torch.cuda.empty_cache()
+
+
+def test_sort_with_the_widest_scales():
+    """2^31 - 1 scales a row: the columns behind the last one do not fit 32 bits with a sign."""
+    n = 2 ** 31 - 1
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("needs 18 GB of device memory")
+    xs = torch.zeros(1, n, device="cuda")
+    xs[0, -300:] = torch.arange(300.0, device="cuda")
+    xs[0, ::1 << 20] = 5.0
+    rs = torch.full((1, n), -1.0, device="cuda")
+    x = torch.randn(1, 8, device="cuda").to(bf)
+    rows = torch.zeros(1, 8, dtype=bf, device="cuda")
+    off, pos, entry = (torch.full(s, -7, dtype=i32, device="cuda") for s in ((4,), (1, 1), (1,)))
+    B.spice_sort_tokens(torch.full((1, 1), 2, dtype=i32, device="cuda"), off, pos, entry, x, rows, xs, rs)
+    torch.cuda.synchronize()
+    assert off.tolist() == [0, 0, 0, 1] and pos.tolist() == [[0]] and entry.tolist() == [0]
+    assert torch.equal(rows, x) and torch.equal(rs, xs)
+    del xs, rs
+    torch.cuda.empty_cache()
