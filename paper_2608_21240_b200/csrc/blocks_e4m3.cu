@@ -147,10 +147,12 @@ extern "C" spice_status spice_quantize_e4m3_blocks(const spice_bf16 *w, int64_t 
         return SPICE_ERR_INVALID_ARG;
     const BlockArgs a{reinterpret_cast<const __nv_bfloat16 *>(w), q, scale, row_blocks * count, (int32_t)rows, cols, kb};
     const int64_t blocks = a.blocks * kb;
+    const int sms = current_device_sms();
+    if (sms <= 0) return SPICE_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     bool ok;
     if (block_rows == 128) ok = launch_early(quantize_squares_kernel, dim3((unsigned)blocks), 256, 0, st, 1, a);
-    else if (blocks < 16 * 4 * 148) ok = launch_early(quantize_rows_kernel<1>, dim3((unsigned)((blocks + 15) / 16)), 256, 0, st, 1, a);
+    else if (blocks < 16 * 4 * sms) ok = launch_early(quantize_rows_kernel<1>, dim3((unsigned)((blocks + 15) / 16)), 256, 0, st, 1, a);
     else ok = launch_early(quantize_rows_kernel<4>, dim3((unsigned)((blocks + 63) / 64)), 256, 0, st, 1, a);
     return ok ? SPICE_OK : SPICE_ERR_CUDA;
 }
