@@ -62,6 +62,27 @@ def test_codes_of_exact_sums(T, inter, k, G):
     assert check_activations(q[bounds[0]:bounds[-1]], s[bounds[0]:bounds[-1]], e, torch.zeros_like(e)) < 1e-3
 
 
+@pytest.mark.parametrize("T", [1, 20, 300])
+def test_gates_that_count_as_zero(T):
+    """Gates of -100 under up products of 1e20: activations of 4e-22, where exp(100) is beyond fp32, count as 0.  A block of nothing else is a block of zeros; beside
+    other gates they have codes of zero."""
+    inter, k = 256, 128
+    one, x = 0x38, torch.full((T, k), 0x38, dtype=u8, device="cuda")
+    w = torch.full((2 * inter, k), one, dtype=u8, device="cuda")
+    w[:inter] = one | 0x80                                        # -1
+    w[128:256:3] = 0x08                                           # 2^-6
+    ws = torch.tensor([[100 / 128], [100 / 128], [1e20 / 128], [1e20 / 128]], device="cuda")
+    q, s = torch.full((T, inter), 0x55, dtype=u8, device="cuda"), torch.full((T, 2), 3.0, device="cuda")
+    B.spice_swiglu_e4m3_blocks(x, torch.ones(T, 1, device="cuda"), w, ws, q, s)
+    torch.cuda.synchronize()
+    g = torch.tensor(100 / 64, dtype=f64)
+    a = float(g * torch.sigmoid(g) * 1e20)
+    v = q.view(E4M3).to(f64)
+    assert (v[:, :128] == 0).all() and (s[:, 0] == 1).all()
+    assert (v[:, 128::3] == 448).all() and (v[:, 129::3] == 0).all() and (v[:, 130::3] == 0).all()
+    assert ((s[:, 1].to(f64) * 448 - a).abs() <= 32 * H32 * a).all()
+
+
 @pytest.mark.parametrize("T,n,k,G", [(1, 264, 2048, 0), (8, 136, 4112, 0), (32, 520, 20480, 0), (77, 264, 20480, 0), (300, 136, 16400, 0), (24, 264, 8208, 16),
                                      (700, 264, 8208, 5)])
 def test_products_of_exact_sums(T, n, k, G):
