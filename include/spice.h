@@ -352,7 +352,8 @@ spice_status spice_route_scored(const float *logits, const float *bias, int32_t 
  *   x [T, row_bytes], optional: rows of any type (row_bytes a multiple of 16) -> rows [T * top_k, row_bytes]: rows[p] = x[entry[p] / top_k];
  *   x_scale [T, scale_cols] fp32, optional with x -> rows_scale [T * top_k, scale_cols], likewise.
  *   Rows behind the kept ones are left as they are.  The gradient of x is spice_combine_tokens of the rows' gradients without gates.
- *   The same expert may stand twice in a token's row: both entries are kept.  (T = 0 writes nothing, offset neither.)
+ *   The same expert may stand twice in a token's row: both entries are kept.  (T = 0 writes nothing, offset
+ *   neither: who reads offset after an empty batch sets it to zeros.)
  *   n_experts up to 1024, top_k up to 32, T * top_k up to 2^28 (SPICE_ERR_UNSUPPORTED_SHAPE); x and rows 16-byte aligned. */
 spice_status spice_sort_tokens(const int32_t *idx, int32_t T, int32_t top_k, int32_t n_experts, int32_t *offset, int32_t *pos,
                                int32_t *entry, const void *x, int32_t row_bytes, void *rows, const float *x_scale,
@@ -378,7 +379,7 @@ spice_status spice_combine_tokens_grad(const void *dy, int32_t dy_type, const vo
 /* E4M3 codes (the format above) of bf16 matrices with a scale for each block of block_rows x 128 values, block_rows = 1 (rows of
  * activations) or 128 (weights); blocks at the ends are smaller.  With m = the block's largest magnitude:
  *     q = the E4M3 value nearest to 448 w / m (ties to the even code, rounded exactly),   scale = m / 448
- *   A block of zeros has codes 0 and scale 1; one with a value that is not finite has codes 0 and scale NaN.
+ *   A block of zeros has codes of zeros (with their signs) and scale 1; one with a value that is not finite has codes 0 and scale NaN.
  *   w, q [count, rows, cols];  scale [count, ceil(rows / block_rows), ceil(cols / 128)] fp32.  cols a multiple of 8 up to 2^24, rows
  *   and count below 2^31, at most 2^31 blocks of 128 x 128 and 2^35 of 1 x 128; w 16-byte, q 8-byte aligned. */
 spice_status spice_quantize_e4m3_blocks(const spice_bf16 *w, int64_t count, int64_t rows, int32_t cols, int32_t block_rows,
@@ -403,7 +404,8 @@ spice_status spice_gemm_e4m3_blocks(const uint8_t *x_q, const float *x_scale, co
                                     int32_t *device_status, void *stream);
 
 /* The gate and up products of a SwiGLU FFN in the same arithmetic, with activations that are rows of blocks again:
- *     g, u = rows j and inter + j of the product above,   a = g / (1 + exp(-g)) * u  (fp32, not rounded to bf16),
+ *     g, u = rows j and inter + j of the product above,   a = g / (1 + exp(-g)) * u  (fp32, not rounded to bf16; fast exponential and
+ *     quotient, off by (4 |g| + 16) 2^-24 of a; a gate below -87, where exp(-g) nears the end of fp32, counts as 0),
  *     act_q, act_scale = codes and scales of a in blocks of 1 x 128 along j (scale = m / 448 within an ulp, codes of the fp32
  *     quotient; a block below 2^-100 is taken for zeros)
  *   w_gate_up_q [n_groups, 2 inter, k]: inter gate rows, then inter up rows;  w_scale [n_groups, 2 inter / 128, ceil(k/128)];

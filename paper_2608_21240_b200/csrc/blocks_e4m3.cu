@@ -66,7 +66,8 @@ struct BlockScale {
     }
 };
 
-// 1 x 128: half a warp per block, U blocks to a half warp.
+// 1 x 128: half a warp per block, U blocks to a half warp.  333 x 2048 2.4 us (launch); 4096 x 2048 9.0, 24576 x 1408 28.5 us: 0.44 and 0.57
+// of the measured copy rate.
 template <int U>
 __global__ void __launch_bounds__(256) quantize_rows_kernel(const BlockArgs a) {
     grid_dependency();
@@ -96,7 +97,7 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const BlockArgs a) {
     }
 }
 
-// 128 x 128: a thread block per block, which it holds in registers.
+// 128 x 128: a thread block per block, which it holds in registers.  131072 x 1408 89 us, 0.96 of the measured copy rate.
 __global__ void __launch_bounds__(256) quantize_squares_kernel(const BlockArgs a) {
     __shared__ uint32_t part[8];
     grid_dependency();

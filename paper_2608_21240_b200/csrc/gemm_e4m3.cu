@@ -127,12 +127,13 @@ __device__ __forceinline__ void store1(const GemmE4m3Args &g, size_t at, float v
 // ------------------------------------------------------------------------------------------------ few rows a group
 // The weights stream through a ring in shared memory at the rate of HBM, and eight warps multiply them with up to 32 tokens in
 // warp-wide products: a warp has 32 weight rows (SwiGLU: 16 gate rows and their up rows) and all the tokens, so that only a stage's
-// operands pass through shared memory and no sums do.  (On tcgen05 the sums of every block would have to come back from tensor
-// memory, 0.47 us a block, more than a block of weights takes to arrive.)  Persistent over (group, 256 weight rows, up to 32
+// operands pass through shared memory and no sums do.  (In the pair kernel below, whose two accumulators let two blocks be on their way, the
+// sums of a block take 0.47 us through tensor memory and back, more than a block of weights takes to arrive.  That is a latency:
+// narrower accumulators, with the tokens as the N operand, could have more of them in flight.  Not built.)  Persistent over (group, 256 weight rows, up to 32
 // tokens); where those are fewer than the SMs, the CTAs of a cluster share the reduction of one and add up through distributed
-// shared memory.  96 rows over 64 groups: SwiGLU 1408 x 2048 60 us, 0.88 of the measured copy rate; product 2048 x 1408 33 us.
+// shared memory.  96 rows over 64 groups: SwiGLU 1408 x 2048 59 us, 0.89 of the measured copy rate; product 2048 x 1408 33 us, 0.80.
 // From 16 tokens on the products of a block (400 a cycle and SM) take longer than its weights: 3584 x 20480 with 1 / 16 / 32 tokens
-// 15.9 / 18.9 / 28.8 us.
+// 15.7 / 18.5 / 27.6 us.
 constexpr int ST_WARPS = 8, ST_THREADS = ST_WARPS * 32 + 32, ST_MAX_SPLIT = 8;
 constexpr int ST_W_BYTES = 256 * BK;
 constexpr int ST_RED_PITCH = 260;                 // fp32 sums of a token's 256 weight rows, padded against bank conflicts
@@ -632,7 +633,7 @@ __device__ __forceinline__ int copied(int rows, int rank) { return (min(max(rows
 
 // A block of the reduction is 128 x 128 values of both operands per CTA; its 256 x 256 sums come back from tensor memory, are scaled
 // and added in registers, a token per thread, while the other accumulator is multiplied into.  24576 rows over 64 groups of very
-// different sizes: product 2048 x 1408 101 to 104 us, SwiGLU 1408 x 2048 199 to 203 us (1400 TFLOP/s), a third of the multiplied rows being padding of the last
+// different sizes: product 2048 x 1408 101 to 105 us, SwiGLU 1408 x 2048 199 to 206 us (1400 TFLOP/s), 22 % of the multiplied rows being padding of the last
 // tile of a group; the copies alone take 72 and 128 us, the matrix instructions 41 and 91.  With half accumulators (four of 128
 // columns) 111 and 203, with 16 epilogue warps 131 and 242.
 // SPLIT: the reduction of a tile is shared by the g.split pairs of a cluster (one tile per cluster, one group): each pair leaves its
@@ -1034,7 +1035,7 @@ spice_status launch_gemm_e4m3(GemmE4m3Args g, const uint8_t *x, const uint8_t *w
     // Few rows: streamed weights, at the rate of HBM as long as the warp-wide products (400 per cycle and SM) keep up.  Streamed / by
     // pairs of CTAs, us, dense 2048 x 2816, 3584 x 20480, SwiGLU 2816 x 2048:  16 tokens 6.8/10.0, 18.6/26.7, 8.0/11.6;  32 tokens
     // 9.4/10.6, 28.6/27.5, 11.0/12.0;  64 tokens (when it took them) 14.7/12.0, 56/29.5, -/13.3.  64 groups of 2048 x 1408, SwiGLU
-    // 1408 x 2048:  96 rows 34.6/49, 65/94;  400 rows 38.8/50, 80/103;  768 rows 57/51, 116/103.
+    // 1408 x 2048:  96 rows 33.0/49, 59.6/94;  400 rows 37.8/50, 76.6/103;  768 rows 57/51, 116/103.
     if (g.G == 1 ? g.T <= 32 : rows <= 8) {
         CUtensorMap map_w;
         if (!tc_encode_map2_bytes(&map_w, w, (uint64_t)g.G * w_rows, (uint64_t)g.k, 128)) return SPICE_ERR_CUDA;

@@ -138,7 +138,8 @@ __global__ void __launch_bounds__(SMALL_THREADS) sort_small_kernel(const SortArg
 
 // ------------------------------------------------------------------------------------------------ many entries
 // A cluster counts: each of its warps owns a run of consecutive entries and a row of counters in shared memory; a first pass
-// counts, prefix sums over experts, blocks and warps turn the counters into places, a second pass hands the places out.
+// counts, prefix sums over experts, blocks and warps turn the counters into places, a second pass hands the places out.  24576 entries
+// of 64 experts 7.9 us; the other SMs wait, so the time grows with the entries: 65536 14.7, 262144 59.7 us.
 constexpr int SORT_CTAS = 8, SORT_THREADS = 1024, SORT_WARPS = SORT_THREADS / 32, SORT_KEPT = 8, SORT_EXPERTS = 1024;
 constexpr size_t sort_smem(int experts) { return (size_t)(SORT_WARPS * (experts | 1) + experts) * 4; }
 
@@ -407,7 +408,8 @@ __global__ void __launch_bounds__(256) grad_entry_kernel(const CombineGradArgs a
 }
 
 // A block per token, for many: dy is read once for all of the token's entries, three of which are on their way at once, with as many
-// blocks as fit (4096 x 6 x 2048: 35.8 us, 0.94 of the measured copy rate; four at a time and five blocks 43).
+// blocks as fit (4096 x 6 x 2048: 35.7 us, 0.95 of the measured copy rate; four at a time and five blocks 43.  fp32 67.8 us, at the copy
+// rate; rows in fp32 and dy in bf16 65.7, 0.99; rows in bf16 and dy in fp32 43.9, 0.83).
 template <bool DY32, bool ROW32>
 __global__ void __launch_bounds__(256, ROW32 || DY32 ? 4 : 8) grad_token_kernel(const CombineGradArgs a) {
     __shared__ float part[8][32];
